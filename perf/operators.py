@@ -170,7 +170,8 @@ def prepare(case, seed):
         state["stats"] = torch.empty(4, device=dev)
     else:
         state["ref"] = (taken + other).float()
-        state["offsets"] = torch.tensor(_pair_offsets(case), dtype=torch.int64, device=dev)
+        state["offsets"] = _pair_offsets(case)                                   # on the host, as the call takes them
+        state["offsets_gpu"] = torch.tensor(state["offsets"], dtype=torch.int64, device=dev)
         state["margins"] = torch.empty(case["pairs"], device=dev)
         state["loss"] = torch.empty(1, device=dev)
     return state
@@ -223,14 +224,14 @@ def _plain_preference(s, case):
     e, total, logp, _, counts = _softmax_parts(s["logits"], s["targets"], case["temperature"])
     away = torch.where(counts, logp.double() - s["ref"].double(), torch.zeros((), device=logp.device, dtype=torch.float64))
     run = torch.cat([torch.zeros(1, dtype=torch.float64, device=away.device), away.cumsum(0)])
-    sums = run[s["offsets"][1:]] - run[s["offsets"][:-1]]
+    sums = run[s["offsets_gpu"][1:]] - run[s["offsets_gpu"][:-1]]
     margin = _BETA * (sums[0::2] - sums[1::2])
     soft = lambda v: torch.clamp(v, min=0.0) + torch.log1p(torch.exp(-v.abs()))  # noqa: E731
     eps, scale = case["smooth"], 1.0 / case["pairs"]
     loss = scale * ((1.0 - eps) * soft(-margin) + eps * soft(margin)).sum()
     slope = scale * _BETA * (1.0 / (1.0 + torch.exp(-margin)) - (1.0 - eps))
     sign = torch.stack([slope, -slope], dim=1).reshape(-1)
-    lengths = s["offsets"][1:] - s["offsets"][:-1]
+    lengths = s["offsets_gpu"][1:] - s["offsets_gpu"][:-1]
     dlogp = torch.repeat_interleave(sign, lengths, output_size=case["tokens"]).float()
     _plain_dlogits(e, total, s["targets"], counts, dlogp, case["temperature"], s["dlogits"])
     return [loss.float().reshape(1), margin.float(), logp, s["dlogits"]]
@@ -375,7 +376,7 @@ def exact(case, seed):
         stats = torch.stack([(w * loss).sum(), (w * kl).sum(), (w * clipped).sum(), w.sum()])
         first, slope = [stats, logp], slope * w
     else:
-        offsets = s["offsets"].tolist()
+        offsets = s["offsets"]
         away = (logp - s["ref"].double()) * counts
         sums = torch.stack([away[a:b].sum() for a, b in zip(offsets, offsets[1:])])
         margin = _BETA * (sums[0::2] - sums[1::2])
