@@ -84,8 +84,10 @@ extern "C" {
 typedef enum {
     STAR_OK = 0,
     STAR_ERR_NULL = 1,   /* a required pointer is NULL                                        */
-    STAR_ERR_SHAPE = 2,  /* P < 0, W < 1, W > STAR_MAX_WORKERS, U < 0                          */
-    STAR_ERR_GROUP = 3,  /* empty group, id outside [0,W), duplicate id, offsets not monotone  */
+    STAR_ERR_SHAPE = 2,  /* P < 0, W < 1, W > STAR_MAX_WORKERS, U < 0; a negative or too large size, a row
+                            distance below the row's length, a workspace too small or misaligned        */
+    STAR_ERR_GROUP = 3,  /* empty group, id outside [0,W), duplicate id, offsets not monotone (of pairs:
+                            decreasing, or not from 0 to the number of tokens)                        */
     STAR_ERR_HPARAM = 4, /* non-finite lr / momentum / weight decay / coefficient, negative
                             staleness, unknown weighting mode                                   */
     STAR_ERR_DTYPE = 5,  /* unknown gradient dtype                                             */
@@ -478,6 +480,132 @@ star_status star_plan_claims(int32_t workgroups, int32_t tiles_per_claim, int64_
  * output.
  */
 star_status star_plan_even_split(int32_t workgroups, int64_t tiles, int64_t *first_tile, int32_t *count);
+
+/* ---- The worker's side: what makes a gradient row ----
+ *
+ * A worker that trains a language model hands the server a gradient.  The entry points below are the two ends of
+ * that which are no plain matrix product: the loss on the logits of the taken tokens, with its gradient, and the
+ * weight gradient from activations kept in 8 bits.  Groups of workers of different staleness are the ordinary case
+ * here (Section 4.2), so the policy loss compares the present policy with the one that sampled the tokens.
+ *
+ * Conventions of this part, besides those above: logits are `tokens` rows of `vocab` values of STAR_F32 or STAR_BF16,
+ * row t at element t * ld (ld >= vocab).  targets[t] is the token taken at row t.  A target outside [0, vocab) marks a
+ * token that does not count (a prompt, padding): its row is not read, its log-probability is reported as 0, its
+ * gradient row is zero.  dlogits has the shape and type of the logits, rows at t * ld_out; it may be the logits
+ * themselves (same address, same ld), but must not overlap them otherwise.  Addresses need the alignment of one
+ * element only.  With z = logits / temperature, logp = z[target] - lse, lse = log sum exp z.  Values of -inf (banned
+ * tokens) have probability 0; a row of nothing else, or one that holds NaN or +inf, has a log-probability of NaN.
+ * All arithmetic is fp32 or wider; a gradient is rounded once, to its own type.  Results are the same from run to run.
+ *
+ * `workspace`: device memory of at least the bytes that the matching *_workspace function returns for the call's
+ * sizes, aligned to 16 bytes, the call's own until its work has run (calls on one stream may share one); where that function returns 0 it may
+ * be NULL.  These calls allocate nothing, copy nothing and keep nothing, so that they can be captured into a HIP
+ * graph, and calls on different streams never meet.
+ */
+
+/* Log-probabilities of the taken tokens: logp_out[t] and, if not NULL, lse_out[t] (both device float[tokens]; 0 for a
+ * token that does not count). */
+star_status star_token_logprobs(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
+                                const int64_t *targets, float temperature, float *logp_out, float *lse_out,
+                                void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The gradient of any function of them: dlogits[t][j] = dlogp[t] / temperature ([j == targets[t]] - exp(z[t][j] - lse[t])).
+ *   lse   : device float[tokens], as star_token_logprobs returned it for the same logits and temperature
+ *   dlogp : device float[tokens], the function's derivatives; a row whose derivative is 0 is not read */
+star_status star_token_logprobs_grad(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
+                                     const int64_t *targets, float temperature, const float *lse, const float *dlogp,
+                                     void *dlogits, int64_t ld_out, void *hip_stream);
+
+/*
+ * Clipped policy loss with a KL term, and its gradient.  With r = exp(logp - old_logp) and c = r held within
+ * [1 - clip_low, 1 + clip_high], token t costs
+ *     l_t = max(-A_t r, -A_t c) + kl_coef (exp(d) - d - 1),   d = ref_logp - logp
+ * and loss = scale sum_t weights[t] l_t.  Where the two sides of the max are equal the unclipped one is taken.  A
+ * token of weight 0 does not count (as one whose target is out of range).
+ *   old_logp, ref_logp, advantages, weights : device float[tokens]; ref_logp may be NULL if kl_coef is 0, weights
+ *               may be NULL (all 1)
+ *   dlogits   : as above, or NULL: the loss alone
+ *   logp_out  : device float[tokens] or NULL
+ *   stats_out : device float[4]: loss, and sum_t scale weights[t] times the KL estimate exp(d) - d - 1 (0 without
+ *               kl_coef), times 1 where the clipped side is the larger, and times 1
+ * star_policy_loss_workspace: bytes for such a call.
+ */
+typedef struct {
+    float scale;
+    float clip_low, clip_high; /* >= 0; clip_high may be infinite                     */
+    float kl_coef;             /* >= 0                                                */
+    float temperature;         /* > 0                                                 */
+} star_policy_params;
+
+star_status star_policy_loss(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
+                             const int64_t *targets, const float *old_logp, const float *ref_logp,
+                             const float *advantages, const float *weights, const star_policy_params *params,
+                             void *dlogits, int64_t ld_out, float *logp_out, float *stats_out, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Preference loss on pairs of answers, and its gradient.  The rows of pair b are the tokens offsets[2b] ..
+ * offsets[2b+1] of the preferred answer and offsets[2b+1] .. offsets[2b+2] of the other (either may be empty).  With
+ *     s_b = beta (sum_preferred weights (logp - ref_logp) - sum_other weights (logp - ref_logp))
+ * loss = scale sum_b [-(1 - label_smoothing) log sigmoid(s_b) - label_smoothing log sigmoid(-s_b)].
+ *   offsets     : host int64[2 pairs + 1], not decreasing, first 0, last `tokens` (STAR_ERR_GROUP otherwise); read
+ *                 before the call returns
+ *   weights     : device float[tokens] or NULL (all 1); a token of weight 0 does not count
+ *   margins_out : device float[pairs] or NULL: s_b
+ *   loss_out    : device float[1]
+ * Sums over tokens and pairs are taken in 64 bits.
+ */
+typedef struct {
+    float scale;
+    float beta;
+    float label_smoothing; /* 0 to 1 */
+    float temperature;     /* > 0    */
+} star_preference_params;
+
+star_status star_preference_loss(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
+                                 const int64_t *targets, const float *ref_logp, const float *weights, int32_t pairs,
+                                 const int64_t *offsets, const star_preference_params *params, void *dlogits,
+                                 int64_t ld_out, float *logp_out, float *margins_out, float *loss_out,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
+size_t star_token_logprobs_workspace(star_dtype dtype, int64_t tokens, int64_t vocab);
+size_t star_policy_loss_workspace(star_dtype dtype, int64_t tokens, int64_t vocab);
+size_t star_preference_loss_workspace(star_dtype dtype, int64_t tokens, int64_t vocab, int32_t pairs);
+
+/*
+ * Activations kept in 8 bits for the backward pass.  x is `tokens` rows of `width` values, row t at t * ld.  The 32
+ * tokens 32 i .. 32 i + 31 of one column (fewer at the end) share a power of two 2^e, the smallest with
+ * max |x| <= 448 * 2^e (e at least -117); each is kept as e4m3 of x * 2^-e, rounded to nearest even.  Nothing is
+ * saturated; every kept value is a bf16 number, off by at most 2^-4 of the element, or by 2^-10 * 2^e where that is
+ * more.  inf and NaN are kept as NaN and do not count for the scale; finite values beyond 240 * 2^120 are held there.
+ * Layout of `packed` (star_act_bytes(tokens, width) bytes, aligned to 16): with B = ceil(tokens / 32) and C = width
+ * rounded up to a multiple of 16, bytes [B][C][32] (token fastest), then [B][C] biased exponents e + 127; columns from
+ * `width` on and tokens from `tokens` on are 0.
+ */
+size_t star_act_bytes(int64_t tokens, int64_t width);
+
+star_status star_act_pack(const void *x, star_dtype dtype, int64_t tokens, int64_t width, int64_t ld, void *packed,
+                          void *hip_stream);
+
+/* The kept values, as STAR_F32 or STAR_BF16 (both exact). */
+star_status star_act_unpack(const void *packed, int64_t tokens, int64_t width, void *out, star_dtype dtype, int64_t ld,
+                            void *hip_stream);
+
+/*
+ * Weight gradient of a linear layer y = x W^T whose input was kept by star_act_pack:
+ *     dw[n][k] = sum_t dy[t][n] x[t][k]         (accumulate nonzero: added to what dw holds)
+ * on the matrix cores, sums in fp32.
+ *   dy : device, `tokens` rows of `out` values of dy_dtype, row t at t * ld.  fp32 values are taken as three bf16
+ *        parts, which hold all of their 24 bits.
+ *   dw : device, out * width values of dw_dtype, contiguous -- a stretch of a worker's gradient row, at any
+ *        element of it.  Must not overlap the inputs.
+ * tokens == 0 gives 0 (or leaves dw as it is).
+ */
+star_status star_act_weight_grad(const void *dy, star_dtype dy_dtype, int64_t tokens, int64_t out, int64_t ld,
+                                 const void *packed, int64_t width, void *dw, star_dtype dw_dtype, int32_t accumulate,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
+size_t star_act_weight_grad_workspace(star_dtype dy_dtype, int64_t tokens, int64_t out, int64_t width);
 
 /* Bytes of internal device workspace one call of this shape uses at most (direct norm sums without an update need the
  * most: partial sums of up to 240 updates). */

@@ -17,6 +17,7 @@
 #include "star_kernels.h"
 #include "star_plan.h"
 #include "star_wait.h"
+#include "star_worker.h"
 
 namespace {
 
@@ -1004,6 +1005,28 @@ star_status run_gram(const void* const* grad_rows, int grad_dtype, int64_t P, in
 }
 
 }  // namespace
+
+// The calling thread's error text, for the worker-side entry points (star_worker_api.cpp), which throw nothing.
+namespace star {
+
+star_status set_error(star_status s, const char* text) {
+    try {
+        g_err = text;
+    } catch (...) {
+        g_err.clear();
+    }
+    return s;
+}
+
+star_status hip_error(hipError_t e, const char* what) {
+    try {
+        return hip_fail(e, what);
+    } catch (...) {
+        return set_error(STAR_ERR_DEVICE, "a HIP call failed");
+    }
+}
+
+}  // namespace star
 
 extern "C" {
 

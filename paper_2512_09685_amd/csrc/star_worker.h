@@ -1,0 +1,80 @@
+// Launch interface of the worker-side operators: loss on logits, activations in 8 bits, weight gradient.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+
+#include <cstdint>
+
+#include "star.h"
+
+namespace star {
+
+// What the C-ABI layer of these operators shares with that of the group update.
+star_status set_error(star_status s, const char* text);
+star_status hip_error(hipError_t e, const char* what);
+
+// ---------------------------------------------------------------- logits
+struct Logits {
+    const void* x;
+    int dtype;             // star_dtype
+    int64_t tokens, vocab, ld;
+    const int64_t* targets;
+    const float* weights;  // null: all 1; a token of weight 0 does not count
+    float inv_t;           // 1 / temperature
+};
+
+struct PolicyArgs {
+    const float *old_logp, *ref_logp, *advantages;
+    float scale, low, high, kl;   // ratio held within [low, high]
+};
+
+// logp, lse (may be null) of rows [first, first + count).
+hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* lse, void* workspace, hipStream_t stream);
+// dlogits of rows [first, first + count) from lse and dlogp.
+hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, const float* lse, const float* dlogp, void* dlogits,
+                                int64_t ld_out, hipStream_t stream);
+// logp and dlogits of the policy loss in one pass.
+hipError_t launch_policy(const Logits& l, const PolicyArgs& a, float* logp, void* dlogits, int64_t ld_out, void* workspace,
+                         hipStream_t stream);
+// The four sums of the policy loss from the log-probabilities.
+hipError_t launch_policy_stats(const Logits& l, const PolicyArgs& a, const float* logp, float* stats, void* workspace, hipStream_t stream);
+
+// Pairs of one launch: their offsets travel in the kernel arguments.
+constexpr int kPairsPerLaunch = 128;
+struct PairOffsets {
+    int64_t at[2 * kPairsPerLaunch + 1];
+};
+struct PreferenceArgs {
+    const float* ref_logp;
+    float scale, beta, smooth;
+};
+// Margins of `pairs` pairs, their tokens' derivatives and the terms of the loss (one double a pair).
+hipError_t launch_pairs(const Logits& l, const PreferenceArgs& a, const PairOffsets& offsets, int pairs, const float* logp, float* dlogp,
+                        float* margins, double* terms, hipStream_t stream);
+hipError_t launch_pair_loss(const double* terms, int pairs, float scale, float* loss, hipStream_t stream);
+
+// ---------------------------------------------------------------- saved activations
+constexpr int kActBlock = 32;    // tokens that share a scale
+constexpr int kActPad = 16;      // columns of the packed form come in multiples of this
+inline int64_t act_blocks(int64_t tokens) { return (tokens + kActBlock - 1) / kActBlock; }
+inline int64_t act_columns(int64_t width) { return (width + kActPad - 1) / kActPad * kActPad; }
+
+hipError_t launch_act_pack(const void* x, int dtype, int64_t tokens, int64_t width, int64_t ld, void* packed, hipStream_t stream);
+hipError_t launch_act_unpack(const void* packed, int64_t tokens, int64_t width, void* out, int dtype, int64_t ld, hipStream_t stream);
+
+// ---------------------------------------------------------------- weight gradient
+struct WeightGrad {
+    const void* dy;
+    int dy_dtype;
+    int64_t tokens, out, ld;
+    const void* packed;
+    int64_t width;
+    void* dw;
+    int dw_dtype;
+    bool accumulate;
+};
+// Parts that the tokens are cut into (each part's sums are written apart and joined by a second launch; 1: none).
+int weight_grad_parts(int dy_dtype, int64_t tokens, int64_t out, int64_t width);
+hipError_t launch_weight_grad(const WeightGrad& g, void* workspace, hipStream_t stream);
+
+}  // namespace star
