@@ -14,7 +14,9 @@ using star::set_error;
 constexpr int64_t kMostRows = (int64_t)1 << 22;     // rows of one launch: fewer than 2^32 threads
 constexpr int64_t kMostVocab = (int64_t)1 << 30;
 constexpr int64_t kMostElements = (int64_t)1 << 42;   // of one tensor: no byte offset leaves 63 bits
-constexpr int64_t kMostTiles = (int64_t)1 << 22;
+constexpr int64_t kMostTiles = (int64_t)1 << 22;      // of dw, 64 by 64 each
+constexpr int64_t kMostSummed = (int64_t)1 << 30;     // tokens that one weight gradient sums over
+constexpr int64_t kMostWidth = (int64_t)1 << 22;      // columns of a weight gradient: 32 rows of it stay within 31 bits of offset
 
 bool known(int dtype) { return dtype == STAR_F32 || dtype == STAR_BF16; }
 size_t bytes_of(int dtype) { return dtype == STAR_F32 ? 4 : 2; }
@@ -245,7 +247,8 @@ star_status star_act_weight_grad(const void* dy, star_dtype dy_dtype, int64_t to
         if (!on_grid(dy, bytes_of(dy_dtype))) return set_error(STAR_ERR_SHAPE, "an address is not a multiple of its element's size");
         if (!on_grid(packed, 16)) return set_error(STAR_ERR_SHAPE, "packed is not aligned to 16 bytes");
     }
-    if ((out + 63) / 64 * ((width + 63) / 64) > kMostTiles) return set_error(STAR_ERR_SHAPE, "dw is too large");
+    if (tokens > kMostSummed || width > kMostWidth || (out + 63) / 64 * ((width + 63) / 64) > kMostTiles)
+        return set_error(STAR_ERR_SHAPE, "tokens is above 2^30, width above 2^22, or dw is too large");
     STAR_CHECK(check_workspace(workspace, workspace_bytes, star_act_weight_grad_workspace(dy_dtype, tokens, out, width)));
     const star::WeightGrad g{dy, dy_dtype, tokens, out, ld, packed, width, dw, dw_dtype, accumulate != 0};
     STAR_LAUNCH(star::launch_weight_grad(g, workspace, static_cast<hipStream_t>(hip_stream)));
