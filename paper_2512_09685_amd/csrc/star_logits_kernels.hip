@@ -21,6 +21,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // 16 bytes of a row as VEC numbers, and back.
 struct ElemF32 {
     static constexpr int VEC = 4, BYTES = 4;
+    static constexpr uint32_t NOTHING = 0xff800000u;   // -inf, in every element of 4 bytes
     template <int K>
     static __device__ __forceinline__ float get(const u32x4& x) { return __uint_as_float(x[K]); }
     static __device__ __forceinline__ float one(const void* row, int64_t j) { return reinterpret_cast<const float*>(row)[j]; }
@@ -31,18 +32,23 @@ struct ElemF32 {
 };
 struct ElemBf16 {
     static constexpr int VEC = 8, BYTES = 2;
+    static constexpr uint32_t NOTHING = 0xff80ff80u;
     template <int K>
     static __device__ __forceinline__ float get(const u32x4& x) { return bf16_of<K>(x[K >> 1]); }
     static __device__ __forceinline__ float one(const void* row, int64_t j) {
         return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(row)[j] << 16);
     }
-    static __device__ __forceinline__ u32x4 pack(const float* v) {
-        u32x4 x;
+    static __device__ __forceinline__ u32x4 pack(const float* v) {   // (one instruction a pair, to nearest even, NaN stays NaN)
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        union {
+            bf16x2 pair[4];
+            u32x4 all;
+        } r;
         static_for<0, 4>([&](auto I) {
             constexpr int i = decltype(I)::value;
-            x[i] = bf16_bits_rne(v[2 * i]) | (bf16_bits_rne(v[2 * i + 1]) << 16);
+            r.pair[i] = bf16x2{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]};
         });
-        return x;
+        return r.all;
     }
     static __device__ __forceinline__ void put(void* row, int64_t j, float v) { reinterpret_cast<uint16_t*>(row)[j] = (uint16_t)bf16_bits_rne(v); }
 };
@@ -133,41 +139,48 @@ __device__ __forceinline__ MaxSum join_group(MaxSum a, float k, MaxSum* shared) 
     const float base = m == -INFINITY ? 0.f : m;
     float s = a.s * __builtin_amdgcn_exp2f((a.m - base) * k);
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    if constexpr (NT > 64) {
-        if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = MaxSum{m, s};
-        __syncthreads();
-        MaxSum all = shared[0];
-        for (int w = 1; w < NT / 64; ++w) all.m = fmaxf(all.m, shared[w].m);
-        const float top = all.m == -INFINITY ? 0.f : all.m;
-        all.s = 0.f;
-        for (int w = 0; w < NT / 64; ++w) all.s += shared[w].s * __builtin_amdgcn_exp2f((shared[w].m - top) * k);
-        return all;
-    } else {
-        return MaxSum{m, s};
-    }
+    constexpr int WAVES = NT / 64;
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = MaxSum{m, s};
+    __syncthreads();
+    // (every wave joins the waves' results for itself, one a lane)
+    const MaxSum w = shared[threadIdx.x % WAVES];
+    MaxSum all{w.m, 0.f};
+    for (int d = WAVES / 2; d; d >>= 1) all.m = fmaxf(all.m, __shfl_xor(all.m, d));
+    all.s = w.s * __builtin_amdgcn_exp2f((w.m - (all.m == -INFINITY ? 0.f : all.m)) * k);
+    for (int d = WAVES / 2; d; d >>= 1) all.s += __shfl_xor(all.s, d);
+    return all;
 }
 
-// dl_j = scaled * 2^((l_j - m) k), plus `c` at the target.
+// dl_j = scaled * 2^((l_j - m) k), plus `c` at the target: one chunk, one element.
+struct Slope {
+    float k, m, scaled, c;
+    int y;
+};
+template <class E>
+__device__ __forceinline__ u32x4 slope_chunk(const u32x4& x, const Slope& p, int first) {
+    float v[E::VEC];
+    static_for<0, E::VEC>([&](auto I) {
+        constexpr int n = decltype(I)::value;
+        v[n] = p.scaled * __builtin_amdgcn_exp2f((E::template get<n>(x) - p.m) * p.k);
+    });
+    const int at = p.y - first;
+    if (at >= 0 && at < E::VEC)
+        static_for<0, E::VEC>([&](auto I) { v[decltype(I)::value] += at == decltype(I)::value ? p.c : 0.f; });
+    return E::pack(v);
+}
+template <class E>
+__device__ __forceinline__ void slope_edge(const char* row, char* out, const RowSpan& sp, const Slope& p) {
+    if ((int)threadIdx.x >= sp.edge) return;
+    const int j = sp.edge_element(threadIdx.x);
+    const float v = p.scaled * __builtin_amdgcn_exp2f((E::one(row, j) - p.m) * p.k);
+    E::put(out, j, j == p.y ? v + p.c : v);
+}
 template <class E, int NT>
-__device__ __forceinline__ void write_row(const char* row, char* out, const RowSpan sp, float k, float m, float scaled, float c, int y) {
-    const int tid = threadIdx.x;
-    for (int i = tid; i < sp.chunks; i += NT) {
-        const u32x4 x = *(reinterpret_cast<const u32x4*>(row + sp.head * E::BYTES) + i);
-        float v[E::VEC];
-        static_for<0, E::VEC>([&](auto I) {
-            constexpr int n = decltype(I)::value;
-            v[n] = scaled * __builtin_amdgcn_exp2f((E::template get<n>(x) - m) * k);
-        });
-        const int at = y - sp.head - i * E::VEC;
-        if (at >= 0 && at < E::VEC)
-            static_for<0, E::VEC>([&](auto I) { v[decltype(I)::value] += at == decltype(I)::value ? c : 0.f; });
-        *(reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES) + i) = E::pack(v);
-    }
-    if (tid < sp.edge) {
-        const int j = sp.edge_element(tid);
-        const float v = scaled * __builtin_amdgcn_exp2f((E::one(row, j) - m) * k);
-        E::put(out, j, j == y ? v + c : v);
-    }
+__device__ __forceinline__ void write_row(const char* row, char* out, const RowSpan sp, const Slope& p) {
+    const u32x4* from = reinterpret_cast<const u32x4*>(row + sp.head * E::BYTES);
+    u32x4_any* to = reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES);
+    for (int i = threadIdx.x; i < sp.chunks; i += NT) to[i] = slope_chunk<E>(from[i], p, sp.head + i * E::VEC);
+    slope_edge<E>(row, out, sp, p);
 }
 
 template <class E, int NT>
@@ -212,7 +225,7 @@ __global__ __launch_bounds__(NT) void logits_row_kernel(const RowArgs a) {
     if constexpr (WORK == RowWork::Grad) {
         // p_j = 2^((l_j - lse temperature) k): the row's maximum is not known here, nor needed
         const float c = a.dlogp[t] * a.l.inv_t, m = a.lse_in[t] / a.l.inv_t;
-        write_row<E, NT>(row, out, sp, k, m, -c, c, (int)y);
+        write_row<E, NT>(row, out, sp, Slope{k, m, -c, c, (int)y});
     } else {
         const float ly = E::one(row, y);
         const MaxSum all = join_group<NT>(scan_row<E, NT>(row, sp, k), k, shared);
@@ -224,18 +237,104 @@ __global__ __launch_bounds__(NT) void logits_row_kernel(const RowArgs a) {
         if constexpr (WORK == RowWork::Policy) {
             const float w = a.policy.scale * (a.l.weights ? a.l.weights[t] : 1.f);
             const float c = w * policy_term(a.policy, t, logp).slope * a.l.inv_t;
-            write_row<E, NT>(row, out, sp, k, all.m, -c / all.s, c, (int)y);
+            write_row<E, NT>(row, out, sp, Slope{k, all.m, -c / all.s, c, (int)y});
         }
     }
+}
+
+// The chunks as they were loaded, for all that the compiler knows: it would keep every element of a bf16 row widened from one use to the
+// next, in twice the registers, for the sake of one instruction an element.
+template <int C>
+__device__ __forceinline__ void keep_packed(u32x4 (&x)[C]) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) asm volatile("" : "+v"(x[i]));
+}
+
+// The same with the whole row in registers, C chunks a thread: read once.
+template <class E, int NT, int C, RowWork WORK>
+__global__ __launch_bounds__(NT, C <= 8 ? 8 : 4) void logits_held_kernel(const RowArgs a) {
+    __shared__ MaxSum shared[NT / 64];
+    const int64_t t = a.first + blockIdx.x;
+    const int V = (int)a.l.vocab, tid = threadIdx.x;
+    const char* row = reinterpret_cast<const char*>(a.l.x) + t * a.l.ld * E::BYTES;
+    char* out = a.dlogits + t * a.ld_out * E::BYTES;
+    const int64_t y = a.l.targets[t];
+    const float k = kLog2e * a.l.inv_t;
+    if (!counts(a.l, t, y)) {
+        if (tid == 0) {
+            a.logp[t] = 0.f;
+            if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = 0.f;
+        }
+        if (WORK == RowWork::Policy) zero_row<E, NT>(out, V);
+        return;
+    }
+    const RowSpan sp = row_span<E>(row, V);
+    const u32x4* from = reinterpret_cast<const u32x4*>(row + sp.head * E::BYTES);
+    u32x4 x[C];
+    static_for<0, C>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        x[i] = u32x4{E::NOTHING, E::NOTHING, E::NOTHING, E::NOTHING};
+        if (tid + i * NT < sp.chunks) x[i] = __builtin_nontemporal_load(from + tid + i * NT);
+    });
+    const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
+    const float ly = E::one(row, y);
+    MaxSum mine{edge, 0.f};
+    static_for<0, C>([&](auto I) {
+        static_for<0, E::VEC>([&](auto J) { mine.m = fmaxf(mine.m, E::template get<decltype(J)::value>(x[decltype(I)::value])); });
+    });
+    const float base = mine.m == -INFINITY ? 0.f : mine.m;
+    mine.s = __builtin_amdgcn_exp2f((edge - base) * k);
+    keep_packed(x);
+    static_for<0, C>([&](auto I) {
+        static_for<0, E::VEC>([&](auto J) {
+            mine.s += __builtin_amdgcn_exp2f((E::template get<decltype(J)::value>(x[decltype(I)::value]) - base) * k);
+        });
+    });
+    const MaxSum all = join_group<NT>(mine, k, shared);
+    const float log_s = logf(all.s), logp = (ly - all.m) * a.l.inv_t - log_s;
+    if (tid == 0) {
+        a.logp[t] = logp;
+        if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = all.m * a.l.inv_t + log_s;
+    }
+    if constexpr (WORK == RowWork::Policy) {
+        const float w = a.policy.scale * (a.l.weights ? a.l.weights[t] : 1.f);
+        const float c = w * policy_term(a.policy, t, logp).slope * a.l.inv_t;
+        const Slope p{k, all.m, -c / all.s, c, (int)y};
+        keep_packed(x);
+        u32x4_any* to = reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES);
+        static_for<0, C>([&](auto I) {
+            constexpr int i = decltype(I)::value;
+            const int at = tid + i * NT;
+            if (at < sp.chunks) __builtin_nontemporal_store(slope_chunk<E>(x[i], p, sp.head + at * E::VEC), to + at);
+        });
+        if (tid < sp.edge) {
+            const int j = sp.edge_element(tid);
+            const float v = p.scaled * __builtin_amdgcn_exp2f((edge - p.m) * p.k);
+            E::put(out, j, j == p.y ? v + p.c : v);
+        }
+    }
+}
+
+template <class E, RowWork WORK>
+void launch_rows_of(const RowArgs& a, unsigned count, hipStream_t stream) {
+    const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;
+    if constexpr (WORK != RowWork::Grad) {
+        if (chunks <= 256) return logits_held_kernel<E, 256, 1, WORK><<<count, 256, 0, stream>>>(a);
+        if (chunks <= 512) return logits_held_kernel<E, 256, 2, WORK><<<count, 256, 0, stream>>>(a);
+        if (chunks <= 1024) return logits_held_kernel<E, 256, 4, WORK><<<count, 256, 0, stream>>>(a);
+        if (chunks <= 2048) return logits_held_kernel<E, 512, 4, WORK><<<count, 512, 0, stream>>>(a);
+        if (chunks <= 4096) return logits_held_kernel<E, 512, 8, WORK><<<count, 512, 0, stream>>>(a);
+        if (chunks <= 8192) return logits_held_kernel<E, 1024, 8, WORK><<<count, 1024, 0, stream>>>(a);
+        if (chunks <= 16384) return logits_held_kernel<E, 1024, 16, WORK><<<count, 1024, 0, stream>>>(a);
+    }
+    logits_row_kernel<E, 512, WORK><<<count, 512, 0, stream>>>(a);
 }
 
 template <RowWork WORK>
 hipError_t launch_rows(const RowArgs& a, int64_t count, hipStream_t stream) {
     if (count <= 0) return hipSuccess;
-    if (a.l.dtype == STAR_F32)
-        logits_row_kernel<ElemF32, 512, WORK><<<dim3((unsigned)count), 512, 0, stream>>>(a);
-    else
-        logits_row_kernel<ElemBf16, 512, WORK><<<dim3((unsigned)count), 512, 0, stream>>>(a);
+    if (a.l.dtype == STAR_F32) launch_rows_of<ElemF32, WORK>(a, (unsigned)count, stream);
+    else launch_rows_of<ElemBf16, WORK>(a, (unsigned)count, stream);
     return hipGetLastError();
 }
 
