@@ -17,6 +17,7 @@ namespace {
 typedef u32x4 u32x4_any __attribute__((aligned(2)));   // (see f32x4_any)
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int64_t kFewTokens = 128;   // up to this many rows are cut into sections
 
 // 16 bytes of a row as VEC numbers, and back.
 struct ElemF32 {
@@ -53,19 +54,20 @@ struct ElemBf16 {
     static __device__ __forceinline__ void put(void* row, int64_t j, float v) { reinterpret_cast<uint16_t*>(row)[j] = (uint16_t)bf16_bits_rne(v); }
 };
 
-// A row as whole 16-byte chunks at aligned addresses, and what is before and behind them: fewer than 2 VEC elements,
-// one a thread.  (An odd vocabulary puts every other row off 16 bytes.)
+// A row as whole 16-byte chunks at aligned addresses, and what is before and behind them, one element a thread.  (An odd
+// vocabulary puts the rows at any address.)  Workgroups of a row begin their chunks on whole cache lines, so that no two waves write
+// parts of one; single waves, with 64 threads for the rest, on 16 bytes.
 struct RowSpan {
     int head, chunks, edge;   // elements before the chunks, chunks, elements outside them
     int V;
     __device__ __forceinline__ int edge_element(int tid) const { return tid < head ? tid : V - edge + tid; }
 };
-template <class E>
+template <class E, int NT>
 __device__ __forceinline__ RowSpan row_span(const char* row, int V) {
+    constexpr int ALIGN = NT > 64 ? 128 : 16;
     RowSpan r;
     r.V = V;
-    const int off = (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / E::BYTES;
-    r.head = off < V ? off : V;
+    r.head = min((int)(-reinterpret_cast<uintptr_t>(row) & (ALIGN - 1)) / E::BYTES, V);
     r.chunks = (V - r.head) / E::VEC;
     r.edge = V - r.chunks * E::VEC;
     return r;
@@ -110,45 +112,75 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& a, int64_t t
     return p;
 }
 
-template <class E, int NT>
-__device__ __forceinline__ MaxSum scan_row(const char* row, const RowSpan sp, float k) {
-    MaxSum a{-INFINITY, 0.f};
-    const int tid = threadIdx.x;
-    for (int c = tid; c < sp.chunks; c += NT) {
-        const u32x4 x = *(reinterpret_cast<const u32x4*>(row + sp.head * E::BYTES) + c);
-        float m = a.m;
-        static_for<0, E::VEC>([&](auto I) { m = fmaxf(m, E::template get<decltype(I)::value>(x)); });
-        const float base = m == -INFINITY ? 0.f : m;
-        float s = a.s * __builtin_amdgcn_exp2f((a.m - base) * k);
-        static_for<0, E::VEC>([&](auto I) { s += __builtin_amdgcn_exp2f((E::template get<decltype(I)::value>(x) - base) * k); });
-        a = MaxSum{m, s};
-    }
-    if (tid < sp.edge) {
-        const float v = E::one(row, sp.edge_element(tid));
-        const float m = fmaxf(a.m, v), base = m == -INFINITY ? 0.f : m;
-        a = MaxSum{m, a.s * __builtin_amdgcn_exp2f((a.m - base) * k) + __builtin_amdgcn_exp2f((v - base) * k)};
-    }
-    return a;
+// What one thread sees of a row: C chunks in registers (those that it does not have hold -inf) and at most one element more.
+template <class E, int C>
+__device__ __forceinline__ float max_of(const u32x4 (&x)[C], float more) {
+    float m = more;
+    static_for<0, C>([&](auto I) {
+        static_for<0, E::VEC>([&](auto J) { m = fmaxf(m, E::template get<decltype(J)::value>(x[decltype(I)::value])); });
+    });
+    return m;
+}
+template <class E, int C>
+__device__ __forceinline__ float sum_from(const u32x4 (&x)[C], float more, float m, float k) {
+    const float base = m == -INFINITY ? 0.f : m;
+    float s = __builtin_amdgcn_exp2f((more - base) * k);
+    static_for<0, C>([&](auto I) {
+        static_for<0, E::VEC>([&](auto J) { s += __builtin_amdgcn_exp2f((E::template get<decltype(J)::value>(x[decltype(I)::value]) - base) * k); });
+    });
+    return s;
 }
 
+// The chunks as they were loaded, for all that the compiler knows: it would keep every element of a bf16 row widened from one use to the
+// next, in twice the registers, for the sake of one instruction an element.
+template <int C>
+__device__ __forceinline__ void keep_packed(u32x4 (&x)[C]) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) asm volatile("" : "+v"(x[i]));
+}
+
+// C chunks a thread from chunk `first` on, NT apart; what is beyond the row holds -inf.
+template <class E, int NT, int C>
+__device__ __forceinline__ void load_chunks(u32x4 (&x)[C], const char* row, const RowSpan& sp, int first) {
+    const u32x4* from = reinterpret_cast<const u32x4*>(row + sp.head * E::BYTES);
+    static_for<0, C>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        x[i] = u32x4{E::NOTHING, E::NOTHING, E::NOTHING, E::NOTHING};
+        if (first + i * NT < sp.chunks) x[i] = __builtin_nontemporal_load(from + first + i * NT);
+    });
+}
+
+// Over a wave; every lane gets the whole.
+template <int LANES = 64>
+__device__ __forceinline__ MaxSum join_wave(const MaxSum a, float k) {
+    float m = a.m;
+    for (int d = LANES / 2; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    float s = a.s * __builtin_amdgcn_exp2f((a.m - (m == -INFINITY ? 0.f : m)) * k);
+    for (int d = LANES / 2; d; d >>= 1) s += __shfl_xor(s, d);
+    return MaxSum{m, s};
+}
 // Over the workgroup, in a fixed order; every thread gets the whole.
 template <int NT>
-__device__ __forceinline__ MaxSum join_group(MaxSum a, float k, MaxSum* shared) {
-    float m = a.m;
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    const float base = m == -INFINITY ? 0.f : m;
-    float s = a.s * __builtin_amdgcn_exp2f((a.m - base) * k);
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    constexpr int WAVES = NT / 64;
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = MaxSum{m, s};
+__device__ __forceinline__ MaxSum join_group(const MaxSum a, float k, MaxSum* shared) {
+    const MaxSum w = join_wave(a, k);
+    if constexpr (NT == 64) return w;
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = w;
     __syncthreads();
-    // (every wave joins the waves' results for itself, one a lane)
-    const MaxSum w = shared[threadIdx.x % WAVES];
-    MaxSum all{w.m, 0.f};
-    for (int d = WAVES / 2; d; d >>= 1) all.m = fmaxf(all.m, __shfl_xor(all.m, d));
-    all.s = w.s * __builtin_amdgcn_exp2f((w.m - (all.m == -INFINITY ? 0.f : all.m)) * k);
-    for (int d = WAVES / 2; d; d >>= 1) all.s += __shfl_xor(all.s, d);
-    return all;
+    return join_wave<NT / 64>(shared[threadIdx.x % (NT / 64)], k);   // (every wave for itself, one result a lane)
+}
+
+// A long row, chunk by chunk, four of them under way at a time.
+template <class E, int NT>
+__device__ __forceinline__ MaxSum scan_row(const char* row, const RowSpan& sp, float k) {
+    MaxSum a{-INFINITY, 0.f};
+    if ((int)threadIdx.x < sp.edge) a = MaxSum{E::one(row, sp.edge_element(threadIdx.x)), 1.f};
+    for (int c = threadIdx.x; c < sp.chunks; c += 4 * NT) {
+        u32x4 x[4];
+        load_chunks<E, NT>(x, row, sp, c);
+        const float m = max_of<E>(x, a.m), base = m == -INFINITY ? 0.f : m;
+        a = MaxSum{m, a.s * __builtin_amdgcn_exp2f((a.m - base) * k) + sum_from<E>(x, -INFINITY, m, k)};
+    }
+    return a;
 }
 
 // dl_j = scaled * 2^((l_j - m) k), plus `c` at the target: one chunk, one element.
@@ -168,174 +200,208 @@ __device__ __forceinline__ u32x4 slope_chunk(const u32x4& x, const Slope& p, int
         static_for<0, E::VEC>([&](auto I) { v[decltype(I)::value] += at == decltype(I)::value ? p.c : 0.f; });
     return E::pack(v);
 }
+template <class E, int NT, int C>
+__device__ __forceinline__ void store_slopes(const u32x4 (&x)[C], char* out, const RowSpan& sp, const Slope& p, int first) {
+    u32x4_any* to = reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES);
+    static_for<0, C>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        const int at = first + i * NT;
+        if (at < sp.chunks) __builtin_nontemporal_store(slope_chunk<E>(x[i], p, sp.head + at * E::VEC), to + at);
+    });
+}
 template <class E>
-__device__ __forceinline__ void slope_edge(const char* row, char* out, const RowSpan& sp, const Slope& p) {
-    if ((int)threadIdx.x >= sp.edge) return;
-    const int j = sp.edge_element(threadIdx.x);
-    const float v = p.scaled * __builtin_amdgcn_exp2f((E::one(row, j) - p.m) * p.k);
+__device__ __forceinline__ void store_slope(float l, char* out, const RowSpan& sp, const Slope& p, int tid) {
+    const int j = sp.edge_element(tid);
+    const float v = p.scaled * __builtin_amdgcn_exp2f((l - p.m) * p.k);
     E::put(out, j, j == p.y ? v + p.c : v);
 }
+
+// Zeros to the chunks of [from, to) by NT threads, and to the rest of the row if they begin it.
 template <class E, int NT>
-__device__ __forceinline__ void write_row(const char* row, char* out, const RowSpan sp, const Slope& p) {
-    const u32x4* from = reinterpret_cast<const u32x4*>(row + sp.head * E::BYTES);
-    u32x4_any* to = reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES);
-    for (int i = threadIdx.x; i < sp.chunks; i += NT) to[i] = slope_chunk<E>(from[i], p, sp.head + i * E::VEC);
-    slope_edge<E>(row, out, sp, p);
+__device__ __forceinline__ void zero_row(char* out, int V, int tid, int from = 0, int to = 0x7fffffff) {
+    const RowSpan sp = row_span<E, NT>(out, V);
+    u32x4* chunk = reinterpret_cast<u32x4*>(out + sp.head * E::BYTES);
+    for (int i = from + tid; i < min(to, sp.chunks); i += NT) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, chunk + i);
+    if (from == 0 && tid < sp.edge) E::put(out, sp.edge_element(tid), 0.f);
 }
 
-template <class E, int NT>
-__device__ __forceinline__ void zero_row(char* out, int V) {
-    const RowSpan sp = row_span<E>(out, V);
-    for (int i = threadIdx.x; i < sp.chunks; i += NT) *(reinterpret_cast<u32x4*>(out + sp.head * E::BYTES) + i) = u32x4{0, 0, 0, 0};
-    if ((int)threadIdx.x < sp.edge) E::put(out, sp.edge_element(threadIdx.x), 0.f);
-}
-
-enum class RowWork { Logprobs, Policy, Grad };
+enum class RowWork { Logprobs, Policy };
 
 struct RowArgs {
     Logits l;
     PolicyArgs policy;
     float *logp, *lse;
-    const float *lse_in, *dlogp;
     char* dlogits;
-    int64_t ld_out, first;
+    int64_t ld_out, first, rows;   // rows [first, first + rows)
+    const float *lse_in, *dlogp;   // of the gradient alone
+    MaxSum* parts;                 // of rows that several workgroups share: [rows][sections]
+    float* picked;                 // of such rows: the target's logit, which a gradient in place would be written over
+    int sections;
+    float* stats;
+    unsigned int* ticket;          // cleared for the launch behind this one; null: it needs none
 };
 
-// A workgroup a row; the row is read a second time for its gradient.
-template <class E, int NT, RowWork WORK>
-__global__ __launch_bounds__(NT) void logits_row_kernel(const RowArgs a) {
-    __shared__ MaxSum shared[NT / 64];
-    const int64_t t = a.first + blockIdx.x;
-    const int V = (int)a.l.vocab;
-    const char* row = reinterpret_cast<const char*>(a.l.x) + t * a.l.ld * E::BYTES;
-    char* out = a.dlogits + t * a.ld_out * E::BYTES;
-    const int64_t y = a.l.targets[t];
-    const float k = kLog2e * a.l.inv_t;
-    bool live = counts(a.l, t, y);
-    if (WORK == RowWork::Grad && live) live = a.dlogp[t] != 0.f;
-    if (!live) {
-        if (WORK != RowWork::Grad && threadIdx.x == 0) {
-            a.logp[t] = 0.f;
-            if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = 0.f;
-        }
-        if (WORK != RowWork::Logprobs) zero_row<E, NT>(out, V);
-        return;
-    }
-    const RowSpan sp = row_span<E>(row, V);
-    if constexpr (WORK == RowWork::Grad) {
-        // p_j = 2^((l_j - lse temperature) k): the row's maximum is not known here, nor needed
-        const float c = a.dlogp[t] * a.l.inv_t, m = a.lse_in[t] / a.l.inv_t;
-        write_row<E, NT>(row, out, sp, Slope{k, m, -c, c, (int)y});
-    } else {
-        const float ly = E::one(row, y);
-        const MaxSum all = join_group<NT>(scan_row<E, NT>(row, sp, k), k, shared);
-        const float log_s = logf(all.s), logp = (ly - all.m) * a.l.inv_t - log_s;
-        if (threadIdx.x == 0) {
-            a.logp[t] = logp;
-            if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = all.m * a.l.inv_t + log_s;
-        }
-        if constexpr (WORK == RowWork::Policy) {
-            const float w = a.policy.scale * (a.l.weights ? a.l.weights[t] : 1.f);
-            const float c = w * policy_term(a.policy, t, logp).slope * a.l.inv_t;
-            write_row<E, NT>(row, out, sp, Slope{k, all.m, -c / all.s, c, (int)y});
-        }
-    }
+__device__ __forceinline__ const char* row_of(const RowArgs& a, int64_t t, int bytes) {
+    return reinterpret_cast<const char*>(a.l.x) + t * a.l.ld * bytes;
+}
+__device__ __forceinline__ float scaled_weight(const RowArgs& a, int64_t t) { return a.policy.scale * (a.l.weights ? a.l.weights[t] : 1.f); }
+
+// logp from the row's maximum and sum; `ly`: the target's logit.
+__device__ __forceinline__ float logp_of(const RowArgs& a, const MaxSum& all, float ly) { return (ly - all.m) * a.l.inv_t - logf(all.s); }
+
+__device__ __forceinline__ void clear_ticket(const RowArgs& a) {
+    if (a.ticket && blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0u;
 }
 
-// The chunks as they were loaded, for all that the compiler knows: it would keep every element of a bf16 row widened from one use to the
-// next, in twice the registers, for the sake of one instruction an element.
-template <int C>
-__device__ __forceinline__ void keep_packed(u32x4 (&x)[C]) {
-#pragma unroll
-    for (int i = 0; i < C; ++i) asm volatile("" : "+v"(x[i]));
-}
-
-// The same with the whole row in registers, C chunks a thread: read once.
-template <class E, int NT, int C, RowWork WORK>
-__global__ __launch_bounds__(NT, C <= 8 ? 8 : 4) void logits_held_kernel(const RowArgs a) {
+// The whole row in registers, C chunks a thread: read once, written once.  NT threads a row, ROWS rows a workgroup.
+// Registers and not LDS, because a unit has three times as much of them; rows of up to 8 chunks a thread let two
+// workgroups of 1024 threads share a unit, of which one reads while the other writes (8192 x 65536, bf16: 376 us with
+// one of them, 392 with this form's two and all 8192 rows read -- 2.1 GB, 5.4 TB/s, what a copy of that length takes;
+// writing in bursts by a common clock, two rows in turn in two sets of registers, changed nothing: half of this traffic is writes,
+// and what the memory-side cache takes at once it has to give back to the DRAM during the reads).
+template <class E, int NT, int C, int ROWS, RowWork WORK>
+__global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(const RowArgs a) {
     __shared__ MaxSum shared[NT / 64];
-    const int64_t t = a.first + blockIdx.x;
-    const int V = (int)a.l.vocab, tid = threadIdx.x;
-    const char* row = reinterpret_cast<const char*>(a.l.x) + t * a.l.ld * E::BYTES;
+    clear_ticket(a);
+    const int V = (int)a.l.vocab, tid = threadIdx.x % NT;
+    const int64_t in = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
+    if (ROWS > 1 && in >= a.rows) return;
+    const int64_t t = a.first + in, y = a.l.targets[t];
+    const char* row = row_of(a, t, E::BYTES);
     char* out = a.dlogits + t * a.ld_out * E::BYTES;
-    const int64_t y = a.l.targets[t];
     const float k = kLog2e * a.l.inv_t;
     if (!counts(a.l, t, y)) {
         if (tid == 0) {
             a.logp[t] = 0.f;
             if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = 0.f;
         }
-        if (WORK == RowWork::Policy) zero_row<E, NT>(out, V);
+        if (WORK == RowWork::Policy) zero_row<E, NT>(out, V, tid);
         return;
     }
-    const RowSpan sp = row_span<E>(row, V);
-    const u32x4* from = reinterpret_cast<const u32x4*>(row + sp.head * E::BYTES);
+    const RowSpan sp = row_span<E, NT>(row, V);
     u32x4 x[C];
-    static_for<0, C>([&](auto I) {
-        constexpr int i = decltype(I)::value;
-        x[i] = u32x4{E::NOTHING, E::NOTHING, E::NOTHING, E::NOTHING};
-        if (tid + i * NT < sp.chunks) x[i] = __builtin_nontemporal_load(from + tid + i * NT);
-    });
-    const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
-    const float ly = E::one(row, y);
-    MaxSum mine{edge, 0.f};
-    static_for<0, C>([&](auto I) {
-        static_for<0, E::VEC>([&](auto J) { mine.m = fmaxf(mine.m, E::template get<decltype(J)::value>(x[decltype(I)::value])); });
-    });
-    const float base = mine.m == -INFINITY ? 0.f : mine.m;
-    mine.s = __builtin_amdgcn_exp2f((edge - base) * k);
+    load_chunks<E, NT>(x, row, sp, tid);
+    const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY, ly = E::one(row, y);
+    MaxSum mine{max_of<E>(x, edge), 0.f};
     keep_packed(x);
-    static_for<0, C>([&](auto I) {
-        static_for<0, E::VEC>([&](auto J) {
-            mine.s += __builtin_amdgcn_exp2f((E::template get<decltype(J)::value>(x[decltype(I)::value]) - base) * k);
-        });
-    });
+    mine.s = sum_from<E>(x, edge, mine.m, k);
     const MaxSum all = join_group<NT>(mine, k, shared);
-    const float log_s = logf(all.s), logp = (ly - all.m) * a.l.inv_t - log_s;
+    const float logp = logp_of(a, all, ly);
     if (tid == 0) {
         a.logp[t] = logp;
-        if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = all.m * a.l.inv_t + log_s;
+        if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = all.m * a.l.inv_t + logf(all.s);
     }
     if constexpr (WORK == RowWork::Policy) {
-        const float w = a.policy.scale * (a.l.weights ? a.l.weights[t] : 1.f);
-        const float c = w * policy_term(a.policy, t, logp).slope * a.l.inv_t;
+        const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp).slope * a.l.inv_t;
         const Slope p{k, all.m, -c / all.s, c, (int)y};
         keep_packed(x);
-        u32x4_any* to = reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES);
-        static_for<0, C>([&](auto I) {
-            constexpr int i = decltype(I)::value;
-            const int at = tid + i * NT;
-            if (at < sp.chunks) __builtin_nontemporal_store(slope_chunk<E>(x[i], p, sp.head + at * E::VEC), to + at);
-        });
-        if (tid < sp.edge) {
-            const int j = sp.edge_element(tid);
-            const float v = p.scaled * __builtin_amdgcn_exp2f((edge - p.m) * p.k);
-            E::put(out, j, j == p.y ? v + p.c : v);
-        }
+        store_slopes<E, NT>(x, out, sp, p, tid);
+        if (tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
     }
 }
 
+// Rows too long for that: a workgroup a row, read a second time for its gradient, from its end, which the caches still hold.
+constexpr int kScanThreads = 512;
 template <class E, RowWork WORK>
-void launch_rows_of(const RowArgs& a, unsigned count, hipStream_t stream) {
-    const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;
-    if constexpr (WORK != RowWork::Grad) {
-        if (chunks <= 256) return logits_held_kernel<E, 256, 1, WORK><<<count, 256, 0, stream>>>(a);
-        if (chunks <= 512) return logits_held_kernel<E, 256, 2, WORK><<<count, 256, 0, stream>>>(a);
-        if (chunks <= 1024) return logits_held_kernel<E, 256, 4, WORK><<<count, 256, 0, stream>>>(a);
-        if (chunks <= 2048) return logits_held_kernel<E, 512, 4, WORK><<<count, 512, 0, stream>>>(a);
-        if (chunks <= 4096) return logits_held_kernel<E, 512, 8, WORK><<<count, 512, 0, stream>>>(a);
-        if (chunks <= 8192) return logits_held_kernel<E, 1024, 8, WORK><<<count, 1024, 0, stream>>>(a);
-        if (chunks <= 16384) return logits_held_kernel<E, 1024, 16, WORK><<<count, 1024, 0, stream>>>(a);
+__global__ __launch_bounds__(kScanThreads) void logits_scan_kernel(const RowArgs a) {
+    constexpr int NT = kScanThreads;
+    __shared__ MaxSum shared[NT / 64];
+    clear_ticket(a);
+    const int V = (int)a.l.vocab, tid = threadIdx.x;
+    const int64_t t = a.first + blockIdx.x, y = a.l.targets[t];
+    const char* row = row_of(a, t, E::BYTES);
+    char* out = a.dlogits + t * a.ld_out * E::BYTES;
+    const float k = kLog2e * a.l.inv_t;
+    if (!counts(a.l, t, y)) {
+        if (tid == 0) {
+            a.logp[t] = 0.f;
+            if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = 0.f;
+        }
+        if (WORK == RowWork::Policy) zero_row<E, NT>(out, V, tid);
+        return;
     }
-    logits_row_kernel<E, 512, WORK><<<count, 512, 0, stream>>>(a);
+    const RowSpan sp = row_span<E, NT>(row, V);
+    const float ly = E::one(row, y);
+    const MaxSum all = join_group<NT>(scan_row<E, NT>(row, sp, k), k, shared);
+    const float logp = logp_of(a, all, ly);
+    if (tid == 0) {
+        a.logp[t] = logp;
+        if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = all.m * a.l.inv_t + logf(all.s);
+    }
+    if constexpr (WORK == RowWork::Policy) {
+        const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp).slope * a.l.inv_t;
+        const Slope p{k, all.m, -c / all.s, c, (int)y};
+        for (int first = (sp.chunks - 1) / (4 * NT) * (4 * NT); first >= 0; first -= 4 * NT) {
+            u32x4 x[4];
+            load_chunks<E, NT>(x, row, sp, first + tid);
+            store_slopes<E, NT>(x, out, sp, p, first + tid);
+        }
+        if (tid < sp.edge) store_slope<E>(E::one(row, sp.edge_element(tid)), out, sp, p, tid);
+    }
 }
 
-template <RowWork WORK>
-hipError_t launch_rows(const RowArgs& a, int64_t count, hipStream_t stream) {
-    if (count <= 0) return hipSuccess;
-    if (a.l.dtype == STAR_F32) launch_rows_of<ElemF32, WORK>(a, (unsigned)count, stream);
-    else launch_rows_of<ElemBf16, WORK>(a, (unsigned)count, stream);
-    return hipGetLastError();
+// Few rows: a row's chunks are cut into sections of NT C, a workgroup each.  First launch: every section's maximum and sum.
+constexpr int kSectionThreads = 256;
+template <class E, int C>
+__global__ __launch_bounds__(kSectionThreads) void logits_part_kernel(const RowArgs a) {
+    constexpr int NT = kSectionThreads;
+    __shared__ MaxSum shared[NT / 64];
+    const int V = (int)a.l.vocab, tid = threadIdx.x, section = (int)(blockIdx.x % (unsigned)a.sections);
+    const int64_t in = blockIdx.x / (unsigned)a.sections, t = a.first + in, y = a.l.targets[t];
+    if (!counts(a.l, t, y)) return;
+    const char* row = row_of(a, t, E::BYTES);
+    const float k = kLog2e * a.l.inv_t;
+    const RowSpan sp = row_span<E, NT>(row, V);
+    u32x4 x[C];
+    load_chunks<E, NT>(x, row, sp, section * NT * C + tid);
+    const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
+    MaxSum mine{max_of<E>(x, edge), 0.f};
+    keep_packed(x);
+    mine.s = sum_from<E>(x, edge, mine.m, k);
+    const MaxSum all = join_group<NT>(mine, k, shared);
+    if (tid == 0) a.parts[in * a.sections + section] = all;
+    if (tid == 0 && section == 0) a.picked[in] = E::one(row, y);
+}
+
+// The sections of a row joined by one thread, 16 of them on their way at a time; and by a wave, one a lane.
+__device__ __forceinline__ MaxSum join_parts(const RowArgs& a, int64_t in, float k) {
+    const MaxSum* p = a.parts + in * a.sections;
+    MaxSum all{-INFINITY, 0.f};
+    for (int first = 0; first < a.sections; first += 16) {
+        MaxSum x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = first + i < a.sections ? p[first + i] : MaxSum{-INFINITY, 0.f};
+        float m = all.m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m = fmaxf(m, x[i].m);
+        const float base = m == -INFINITY ? 0.f : m;
+        float s = all.s * __builtin_amdgcn_exp2f((all.m - base) * k);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += x[i].s * __builtin_amdgcn_exp2f((x[i].m - base) * k);
+        all = MaxSum{m, s};
+    }
+    return all;
+}
+__device__ __forceinline__ MaxSum join_parts_by_wave(const RowArgs& a, int64_t in, float k) {
+    const MaxSum* p = a.parts + in * a.sections;
+    MaxSum mine{-INFINITY, 0.f};
+    for (int i = threadIdx.x & 63; i < a.sections; i += 64) {
+        const MaxSum x = p[i];
+        const float m = fmaxf(mine.m, x.m), base = m == -INFINITY ? 0.f : m;
+        mine = MaxSum{m, mine.s * __builtin_amdgcn_exp2f((mine.m - base) * k) + x.s * __builtin_amdgcn_exp2f((x.m - base) * k)};
+    }
+    return join_wave(mine, k);
+}
+
+// Second launch of the log-probabilities: a thread a row.
+__global__ __launch_bounds__(64) void logits_join_kernel(const RowArgs a) {
+    const int64_t in = (int64_t)blockIdx.x * 64 + threadIdx.x, t = a.first + in;
+    if (in >= a.rows) return;
+    const int64_t y = a.l.targets[t];
+    const bool live = counts(a.l, t, y);
+    const MaxSum all = live ? join_parts(a, in, kLog2e * a.l.inv_t) : MaxSum{0.f, 1.f};
+    a.logp[t] = live ? logp_of(a, all, a.picked[in]) : 0.f;
+    if (a.lse) a.lse[t] = live ? all.m * a.l.inv_t + logf(all.s) : 0.f;
 }
 
 // ---------------------------------------------------------------- sums over tokens
@@ -353,22 +419,113 @@ __device__ __forceinline__ double group_sum(double x, double* shared) {
     return s;
 }
 
-__global__ __launch_bounds__(kSumThreads) void policy_stats_kernel(const Logits l, const PolicyArgs a, const float* logp, float* stats) {
+// What the tokens t0, t0 + step, ... add to the four sums of the policy loss.
+__device__ __forceinline__ void add_policy_terms(double (&sum)[4], const Logits& l, const PolicyArgs& a, int64_t t, float logp) {
+    const PolicyTerm p = policy_term(a, t, logp);
+    const double w = l.weights ? (double)l.weights[t] : 1.0;
+    sum[0] += w * p.loss;
+    sum[1] += w * p.kl;
+    sum[2] += w * p.clipped;
+    sum[3] += w;
+}
+
+// Second launch of the policy loss on few rows: every section's gradient, and, by one workgroup more, the log-probabilities and
+// sums.
+template <class E, int C>
+__global__ __launch_bounds__(kSectionThreads) void policy_section_kernel(const RowArgs a) {
+    constexpr int NT = kSectionThreads;
+    __shared__ double shared[NT / 64];
+    const int V = (int)a.l.vocab, tid = threadIdx.x, section = (int)(blockIdx.x % (unsigned)a.sections);
+    const int64_t in = blockIdx.x / (unsigned)a.sections;
+    const float k = kLog2e * a.l.inv_t;
+    if (in >= a.rows) {
+        double sum[4] = {0, 0, 0, 0};
+        for (int64_t t = tid; t < a.rows; t += NT) {
+            const int64_t y = a.l.targets[t];
+            const bool live = counts(a.l, t, y);
+            const float logp = live ? logp_of(a, join_parts(a, t, k), a.picked[t]) : 0.f;
+            a.logp[t] = logp;
+            if (live) add_policy_terms(sum, a.l, a.policy, t, logp);
+        }
+        for (int i = 0; i < 4; ++i) {
+            const double s = group_sum(sum[i], shared);
+            if (tid == 0) a.stats[i] = (float)(s * a.policy.scale);
+        }
+        return;
+    }
+    const int64_t t = in, y = a.l.targets[t];
+    const char* row = row_of(a, t, E::BYTES);
+    char* out = a.dlogits + t * a.ld_out * E::BYTES;
+    const int first = section * NT * C;
+    if (!counts(a.l, t, y)) {
+        // (the output's own chunks, which need not lie as the row's do)
+        zero_row<E, NT>(out, V, tid, first, section + 1 == a.sections ? 0x7fffffff : first + NT * C);
+        return;
+    }
+    const RowSpan sp = row_span<E, NT>(row, V);
+    u32x4 x[C];
+    load_chunks<E, NT>(x, row, sp, first + tid);
+    const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
+    const MaxSum all = join_parts_by_wave(a, in, k);
+    const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp_of(a, all, a.picked[in])).slope * a.l.inv_t;
+    const Slope p{k, all.m, -c / all.s, c, (int)y};
+    store_slopes<E, NT>(x, out, sp, p, first + tid);
+    if (section == 0 && tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
+}
+
+// The gradient alone, which needs nothing of the rest of its row: NT threads to a section of C chunks each, ROWS rows a workgroup.
+template <class E, int NT, int C, int ROWS>
+__global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) {
+    const int V = (int)a.l.vocab, tid = threadIdx.x % NT, section = (int)(blockIdx.x % (unsigned)a.sections);
+    const int64_t in = (int64_t)(blockIdx.x / (unsigned)a.sections) * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
+    if (ROWS > 1 && in >= a.rows) return;
+    const int64_t t = a.first + in, y = a.l.targets[t];
+    const char* row = row_of(a, t, E::BYTES);
+    char* out = a.dlogits + t * a.ld_out * E::BYTES;
+    const float d = a.dlogp[t];
+    const int first = section * NT * C;
+    if (!counts(a.l, t, y) || d == 0.f) {
+        zero_row<E, NT>(out, V, tid, first, section + 1 == a.sections ? 0x7fffffff : first + NT * C);
+        return;
+    }
+    const RowSpan sp = row_span<E, NT>(row, V);
+    u32x4 x[C];
+    load_chunks<E, NT>(x, row, sp, first + tid);
+    const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
+    // p_j = 2^((l_j - lse temperature) k): the row's maximum is not known here, nor needed
+    const float c = d * a.l.inv_t;
+    const Slope p{kLog2e * a.l.inv_t, a.lse_in[t] / a.l.inv_t, -c, c, (int)y};
+    store_slopes<E, NT>(x, out, sp, p, first + tid);
+    if (section == 0 && tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
+}
+
+// Workspace of the sums: a ticket, then four doubles a workgroup.
+constexpr int kStatsGroups = 64;
+
+__global__ __launch_bounds__(kSumThreads) void policy_stats_kernel(const Logits l, const PolicyArgs a, const float* logp, float* stats,
+                                                                   unsigned int* ticket, double* sums) {
     __shared__ double shared[kSumThreads / 64];
+    __shared__ bool last;
     double sum[4] = {0, 0, 0, 0};
-    for (int64_t t = threadIdx.x; t < l.tokens; t += kSumThreads) {
-        if (!counts(l, t, l.targets[t])) continue;
-        const PolicyTerm p = policy_term(a, t, logp[t]);
-        const double w = l.weights ? (double)l.weights[t] : 1.0;
-        sum[0] += w * p.loss;
-        sum[1] += w * p.kl;
-        sum[2] += w * p.clipped;
-        sum[3] += w;
+    for (int64_t t = (int64_t)blockIdx.x * kSumThreads + threadIdx.x; t < l.tokens; t += (int64_t)gridDim.x * kSumThreads)
+        if (counts(l, t, l.targets[t])) add_policy_terms(sum, l, a, t, logp[t]);
+    for (int i = 0; i < 4; ++i) sum[i] = group_sum(sum[i], shared);
+    if (gridDim.x > 1) {
+        // the workgroup that comes last joins all of them, in their own order
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < 4; ++i) __hip_atomic_store(sums + 4 * blockIdx.x + i, sum[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
+        }
+        __syncthreads();
+        if (!last) return;
+        for (int i = 0; i < 4; ++i) {
+            double mine = 0.0;
+            if (threadIdx.x < gridDim.x) mine = __hip_atomic_load(sums + 4 * threadIdx.x + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            sum[i] = group_sum(mine, shared);
+        }
     }
-    for (int i = 0; i < 4; ++i) {
-        const double s = group_sum(sum[i], shared);
-        if (threadIdx.x == 0) stats[i] = (float)(s * a.scale);
-    }
+    if (threadIdx.x == 0)
+        for (int i = 0; i < 4; ++i) stats[i] = (float)(sum[i] * a.scale);
 }
 
 // A workgroup a pair.
@@ -413,15 +570,138 @@ __global__ __launch_bounds__(kBlock) void pair_loss_kernel(const double* terms, 
     if (threadIdx.x == 0) *loss = (float)(sum * scale);
 }
 
+// ---------------------------------------------------------------- launches
+template <class E>
+int64_t chunks_of(const Logits& l) {
+    return (l.vocab + E::VEC - 1) / E::VEC;
+}
+int64_t chunks_of(int dtype, int64_t vocab) { return dtype == STAR_F32 ? (vocab + 3) / 4 : (vocab + 7) / 8; }
+
+// Few rows are cut into sections, of the largest size that still makes two workgroups a compute unit of them.
+struct Sections {
+    int chunks_a_thread, count;   // 0: rows are not cut
+};
+Sections sections_of(int dtype, int64_t tokens, int64_t vocab) {
+    const int64_t chunks = chunks_of(dtype, vocab);
+    if (tokens > kFewTokens || chunks < 2048) return Sections{0, 0};
+    int c = 8;
+    while (c > 1 && tokens * ((chunks + kSectionThreads * c - 1) / (kSectionThreads * c)) < 512) c /= 2;
+    return Sections{c, (int)((chunks + kSectionThreads * c - 1) / (kSectionThreads * c))};
+}
+
+template <class E, class F>
+void for_section(const Sections& s, F&& launch) {
+    if (s.chunks_a_thread == 8) launch(std::integral_constant<int, 8>{});
+    else if (s.chunks_a_thread == 4) launch(std::integral_constant<int, 4>{});
+    else if (s.chunks_a_thread == 2) launch(std::integral_constant<int, 2>{});
+    else launch(std::integral_constant<int, 1>{});
+}
+
+template <class E, RowWork WORK>
+void launch_rows_of(const RowArgs& a, hipStream_t stream) {
+    const int64_t chunks = chunks_of<E>(a.l);
+    const unsigned rows = (unsigned)a.rows, fours = (rows + 3) / 4;
+    if (chunks <= 64) return logits_held_kernel<E, 64, 1, 4, WORK><<<fours, 256, 0, stream>>>(a);
+    if (chunks <= 128) return logits_held_kernel<E, 64, 2, 4, WORK><<<fours, 256, 0, stream>>>(a);
+    if (chunks <= 256) return logits_held_kernel<E, 64, 4, 4, WORK><<<fours, 256, 0, stream>>>(a);
+    if (chunks <= 512) return logits_held_kernel<E, 64, 8, 4, WORK><<<fours, 256, 0, stream>>>(a);
+    if (chunks <= 1024) return logits_held_kernel<E, 256, 4, 1, WORK><<<rows, 256, 0, stream>>>(a);
+    if (chunks <= 2048) return logits_held_kernel<E, 256, 8, 1, WORK><<<rows, 256, 0, stream>>>(a);
+    if (chunks <= 4096) return logits_held_kernel<E, 512, 8, 1, WORK><<<rows, 512, 0, stream>>>(a);
+    if (chunks <= 8192) return logits_held_kernel<E, 1024, 8, 1, WORK><<<rows, 1024, 0, stream>>>(a);
+    if constexpr (WORK == RowWork::Policy)
+        if (chunks <= 16384) return logits_held_kernel<E, 1024, 16, 1, WORK><<<rows, 1024, 0, stream>>>(a);
+    logits_scan_kernel<E, WORK><<<rows, kScanThreads, 0, stream>>>(a);
+}
+
+template <class E>
+void launch_grad_of(RowArgs a, hipStream_t stream) {
+    const int64_t chunks = chunks_of<E>(a.l);
+    const unsigned rows = (unsigned)a.rows;
+    a.sections = 1;
+    if (chunks <= 128) return logits_grad_kernel<E, 64, 2, 4><<<(rows + 3) / 4, 256, 0, stream>>>(a);
+    if (chunks <= 512) return logits_grad_kernel<E, 64, 8, 4><<<(rows + 3) / 4, 256, 0, stream>>>(a);
+    const bool few = a.rows * chunks < 512 * 2048;   // (fewer than two workgroups a unit with sections of 2048 chunks)
+    a.sections = (int)(few ? (chunks + 511) / 512 : (chunks + 2047) / 2048);
+    const unsigned grid = rows * (unsigned)a.sections;
+    if (few) logits_grad_kernel<E, 256, 2, 1><<<grid, 256, 0, stream>>>(a);
+    else logits_grad_kernel<E, 256, 8, 1><<<grid, 256, 0, stream>>>(a);
+}
+
+// Workspace of rows in sections: their results, then the targets' logits.
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+size_t parts_bytes(int dtype, int64_t tokens, int64_t vocab) {
+    return round16(sizeof(MaxSum) * (size_t)tokens * (size_t)sections_of(dtype, tokens, vocab).count);
+}
+size_t section_bytes(int dtype, int64_t tokens, int64_t vocab) {
+    const size_t parts = parts_bytes(dtype, tokens, vocab);
+    return parts ? parts + round16(sizeof(float) * (size_t)tokens) : 0;
+}
+
+// Workspace of the policy loss: ticket | sums of the workgroups | sections | log-probabilities.
+struct PolicySpace {
+    size_t sums, parts, logp, total;
+};
+PolicySpace policy_space(int dtype, int64_t tokens, int64_t vocab) {
+    PolicySpace s;
+    s.sums = 16;
+    s.parts = s.sums + sizeof(double) * 4 * kStatsGroups;
+    s.logp = s.parts + section_bytes(dtype, tokens, vocab);
+    s.total = s.logp + round16(sizeof(float) * (size_t)tokens);
+    return s;
+}
+template <class T>
+T* at(void* workspace, size_t offset) {
+    return reinterpret_cast<T*>(reinterpret_cast<char*>(workspace) + offset);
+}
+
+// Launches hold at most this many rows (sections of a row are workgroups of their own).
+template <class F>
+hipError_t in_launches(RowArgs a, int64_t first, int64_t count, F&& launch) {
+    constexpr int64_t kRows = (int64_t)1 << 21;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kRows, ((int64_t)1 << 23) / std::max<int64_t>(1, chunks_of(a.l.dtype, a.l.vocab) / 512)));
+    for (a.first = first; count > 0; a.first += a.rows, count -= a.rows) {
+        a.rows = std::min(count, most);
+        launch(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 }  // namespace
 
-hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* lse, void*, hipStream_t stream) {
+size_t logprobs_workspace(int dtype, int64_t tokens, int64_t vocab) {
+    return section_bytes(dtype, tokens, vocab);
+}
+size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab) { return policy_space(dtype, tokens, vocab).total; }
+
+hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* lse, void* workspace, hipStream_t stream) {
     RowArgs a{};
     a.l = l;
     a.logp = logp;
     a.lse = lse;
-    a.first = first;
-    return launch_rows<RowWork::Logprobs>(a, count, stream);
+    const Sections s = workspace ? sections_of(l.dtype, count, l.vocab) : Sections{0, 0};
+    if (s.count > 1) {
+        a.first = first;
+        a.rows = count;
+        a.parts = at<MaxSum>(workspace, 0);
+        a.picked = at<float>(workspace, parts_bytes(l.dtype, count, l.vocab));
+        a.sections = s.count;
+        const unsigned grid = (unsigned)(count * s.count), joins = (unsigned)((count + 63) / 64);
+        auto both = [&](auto elem) {
+            typedef decltype(elem) E;
+            for_section<E>(s, [&](auto C) { logits_part_kernel<E, decltype(C)::value><<<grid, kSectionThreads, 0, stream>>>(a); });
+            logits_join_kernel<<<joins, 64, 0, stream>>>(a);
+        };
+        if (l.dtype == STAR_F32) both(ElemF32{});
+        else both(ElemBf16{});
+        return hipGetLastError();
+    }
+    return in_launches(a, first, count, [&](const RowArgs& r) {
+        if (l.dtype == STAR_F32) launch_rows_of<ElemF32, RowWork::Logprobs>(r, stream);
+        else launch_rows_of<ElemBf16, RowWork::Logprobs>(r, stream);
+    });
 }
 
 hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, const float* lse, const float* dlogp, void* dlogits,
@@ -432,22 +712,48 @@ hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, c
     a.dlogp = dlogp;
     a.dlogits = reinterpret_cast<char*>(dlogits);
     a.ld_out = ld_out;
-    a.first = first;
-    return launch_rows<RowWork::Grad>(a, count, stream);
+    return in_launches(a, first, count, [&](const RowArgs& r) {
+        if (l.dtype == STAR_F32) launch_grad_of<ElemF32>(r, stream);
+        else launch_grad_of<ElemBf16>(r, stream);
+    });
 }
 
-hipError_t launch_policy(const Logits& l, const PolicyArgs& p, float* logp, void* dlogits, int64_t ld_out, void*, hipStream_t stream) {
+hipError_t launch_policy(const Logits& l, const PolicyArgs& p, float* logp, void* dlogits, int64_t ld_out, float* stats, void* workspace,
+                         hipStream_t stream) {
     RowArgs a{};
     a.l = l;
     a.policy = p;
     a.logp = logp;
     a.dlogits = reinterpret_cast<char*>(dlogits);
     a.ld_out = ld_out;
-    return launch_rows<RowWork::Policy>(a, l.tokens, stream);
-}
-
-hipError_t launch_policy_stats(const Logits& l, const PolicyArgs& a, const float* logp, float* stats, void*, hipStream_t stream) {
-    policy_stats_kernel<<<dim3(1), kSumThreads, 0, stream>>>(l, a, logp, stats);
+    const PolicySpace space = policy_space(l.dtype, l.tokens, l.vocab);
+    if (!a.logp && l.tokens > 0) a.logp = at<float>(workspace, space.logp);
+    const Sections s = sections_of(l.dtype, l.tokens, l.vocab);
+    if (s.count > 1 && l.tokens > 0 && dlogits) {
+        a.rows = l.tokens;
+        a.parts = at<MaxSum>(workspace, space.parts);
+        a.picked = at<float>(workspace, space.parts + parts_bytes(l.dtype, l.tokens, l.vocab));
+        a.sections = s.count;
+        a.stats = stats;
+        const unsigned grid = (unsigned)(l.tokens * s.count);
+        auto both = [&](auto elem) {
+            typedef decltype(elem) E;
+            for_section<E>(s, [&](auto C) { logits_part_kernel<E, decltype(C)::value><<<grid, kSectionThreads, 0, stream>>>(a); });
+            for_section<E>(s, [&](auto C) { policy_section_kernel<E, decltype(C)::value><<<grid + 1, kSectionThreads, 0, stream>>>(a); });
+        };
+        if (l.dtype == STAR_F32) both(ElemF32{});
+        else both(ElemBf16{});
+        return hipGetLastError();
+    }
+    const int64_t groups = std::min<int64_t>(kStatsGroups, (l.tokens + 4 * kSumThreads - 1) / (4 * kSumThreads));
+    a.ticket = groups > 1 ? at<unsigned int>(workspace, 0) : nullptr;
+    const hipError_t e = in_launches(a, 0, l.tokens, [&](const RowArgs& r) {
+        if (!dlogits) l.dtype == STAR_F32 ? launch_rows_of<ElemF32, RowWork::Logprobs>(r, stream) : launch_rows_of<ElemBf16, RowWork::Logprobs>(r, stream);
+        else l.dtype == STAR_F32 ? launch_rows_of<ElemF32, RowWork::Policy>(r, stream) : launch_rows_of<ElemBf16, RowWork::Policy>(r, stream);
+    });
+    if (e != hipSuccess) return e;
+    policy_stats_kernel<<<dim3((unsigned)std::max<int64_t>(1, groups)), kSumThreads, 0, stream>>>(l, p, a.logp, stats, a.ticket,
+                                                                                                 groups > 1 ? at<double>(workspace, space.sums) : nullptr);
     return hipGetLastError();
 }
 

@@ -28,16 +28,18 @@ struct PolicyArgs {
     float scale, low, high, kl;   // ratio held within [low, high]
 };
 
-// logp, lse (may be null) of rows [first, first + count).
+// Workspace bytes of the launches below.
+size_t logprobs_workspace(int dtype, int64_t tokens, int64_t vocab);
+size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab);
+
+// logp, lse (may be null) of rows [first, first + count).  Without a workspace a row is one workgroup's.
 hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* lse, void* workspace, hipStream_t stream);
 // dlogits of rows [first, first + count) from lse and dlogp.
 hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, const float* lse, const float* dlogp, void* dlogits,
                                 int64_t ld_out, hipStream_t stream);
-// logp and dlogits of the policy loss in one pass.
-hipError_t launch_policy(const Logits& l, const PolicyArgs& a, float* logp, void* dlogits, int64_t ld_out, void* workspace,
+// logp (may be null), dlogits (may be null) and the four sums of the policy loss.
+hipError_t launch_policy(const Logits& l, const PolicyArgs& a, float* logp, void* dlogits, int64_t ld_out, float* stats, void* workspace,
                          hipStream_t stream);
-// The four sums of the policy loss from the log-probabilities.
-hipError_t launch_policy_stats(const Logits& l, const PolicyArgs& a, const float* logp, float* stats, void* workspace, hipStream_t stream);
 
 // Pairs of one launch: their offsets travel in the kernel arguments.
 constexpr int kPairsPerLaunch = 128;

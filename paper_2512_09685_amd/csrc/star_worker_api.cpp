@@ -60,18 +60,19 @@ star::Logits make_logits(const void* x, int dtype, int64_t tokens, int64_t vocab
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-// Workspace of the preference loss: terms [pairs] double, then lse, dlogp, logp [tokens] float.
+// Workspace of the preference loss: terms [pairs] double, then lse, dlogp, logp [tokens] float, then that of the log-probabilities.
 struct PreferenceSpace {
-    size_t terms, lse, dlogp, logp, total;
+    size_t terms, lse, dlogp, logp, rows, total;
 };
-PreferenceSpace preference_space(int64_t tokens, int32_t pairs) {
+PreferenceSpace preference_space(int dtype, int64_t tokens, int64_t vocab, int32_t pairs) {
     PreferenceSpace s;
     const size_t each = round16(sizeof(float) * (size_t)tokens);
     s.terms = 0;
     s.lse = round16(sizeof(double) * (size_t)pairs);
     s.dlogp = s.lse + each;
     s.logp = s.dlogp + each;
-    s.total = s.logp + each;
+    s.rows = s.logp + each;
+    s.total = s.rows + round16(star::logprobs_workspace(dtype, tokens, vocab));
     return s;
 }
 
@@ -95,15 +96,21 @@ T* at(void* workspace, size_t offset) {
 
 extern "C" {
 
-size_t star_token_logprobs_workspace(star_dtype, int64_t, int64_t) { return 0; }
-
-size_t star_policy_loss_workspace(star_dtype, int64_t tokens, int64_t) {
-    return tokens > 0 && tokens <= kMostRows ? round16(sizeof(float) * (size_t)tokens) : 0;
+static bool logits_fit(int dtype, int64_t tokens, int64_t vocab) {
+    return known(dtype) && tokens > 0 && tokens <= kMostRows && vocab > 0 && vocab <= kMostVocab;
 }
 
-size_t star_preference_loss_workspace(star_dtype, int64_t tokens, int64_t, int32_t pairs) {
-    if (tokens < 0 || tokens > kMostRows || pairs < 0) return 0;
-    return preference_space(tokens, pairs).total;
+size_t star_token_logprobs_workspace(star_dtype dtype, int64_t tokens, int64_t vocab) {
+    return logits_fit(dtype, tokens, vocab) ? star::logprobs_workspace(dtype, tokens, vocab) : 0;
+}
+
+size_t star_policy_loss_workspace(star_dtype dtype, int64_t tokens, int64_t vocab) {
+    return logits_fit(dtype, tokens, vocab) ? star::policy_workspace(dtype, tokens, vocab) : 0;
+}
+
+size_t star_preference_loss_workspace(star_dtype dtype, int64_t tokens, int64_t vocab, int32_t pairs) {
+    if ((tokens != 0 && !logits_fit(dtype, tokens, vocab)) || pairs < 0) return 0;
+    return preference_space(dtype, tokens, vocab, pairs).total;
 }
 
 star_status star_token_logprobs(const void* logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld, const int64_t* targets,
@@ -150,10 +157,7 @@ star_status star_policy_loss(const void* logits, star_dtype dtype, int64_t token
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, weights, params->temperature);
     const star::PolicyArgs a{old_logp, ref_logp, advantages, params->scale, 1.f - params->clip_low, 1.f + params->clip_high, params->kl_coef};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    float* logp = logp_out ? logp_out : static_cast<float*>(workspace);
-    if (dlogits) STAR_LAUNCH(star::launch_policy(l, a, logp, dlogits, ld_out, workspace, stream));
-    else STAR_LAUNCH(star::launch_logprobs(l, 0, tokens, logp, nullptr, workspace, stream));
-    STAR_LAUNCH(star::launch_policy_stats(l, a, logp, stats_out, workspace, stream));
+    STAR_LAUNCH(star::launch_policy(l, a, logp_out, dlogits, ld_out, stats_out, workspace, stream));
     return STAR_OK;
 }
 
@@ -172,7 +176,7 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
     if (offsets[0] != 0 || offsets[2 * (int64_t)pairs] != tokens) return set_error(STAR_ERR_GROUP, "offsets must run from 0 to tokens");
     for (int64_t i = 0; i < 2 * (int64_t)pairs; ++i)
         if (offsets[i + 1] < offsets[i]) return set_error(STAR_ERR_GROUP, "offsets decrease");
-    const PreferenceSpace space = preference_space(tokens, pairs);
+    const PreferenceSpace space = preference_space(dtype, tokens, vocab, pairs);
     STAR_CHECK(check_workspace(workspace, workspace_bytes, space.total));
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, weights, params->temperature);
     const star::PreferenceArgs a{ref_logp, params->scale, params->beta, params->label_smoothing};
@@ -180,12 +184,13 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
     double* terms = at<double>(workspace, space.terms);
     float *lse = at<float>(workspace, space.lse), *dlogp = at<float>(workspace, space.dlogp);
     float* logp = logp_out ? logp_out : at<float>(workspace, space.logp);
+    void* rows = space.total > space.rows ? at<char>(workspace, space.rows) : nullptr;
     for (int32_t first = 0; first < pairs; first += star::kPairsPerLaunch) {
         const int n = std::min<int32_t>(star::kPairsPerLaunch, pairs - first);
         star::PairOffsets o{};
         for (int i = 0; i <= 2 * n; ++i) o.at[i] = offsets[2 * (int64_t)first + i];
         const int64_t from = o.at[0], count = o.at[2 * n] - from;
-        STAR_LAUNCH(star::launch_logprobs(l, from, count, logp, dlogits ? lse : nullptr, nullptr, stream));
+        STAR_LAUNCH(star::launch_logprobs(l, from, count, logp, dlogits ? lse : nullptr, count == tokens ? rows : nullptr, stream));
         STAR_LAUNCH(star::launch_pairs(l, a, o, n, logp, dlogits ? dlogp : nullptr, margins_out ? margins_out + first : nullptr, terms + first,
                                        stream));
         if (dlogits) STAR_LAUNCH(star::launch_logprobs_grad(l, from, count, lse, dlogp, dlogits, ld_out, stream));

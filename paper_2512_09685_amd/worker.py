@@ -5,6 +5,7 @@ passed in (a uint8 tensor of at least the bytes the C header's ``*_workspace`` f
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional
 
 import numpy as np
@@ -57,62 +58,72 @@ def _check(status: int):
         raise StarError(status, last_error())
 
 
-_codes = None
+# torch's own names, looked up once: these checks are most of what a call on a few rows costs the host (a call of
+# star_token_logprobs on one row 6.4 us with them in their first form, the kernel itself 2).
+_torch = _codes = _f32 = _i64 = None
+
+
+def _names():
+    global _torch, _codes, _f32, _i64
+    import torch
+    _torch, _f32, _i64 = torch, torch.float32, torch.int64
+    _codes = {torch.float32: F32, torch.bfloat16: BF16}
 
 
 def _dtype(x, what: str) -> int:
-    global _codes
     if _codes is None:
-        import torch
-        _codes = {torch.float32: F32, torch.bfloat16: BF16}
+        _names()
     code = _codes.get(x.dtype)
     if code is None:
         raise TypeError(f"{what} must be a float32 or bfloat16 tensor")
     return code
 
 
-def _matrix(x, what: str, shape=None):
+def _matrix(x, what: str, rows=None, columns=None):
     """(address, rows, columns, distance of the rows) of a 2-D tensor whose rows are contiguous."""
-    if x.dim() != 2 or (shape is not None and tuple(x.shape) != shape):
-        raise ValueError(f"{what} must be a 2-D tensor" + ("" if shape is None else f" of shape {shape}"))
+    if x.dim() != 2 or (rows is not None and (x.size(0) != rows or x.size(1) != columns)):
+        raise ValueError(f"{what} must be a 2-D tensor" + ("" if rows is None else f" of shape ({rows}, {columns})"))
     rows, columns = x.shape
+    if x.is_contiguous():
+        return x.data_ptr(), rows, columns, columns
     step = x.stride(0) if rows > 1 else columns
-    if columns > 1 and x.stride(1) != 1 or step < columns:
+    if (columns > 1 and x.stride(1) != 1) or step < columns:
         raise ValueError(f"the rows of {what} must be contiguous and must not overlap")
     return x.data_ptr(), rows, columns, step
 
 
-def _floats(x, n: int, what: str, device):
-    import torch
+def _vector(x, dtype, n: int, what: str, device: int):
+    """Address of a contiguous vector of n; ``device``: the index of the logits' device."""
     if x is None:
         return None
-    if x.dtype != torch.float32 or x.dim() != 1 or x.shape[0] != n or not x.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous float32 tensor [{n}]")
-    if x.device != device:
+    if x.dtype is not dtype or x.dim() != 1 or x.size(0) != n or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor [{n}]")
+    if x.get_device() != device:
         raise ValueError(f"{what} must be on the logits' device")
     return x.data_ptr()
 
 
 def _logits(logits, targets, dlogits=None):
-    """The arguments that every call on logits begins with, and those of its gradient."""
-    import torch
+    """What every call on logits begins with: (address, dtype code, tokens, vocab, ld, targets), its gradient's (address,
+    ld), and the device's index."""
     code = _dtype(logits, "logits")
     x, tokens, vocab, ld = _matrix(logits, "logits")
-    if targets.dtype != torch.int64 or targets.dim() != 1 or targets.shape[0] != tokens or not targets.is_contiguous():
-        raise ValueError(f"targets must be a contiguous int64 tensor [{tokens}]")
-    if targets.device != logits.device:
-        raise ValueError("targets must be on the logits' device")
+    device = logits.get_device()
     out, ld_out = None, ld
     if dlogits is not None:
-        if dlogits.dtype != logits.dtype or dlogits.device != logits.device:
+        if dlogits.dtype is not logits.dtype or dlogits.get_device() != device:
             raise TypeError("dlogits must have the logits' type and device")
-        out, _, _, ld_out = _matrix(dlogits, "dlogits", (tokens, vocab))
-        if out == x:
-            ld_out = ld if tokens <= 1 else ld_out
-    return (x, code, tokens, vocab, ld, targets.data_ptr()), (out, ld_out)
+        out, _, _, ld_out = _matrix(dlogits, "dlogits", tokens, vocab)
+    return (x, code, tokens, vocab, ld, _vector(targets, _i64, tokens, "targets", device)), (out, ld_out), device
 
 
-def _workspace(given, need: int, device, stream):
+@functools.lru_cache(maxsize=4096)
+def _need(name: str, *sizes) -> int:
+    """Workspace bytes of a call, by its sizes."""
+    return getattr(_library(), name)(*sizes)
+
+
+def _workspace(given, need: int, device: int, stream):
     """(address, bytes, the tensor to keep until the call is enqueued)."""
     if given is not None:
         if given.element_size() != 1 or not given.is_contiguous():
@@ -120,14 +131,14 @@ def _workspace(given, need: int, device, stream):
         return given.data_ptr(), given.numel(), given
     if need == 0:
         return None, 0, None
-    import torch
-    if stream is None or device.type != "cuda":
-        w = torch.empty(need, dtype=torch.uint8, device=device)
+    where = "cpu" if device < 0 else device
+    if stream is None or device < 0:
+        w = _torch.empty(need, dtype=_torch.uint8, device=where)
     else:
         # on the call's own stream, so that the memory is not handed out again before the call has run
-        s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)
-        with torch.cuda.stream(s):
-            w = torch.empty(need, dtype=torch.uint8, device=device)
+        s = stream if isinstance(stream, _torch.cuda.Stream) else _torch.cuda.ExternalStream(int(stream), device=where)
+        with _torch.cuda.stream(s):
+            w = _torch.empty(need, dtype=_torch.uint8, device=where)
     return w.data_ptr(), need, w
 
 
@@ -137,10 +148,10 @@ def star_token_logprobs(logits, targets, logp_out, *, lse_out=None, temperature:
     normaliser (float32 [tokens]); both 0 where the target is outside the vocabulary.  ``logits``: float32 or bfloat16
     [tokens, vocab], rows at any distance; ``targets``: int64 [tokens]."""
     lib = _library()
-    head, _ = _logits(logits, targets)
-    _, code, tokens, vocab, _, _ = head
-    logp, lse = _floats(logp_out, tokens, "logp_out", logits.device), _floats(lse_out, tokens, "lse_out", logits.device)
-    w, size, _keep = _workspace(workspace, lib.star_token_logprobs_workspace(code, tokens, vocab), logits.device, stream)
+    head, _, device = _logits(logits, targets)
+    tokens = head[2]
+    logp, lse = _vector(logp_out, _f32, tokens, "logp_out", device), _vector(lse_out, _f32, tokens, "lse_out", device)
+    w, size, _keep = _workspace(workspace, _need("star_token_logprobs_workspace", *head[1:4]), device, stream)
     _check(lib.star_token_logprobs(*head, temperature, logp, lse, w, size, _stream_handle(stream)))
 
 
@@ -148,10 +159,10 @@ def star_token_logprobs_grad(logits, targets, lse, dlogp, dlogits, *, temperatur
     """``dlogits`` of a function whose derivatives by the log-probabilities are ``dlogp`` (float32 [tokens]); ``lse`` as
     ``star_token_logprobs`` left it.  ``dlogits`` may be ``logits``."""
     lib = _library()
-    head, out = _logits(logits, targets, dlogits)
+    head, out, device = _logits(logits, targets, dlogits)
     tokens = head[2]
-    _check(lib.star_token_logprobs_grad(*head, temperature, _floats(lse, tokens, "lse", logits.device),
-                                        _floats(dlogp, tokens, "dlogp", logits.device), *out, _stream_handle(stream)))
+    _check(lib.star_token_logprobs_grad(*head, temperature, _vector(lse, _f32, tokens, "lse", device),
+                                        _vector(dlogp, _f32, tokens, "dlogp", device), *out, _stream_handle(stream)))
 
 
 def star_policy_loss(logits, targets, old_logp, advantages, stats_out, *, dlogits=None, ref_logp=None, weights=None,
@@ -160,14 +171,13 @@ def star_policy_loss(logits, targets, old_logp, advantages, stats_out, *, dlogit
     """Clipped policy loss with a KL term and, if ``dlogits`` is given, its gradient.  ``stats_out``: float32 [4]: loss,
     KL estimate, clipped share, weight, each summed with ``scale * weights``.  ``scale``: None = 1 / tokens."""
     lib = _library()
-    head, out = _logits(logits, targets, dlogits)
-    _, code, tokens, vocab, _, _ = head
-    device = logits.device
-    p = _PolicyParams(1.0 / max(tokens, 1) if scale is None else scale, clip_low, clip_high, kl_coef, temperature)
-    old, ref = _floats(old_logp, tokens, "old_logp", device), _floats(ref_logp, tokens, "ref_logp", device)
-    adv, wts = _floats(advantages, tokens, "advantages", device), _floats(weights, tokens, "weights", device)
-    logp, stats = _floats(logp_out, tokens, "logp_out", device), _floats(stats_out, 4, "stats_out", device)
-    w, size, _keep = _workspace(workspace, lib.star_policy_loss_workspace(code, tokens, vocab), device, stream)
+    head, out, device = _logits(logits, targets, dlogits)
+    n = head[2]
+    p = _PolicyParams(1.0 / max(n, 1) if scale is None else scale, clip_low, clip_high, kl_coef, temperature)
+    old, ref = _vector(old_logp, _f32, n, "old_logp", device), _vector(ref_logp, _f32, n, "ref_logp", device)
+    adv, wts = _vector(advantages, _f32, n, "advantages", device), _vector(weights, _f32, n, "weights", device)
+    logp, stats = _vector(logp_out, _f32, n, "logp_out", device), _vector(stats_out, _f32, 4, "stats_out", device)
+    w, size, _keep = _workspace(workspace, _need("star_policy_loss_workspace", *head[1:4]), device, stream)
     _check(lib.star_policy_loss(*head, old, ref, adv, wts, ctypes.byref(p), *out, logp, stats, w, size,
                                 _stream_handle(stream)))
 
@@ -179,31 +189,30 @@ def star_preference_loss(logits, targets, ref_logp, offsets, loss_out, *, dlogit
     2 pairs + 1 row numbers (preferred, other, preferred, ...); ``loss_out``: float32 [1]; ``margins_out``: float32
     [pairs].  ``scale``: None = 1 / pairs."""
     lib = _library()
-    head, out = _logits(logits, targets, dlogits)
-    _, code, tokens, vocab, _, _ = head
-    device = logits.device
+    head, out, device = _logits(logits, targets, dlogits)
+    n = head[2]
     at = np.ascontiguousarray(offsets, dtype=np.int64)
     if at.ndim != 1 or at.shape[0] % 2 != 1:
         raise ValueError("offsets must hold 2 pairs + 1 numbers")
     pairs = (at.shape[0] - 1) // 2
     p = _PreferenceParams(1.0 / max(pairs, 1) if scale is None else scale, beta, label_smoothing, temperature)
-    ref, wts = _floats(ref_logp, tokens, "ref_logp", device), _floats(weights, tokens, "weights", device)
-    logp, margins = _floats(logp_out, tokens, "logp_out", device), _floats(margins_out, pairs, "margins_out", device)
-    loss = _floats(loss_out, 1, "loss_out", device)
-    w, size, _keep = _workspace(workspace, lib.star_preference_loss_workspace(code, tokens, vocab, pairs), device, stream)
+    ref, wts = _vector(ref_logp, _f32, n, "ref_logp", device), _vector(weights, _f32, n, "weights", device)
+    logp, margins = _vector(logp_out, _f32, n, "logp_out", device), _vector(margins_out, _f32, pairs, "margins_out", device)
+    loss = _vector(loss_out, _f32, 1, "loss_out", device)
+    w, size, _keep = _workspace(workspace, _need("star_preference_loss_workspace", *head[1:4], pairs), device, stream)
     _check(lib.star_preference_loss(*head, ref, wts, pairs, at.ctypes.data, ctypes.byref(p), *out, logp, margins, loss, w,
                                     size, _stream_handle(stream)))
 
 
 def star_act_bytes(tokens: int, width: int) -> int:
     """Bytes of the packed form of activations [tokens, width]."""
-    return int(_library().star_act_bytes(tokens, width))
+    return _need("star_act_bytes", tokens, width)
 
 
-def _packed(packed, tokens: int, width: int, device) -> int:
-    if packed.element_size() != 1 or packed.dim() != 1 or not packed.is_contiguous() or packed.device != device:
+def _packed(packed, tokens: int, width: int, device: int) -> int:
+    if packed.element_size() != 1 or packed.dim() != 1 or not packed.is_contiguous() or packed.get_device() != device:
         raise ValueError("packed must be a contiguous 1-D uint8 tensor on the same device")
-    if packed.shape[0] < star_act_bytes(tokens, width):
+    if packed.size(0) < _need("star_act_bytes", tokens, width):
         raise ValueError("packed must hold star_act_bytes(tokens, width) bytes")
     return packed.data_ptr()
 
@@ -213,7 +222,7 @@ def star_act_pack(x, packed, *, stream=None) -> None:
     ``star_act_bytes(tokens, width)`` bytes."""
     code = _dtype(x, "x")
     p, tokens, width, ld = _matrix(x, "x")
-    _check(_library().star_act_pack(p, code, tokens, width, ld, _packed(packed, tokens, width, x.device),
+    _check(_library().star_act_pack(p, code, tokens, width, ld, _packed(packed, tokens, width, x.get_device()),
                                     _stream_handle(stream)))
 
 
@@ -221,7 +230,7 @@ def star_act_unpack(packed, out, *, stream=None) -> None:
     """The kept values of ``packed``, into ``out`` (float32 or bfloat16 [tokens, width])."""
     code = _dtype(out, "out")
     p, tokens, width, ld = _matrix(out, "out")
-    _check(_library().star_act_unpack(_packed(packed, tokens, width, out.device), tokens, width, p, code, ld,
+    _check(_library().star_act_unpack(_packed(packed, tokens, width, out.get_device()), tokens, width, p, code, ld,
                                       _stream_handle(stream)))
 
 
@@ -232,11 +241,12 @@ def star_act_weight_grad(dy, packed, dw, *, accumulate: bool = False, workspace=
     lib = _library()
     dy_code, dw_code = _dtype(dy, "dy"), _dtype(dw, "dw")
     p, tokens, out, ld = _matrix(dy, "dy")
-    if dw.dim() != 2 or dw.shape[0] != out or not dw.is_contiguous():
+    if dw.dim() != 2 or dw.size(0) != out or not dw.is_contiguous():
         raise ValueError(f"dw must be a contiguous tensor [{out}, width]")
-    if dw.device != dy.device:
+    device = dy.get_device()
+    if dw.get_device() != device:
         raise ValueError("dw must be on dy's device")
-    width = dw.shape[1]
-    w, size, _keep = _workspace(workspace, lib.star_act_weight_grad_workspace(dy_code, tokens, out, width), dy.device, stream)
-    _check(lib.star_act_weight_grad(p, dy_code, tokens, out, ld, _packed(packed, tokens, width, dy.device), width,
+    width = dw.size(1)
+    w, size, _keep = _workspace(workspace, _need("star_act_weight_grad_workspace", dy_code, tokens, out, width), device, stream)
+    _check(lib.star_act_weight_grad(p, dy_code, tokens, out, ld, _packed(packed, tokens, width, device), width,
                                     dw.data_ptr(), dw_code, int(bool(accumulate)), w, size, _stream_handle(stream)))
