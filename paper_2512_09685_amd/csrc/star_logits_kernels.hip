@@ -16,7 +16,7 @@ namespace {
 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));   // (see f32x4_any)
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 constexpr int64_t kFewTokens = 128;   // up to this many rows are cut into sections
 
 // 16 bytes of a row as VEC numbers, and back.
@@ -171,9 +171,8 @@ __device__ __forceinline__ MaxSum join_group(const MaxSum a, float k, MaxSum* sh
 
 // A long row, chunk by chunk, four of them under way at a time.
 template <class E, int NT>
-__device__ __forceinline__ MaxSum scan_row(const char* row, const RowSpan& sp, float k) {
+__device__ __forceinline__ MaxSum scan_chunks(const char* row, const RowSpan& sp, float k) {
     MaxSum a{-INFINITY, 0.f};
-    if ((int)threadIdx.x < sp.edge) a = MaxSum{E::one(row, sp.edge_element(threadIdx.x)), 1.f};
     for (int c = threadIdx.x; c < sp.chunks; c += 4 * NT) {
         u32x4 x[4];
         load_chunks<E, NT>(x, row, sp, c);
@@ -181,6 +180,14 @@ __device__ __forceinline__ MaxSum scan_row(const char* row, const RowSpan& sp, f
         a = MaxSum{m, a.s * __builtin_amdgcn_exp2f((a.m - base) * k) + sum_from<E>(x, -INFINITY, m, k)};
     }
     return a;
+}
+
+// One chunk of the gradient from its elements but for the target: `c` more at element `at` of it, rounded.
+template <class E>
+__device__ __forceinline__ u32x4 finish_chunk(float (&v)[E::VEC], float c, int at) {
+    if (at >= 0 && at < E::VEC)
+        static_for<0, E::VEC>([&](auto I) { v[decltype(I)::value] += at == decltype(I)::value ? c : 0.f; });
+    return E::pack(v);
 }
 
 // dl_j = scaled * 2^((l_j - m) k), plus `c` at the target: one chunk, one element.
@@ -195,10 +202,7 @@ __device__ __forceinline__ u32x4 slope_chunk(const u32x4& x, const Slope& p, int
         constexpr int n = decltype(I)::value;
         v[n] = p.scaled * __builtin_amdgcn_exp2f((E::template get<n>(x) - p.m) * p.k);
     });
-    const int at = p.y - first;
-    if (at >= 0 && at < E::VEC)
-        static_for<0, E::VEC>([&](auto I) { v[decltype(I)::value] += at == decltype(I)::value ? p.c : 0.f; });
-    return E::pack(v);
+    return finish_chunk<E>(v, p.c, p.y - first);
 }
 template <class E, int NT, int C>
 __device__ __forceinline__ void store_slopes(const u32x4 (&x)[C], char* out, const RowSpan& sp, const Slope& p, int first) {
@@ -253,18 +257,42 @@ __device__ __forceinline__ void clear_ticket(const RowArgs& a) {
     if (a.ticket && blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0u;
 }
 
+// Maximum and sum over the threads of a row, in a fixed order; every thread gets them.
+template <int LANES, class Op>
+__device__ __forceinline__ float fold_wave(float x, Op&& op) {
+    for (int d = LANES / 2; d; d >>= 1) x = op(x, __shfl_xor(x, d));
+    return x;
+}
+template <int NT, class Op>
+__device__ __forceinline__ float fold_row(float x, float* shared, Op&& op) {
+    x = fold_wave<64>(x, op);
+    if constexpr (NT == 64) return x;
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return fold_wave<NT / 64>(shared[threadIdx.x % (NT / 64)], op);
+}
+
+// Workgroups go round the 8 dies; this gives each die a run of long rows of its own (8192 x 65536, bf16: 397 -> 380 us, 16384 x
+// 32768: 381 -> 356; rows of 16 KB and less are up to 5 % slower that way and stay in the order of the workgroups).
+__device__ __forceinline__ int64_t die_run(unsigned id) {
+    return gridDim.x % 8 == 0 ? (id % 8) * (gridDim.x / 8) + id / 8 : id;
+}
+
 // The whole row in registers, C chunks a thread: read once, written once.  NT threads a row, ROWS rows a workgroup.
 // Registers and not LDS, because a unit has three times as much of them; rows of up to 8 chunks a thread let two
-// workgroups of 1024 threads share a unit, of which one reads while the other writes (8192 x 65536, bf16: 376 us with
-// one of them, 392 with this form's two and all 8192 rows read -- 2.1 GB, 5.4 TB/s, what a copy of that length takes;
-// writing in bursts by a common clock, two rows in turn in two sets of registers, changed nothing: half of this traffic is writes,
-// and what the memory-side cache takes at once it has to give back to the DRAM during the reads).
+// workgroups of 1024 threads share a unit, of which one reads while the other writes.
+// Beside the memory it is the vector instructions that count (an exponential takes four turns of the others), so an
+// exponent is one multiply-add, l k - e with e = round(max l k), a whole number that costs the sum no rounding; and
+// where the registers allow it, fp32 rows and bf16 rows of up to 4 chunks, the exponentials are kept for the gradient
+// in the logits' place.  Rows whose maximum is beyond 1e30 (nothing but a type's lowest value, or infinite) are taken relative to
+// it first: no product with k would hold them.
 template <class E, int NT, int C, int ROWS, RowWork WORK>
 __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(const RowArgs a) {
-    __shared__ MaxSum shared[NT / 64];
+    constexpr bool KEEP = WORK == RowWork::Policy && (E::VEC == 4 || C <= 4);
+    __shared__ float shared[2][NT / 64];
     clear_ticket(a);
     const int V = (int)a.l.vocab, tid = threadIdx.x % NT;
-    const int64_t in = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
+    const int64_t in = NT == 1024 ? die_run(blockIdx.x) : (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
     if (ROWS > 1 && in >= a.rows) return;
     const int64_t t = a.first + in, y = a.l.targets[t];
     const char* row = row_of(a, t, E::BYTES);
@@ -281,34 +309,71 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
     const RowSpan sp = row_span<E, NT>(row, V);
     u32x4 x[C];
     load_chunks<E, NT>(x, row, sp, tid);
-    const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY, ly = E::one(row, y);
-    MaxSum mine{max_of<E>(x, edge), 0.f};
+    float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
+    const float ly = E::one(row, y);
+    const float m = fold_row<NT>(max_of<E>(x, edge), shared[0], [](float p, float q) { return fmaxf(p, q); });
     keep_packed(x);
-    mine.s = sum_from<E>(x, edge, mine.m, k);
-    const MaxSum all = join_group<NT>(mine, k, shared);
-    const float logp = logp_of(a, all, ly);
+    const bool far = !(fabsf(m) <= 1e30f);
+    if (far) {
+        static_for<0, C>([&](auto I) {
+            float v[E::VEC];
+            static_for<0, E::VEC>([&](auto J) { v[decltype(J)::value] = E::template get<decltype(J)::value>(x[decltype(I)::value]) - m; });
+            x[decltype(I)::value] = E::pack(v);
+        });
+        edge -= m;
+    }
+    const float e = far ? 0.f : rintf(m * k);
+    float kept[KEEP ? C * E::VEC : 1];
+    const float kept_edge = __builtin_amdgcn_exp2f(__builtin_fmaf(edge, k, -e));
+    float s = kept_edge;
+    static_for<0, C>([&](auto I) {
+        static_for<0, E::VEC>([&](auto J) {
+            constexpr int i = decltype(I)::value, j = decltype(J)::value;
+            const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(E::template get<j>(x[i]), k, -e));
+            if constexpr (KEEP) kept[i * E::VEC + j] = v;
+            s += v;
+        });
+    });
+    s = fold_row<NT>(s, shared[1], [](float p, float q) { return p + q; });
+    // log sum exp(z - max z): the sum is that of 2^(z' - e)
+    const float log_s = logf(s) - (far ? 0.f : __builtin_fmaf(m, k, -e) * kLn2), logp = (ly - m) * a.l.inv_t - log_s;
     if (tid == 0) {
         a.logp[t] = logp;
-        if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = all.m * a.l.inv_t + logf(all.s);
+        if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = m * a.l.inv_t + log_s;
     }
     if constexpr (WORK == RowWork::Policy) {
-        const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp).slope * a.l.inv_t;
-        const Slope p{k, all.m, -c / all.s, c, (int)y};
-        keep_packed(x);
-        store_slopes<E, NT>(x, out, sp, p, tid);
-        if (tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
+        const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp).slope * a.l.inv_t, scaled = -c / s;
+        if constexpr (!KEEP) keep_packed(x);
+        u32x4_any* to = reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES);
+        static_for<0, C>([&](auto I) {
+            constexpr int i = decltype(I)::value;
+            const int at = tid + i * NT;
+            if (at < sp.chunks) {
+                float v[E::VEC];
+                static_for<0, E::VEC>([&](auto J) {
+                    constexpr int j = decltype(J)::value;
+                    if constexpr (KEEP) v[j] = scaled * kept[i * E::VEC + j];
+                    else v[j] = scaled * __builtin_amdgcn_exp2f(__builtin_fmaf(E::template get<j>(x[i]), k, -e));
+                });
+                __builtin_nontemporal_store(finish_chunk<E>(v, c, (int)y - sp.head - at * E::VEC), to + at);
+            }
+        });
+        if (tid < sp.edge) {
+            const int j = sp.edge_element(tid);
+            E::put(out, j, j == (int)y ? scaled * kept_edge + c : scaled * kept_edge);
+        }
     }
 }
 
-// Rows too long for that: a workgroup a row, read a second time for its gradient, from its end, which the caches still hold.
-constexpr int kScanThreads = 512;
-template <class E, RowWork WORK>
-__global__ __launch_bounds__(kScanThreads) void logits_scan_kernel(const RowArgs a) {
-    constexpr int NT = kScanThreads;
+// Rows too long for that: a workgroup a row, H chunks a thread of its end in registers; for its gradient the rest of the row is read a second
+// time, from its end, which the caches still hold.  (2048 x 131072, fp32: 560 us with nothing in
+// registers, 523 / 467 / 443 / 447 with H = 8 / 14 / 20 / 22.)
+template <class E, int NT, int H, RowWork WORK>
+__global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
     __shared__ MaxSum shared[NT / 64];
     clear_ticket(a);
     const int V = (int)a.l.vocab, tid = threadIdx.x;
-    const int64_t t = a.first + blockIdx.x, y = a.l.targets[t];
+    const int64_t t = a.first + die_run(blockIdx.x), y = a.l.targets[t];
     const char* row = row_of(a, t, E::BYTES);
     char* out = a.dlogits + t * a.ld_out * E::BYTES;
     const float k = kLog2e * a.l.inv_t;
@@ -321,8 +386,22 @@ __global__ __launch_bounds__(kScanThreads) void logits_scan_kernel(const RowArgs
         return;
     }
     const RowSpan sp = row_span<E, NT>(row, V);
-    const float ly = E::one(row, y);
-    const MaxSum all = join_group<NT>(scan_row<E, NT>(row, sp, k), k, shared);
+    const int rest = max(sp.chunks - H * NT, 0);
+    const float ly = E::one(row, y), edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
+    RowSpan before = sp;
+    before.chunks = rest;
+    MaxSum mine = scan_chunks<E, NT>(row, before, k);
+    u32x4 x[H > 0 ? H : 1];
+    if constexpr (H > 0) {
+        load_chunks<E, NT>(x, row, sp, rest + tid);
+        const float m = max_of<E>(x, fmaxf(mine.m, edge)), base = m == -INFINITY ? 0.f : m;
+        keep_packed(x);
+        mine = MaxSum{m, mine.s * __builtin_amdgcn_exp2f((mine.m - base) * k) + sum_from<E>(x, edge, m, k)};
+    } else {
+        const float m = fmaxf(mine.m, edge), base = m == -INFINITY ? 0.f : m;
+        mine = MaxSum{m, mine.s * __builtin_amdgcn_exp2f((mine.m - base) * k) + __builtin_amdgcn_exp2f((edge - base) * k)};
+    }
+    const MaxSum all = join_group<NT>(mine, k, shared);
     const float logp = logp_of(a, all, ly);
     if (tid == 0) {
         a.logp[t] = logp;
@@ -331,12 +410,16 @@ __global__ __launch_bounds__(kScanThreads) void logits_scan_kernel(const RowArgs
     if constexpr (WORK == RowWork::Policy) {
         const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp).slope * a.l.inv_t;
         const Slope p{k, all.m, -c / all.s, c, (int)y};
-        for (int first = (sp.chunks - 1) / (4 * NT) * (4 * NT); first >= 0; first -= 4 * NT) {
-            u32x4 x[4];
-            load_chunks<E, NT>(x, row, sp, first + tid);
-            store_slopes<E, NT>(x, out, sp, p, first + tid);
+        if constexpr (H > 0) {
+            keep_packed(x);
+            store_slopes<E, NT>(x, out, sp, p, rest + tid);
         }
-        if (tid < sp.edge) store_slope<E>(E::one(row, sp.edge_element(tid)), out, sp, p, tid);
+        for (int first = (rest - 1) / (4 * NT) * (4 * NT); first >= 0; first -= 4 * NT) {
+            u32x4 z[4];
+            load_chunks<E, NT>(z, row, before, first + tid);
+            store_slopes<E, NT>(z, out, before, p, first + tid);
+        }
+        if (tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
     }
 }
 
@@ -607,11 +690,14 @@ void launch_rows_of(const RowArgs& a, hipStream_t stream) {
     if (chunks <= 512) return logits_held_kernel<E, 64, 8, 4, WORK><<<fours, 256, 0, stream>>>(a);
     if (chunks <= 1024) return logits_held_kernel<E, 256, 4, 1, WORK><<<rows, 256, 0, stream>>>(a);
     if (chunks <= 2048) return logits_held_kernel<E, 256, 8, 1, WORK><<<rows, 256, 0, stream>>>(a);
-    if (chunks <= 4096) return logits_held_kernel<E, 512, 8, 1, WORK><<<rows, 512, 0, stream>>>(a);
+    if (chunks <= 4096) return logits_held_kernel<E, 1024, 4, 1, WORK><<<rows, 1024, 0, stream>>>(a);
     if (chunks <= 8192) return logits_held_kernel<E, 1024, 8, 1, WORK><<<rows, 1024, 0, stream>>>(a);
-    if constexpr (WORK == RowWork::Policy)
+    if constexpr (WORK == RowWork::Policy) {
         if (chunks <= 16384) return logits_held_kernel<E, 1024, 16, 1, WORK><<<rows, 1024, 0, stream>>>(a);
-    logits_scan_kernel<E, WORK><<<rows, kScanThreads, 0, stream>>>(a);
+        logits_scan_kernel<E, 1024, 20, WORK><<<rows, 1024, 0, stream>>>(a);
+    } else {
+        logits_scan_kernel<E, 512, 0, WORK><<<rows, 512, 0, stream>>>(a);
+    }
 }
 
 template <class E>
