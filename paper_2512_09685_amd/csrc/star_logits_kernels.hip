@@ -17,7 +17,10 @@ namespace {
 typedef u32x4 u32x4_any __attribute__((aligned(2)));   // (see f32x4_any)
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
-constexpr int64_t kFewTokens = 128;   // up to this many rows are cut into sections
+// Up to this many rows are cut into sections, if they have at least so many chunks: for the policy loss, which is two launches either
+// way (48 x 32000, bf16: 11.2 against 12.7 us, 1 x 131072 11 against 19), and for log-probabilities, where the second launch
+// has to pay (1 x 131072, fp32: 9.8 against 12.6 us, bf16 9.1 against 9.9; 48 x 32000, fp32: 9.0 against 6.4).
+constexpr int64_t kFewTokens = 128, kPolicySections = 2048, kLogprobsSections = 16384;
 
 // 16 bytes of a row as VEC numbers, and back.
 struct ElemF32 {
@@ -229,6 +232,25 @@ __device__ __forceinline__ void zero_row(char* out, int V, int tid, int from = 0
     if (from == 0 && tid < sp.edge) E::put(out, sp.edge_element(tid), 0.f);
 }
 
+// N sums over a workgroup of NT threads in a fixed order, valid in thread 0.
+template <int NT, int N>
+__device__ __forceinline__ void group_sums(double (&x)[N], double (*shared)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = wave_sum_to_lane63(x[i]);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63)
+#pragma unroll
+        for (int i = 0; i < N; ++i) shared[threadIdx.x >> 6][i] = x[i];
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[i] = 0.0;
+            for (int w = 0; w < NT / 64; ++w) x[i] += shared[w][i];
+        }
+    }
+}
+
 enum class RowWork { Logprobs, Policy };
 
 struct RowArgs {
@@ -242,6 +264,7 @@ struct RowArgs {
     float* picked;                 // of such rows: the target's logit, which a gradient in place would be written over
     int sections;
     float* stats;
+    PairLoss loss;                 // of the pairs whose gradient this is; its output null: none
     unsigned int* ticket;          // cleared for the launch behind this one; null: it needs none
 };
 
@@ -490,22 +513,8 @@ __global__ __launch_bounds__(64) void logits_join_kernel(const RowArgs a) {
 // ---------------------------------------------------------------- sums over tokens
 constexpr int kSumThreads = 1024;
 
-// Sum over the workgroup in a fixed order, valid in thread 0.
-__device__ __forceinline__ double group_sum(double x, double* shared) {
-    x = wave_sum_to_lane63(x);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) shared[threadIdx.x >> 6] = x;
-    __syncthreads();
-    double s = 0.0;
-    if (threadIdx.x == 0)
-        for (int w = 0; w < (int)blockDim.x / 64; ++w) s += shared[w];
-    return s;
-}
-
-// What the tokens t0, t0 + step, ... add to the four sums of the policy loss.
-__device__ __forceinline__ void add_policy_terms(double (&sum)[4], const Logits& l, const PolicyArgs& a, int64_t t, float logp) {
-    const PolicyTerm p = policy_term(a, t, logp);
-    const double w = l.weights ? (double)l.weights[t] : 1.0;
+// What a token adds to the four sums of the policy loss.
+__device__ __forceinline__ void add_policy_term(double (&sum)[4], const PolicyTerm& p, double w) {
     sum[0] += w * p.loss;
     sum[1] += w * p.kl;
     sum[2] += w * p.clipped;
@@ -517,23 +526,26 @@ __device__ __forceinline__ void add_policy_terms(double (&sum)[4], const Logits&
 template <class E, int C>
 __global__ __launch_bounds__(kSectionThreads) void policy_section_kernel(const RowArgs a) {
     constexpr int NT = kSectionThreads;
-    __shared__ double shared[NT / 64];
+    __shared__ double shared[NT / 64][4];
     const int V = (int)a.l.vocab, tid = threadIdx.x, section = (int)(blockIdx.x % (unsigned)a.sections);
     const int64_t in = blockIdx.x / (unsigned)a.sections;
     const float k = kLog2e * a.l.inv_t;
     if (in >= a.rows) {
         double sum[4] = {0, 0, 0, 0};
         for (int64_t t = tid; t < a.rows; t += NT) {
+            // (everything is read before anything is decided: this workgroup is the one that the others wait for; what a row that does not
+            // count left in the workspace is not used)
             const int64_t y = a.l.targets[t];
-            const bool live = counts(a.l, t, y);
-            const float logp = live ? logp_of(a, join_parts(a, t, k), a.picked[t]) : 0.f;
-            a.logp[t] = logp;
-            if (live) add_policy_terms(sum, a.l, a.policy, t, logp);
+            const double w = a.l.weights ? (double)a.l.weights[t] : 1.0;
+            const float all = logp_of(a, join_parts(a, t, k), a.picked[t]);
+            const PolicyTerm p = policy_term(a.policy, t, all);
+            const bool live = y >= 0 && y < a.l.vocab && w != 0.0;
+            a.logp[t] = live ? all : 0.f;
+            if (live) add_policy_term(sum, p, w);
         }
-        for (int i = 0; i < 4; ++i) {
-            const double s = group_sum(sum[i], shared);
-            if (tid == 0) a.stats[i] = (float)(s * a.policy.scale);
-        }
+        group_sums<NT>(sum, shared);
+        if (tid == 0)
+            for (int i = 0; i < 4; ++i) a.stats[i] = (float)(sum[i] * a.policy.scale);
         return;
     }
     const int64_t t = in, y = a.l.targets[t];
@@ -556,11 +568,21 @@ __global__ __launch_bounds__(kSectionThreads) void policy_section_kernel(const R
     if (section == 0 && tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
 }
 
+// The pairs' terms joined, by a workgroup of kBlock threads.
+__device__ __forceinline__ void join_pair_loss(const PairLoss& p) {
+    __shared__ double shared[kBlock / 64][1];
+    double sum[1] = {0.0};
+    for (int b = threadIdx.x; b < p.pairs; b += kBlock) sum[0] += p.terms[b];
+    group_sums<kBlock>(sum, shared);
+    if (threadIdx.x == 0) *p.out = (float)(sum[0] * p.scale);
+}
+
 // The gradient alone, which needs nothing of the rest of its row: NT threads to a section of C chunks each, ROWS rows a workgroup.
 template <class E, int NT, int C, int ROWS>
 __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) {
     const int V = (int)a.l.vocab, tid = threadIdx.x % NT, section = (int)(blockIdx.x % (unsigned)a.sections);
     const int64_t in = (int64_t)(blockIdx.x / (unsigned)a.sections) * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
+    if (a.loss.out && blockIdx.x == gridDim.x - 1) return join_pair_loss(a.loss);   // (a workgroup more than the rows need)
     if (ROWS > 1 && in >= a.rows) return;
     const int64_t t = a.first + in, y = a.l.targets[t];
     const char* row = row_of(a, t, E::BYTES);
@@ -587,12 +609,12 @@ constexpr int kStatsGroups = 64;
 
 __global__ __launch_bounds__(kSumThreads) void policy_stats_kernel(const Logits l, const PolicyArgs a, const float* logp, float* stats,
                                                                    unsigned int* ticket, double* sums) {
-    __shared__ double shared[kSumThreads / 64];
+    __shared__ double shared[kSumThreads / 64][4];
     __shared__ bool last;
     double sum[4] = {0, 0, 0, 0};
     for (int64_t t = (int64_t)blockIdx.x * kSumThreads + threadIdx.x; t < l.tokens; t += (int64_t)gridDim.x * kSumThreads)
-        if (counts(l, t, l.targets[t])) add_policy_terms(sum, l, a, t, logp[t]);
-    for (int i = 0; i < 4; ++i) sum[i] = group_sum(sum[i], shared);
+        if (counts(l, t, l.targets[t])) add_policy_term(sum, policy_term(a, t, logp[t]), l.weights ? (double)l.weights[t] : 1.0);
+    group_sums<kSumThreads>(sum, shared);
     if (gridDim.x > 1) {
         // the workgroup that comes last joins all of them, in their own order
         if (threadIdx.x == 0) {
@@ -601,11 +623,9 @@ __global__ __launch_bounds__(kSumThreads) void policy_stats_kernel(const Logits 
         }
         __syncthreads();
         if (!last) return;
-        for (int i = 0; i < 4; ++i) {
-            double mine = 0.0;
-            if (threadIdx.x < gridDim.x) mine = __hip_atomic_load(sums + 4 * threadIdx.x + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            sum[i] = group_sum(mine, shared);
-        }
+        for (int i = 0; i < 4; ++i)
+            sum[i] = threadIdx.x < gridDim.x ? __hip_atomic_load(sums + 4 * threadIdx.x + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+        group_sums<kSumThreads>(sum, shared);
     }
     if (threadIdx.x == 0)
         for (int i = 0; i < 4; ++i) stats[i] = (float)(sum[i] * a.scale);
@@ -614,18 +634,18 @@ __global__ __launch_bounds__(kSumThreads) void policy_stats_kernel(const Logits 
 // A workgroup a pair.
 __global__ __launch_bounds__(kBlock) void pair_kernel(const Logits l, const PreferenceArgs a, const PairOffsets offsets, const float* logp,
                                                       float* dlogp, float* margins, double* terms) {
-    __shared__ double shared[kBlock / 64];
+    __shared__ double shared[kBlock / 64][1];
     __shared__ double all;
     const int b = blockIdx.x;
     const int64_t from = offsets.at[2 * b], mid = offsets.at[2 * b + 1], to = offsets.at[2 * b + 2];
-    double sum = 0.0;
+    double sum[1] = {0.0};
     for (int64_t t = from + threadIdx.x; t < to; t += kBlock) {
         if (!counts(l, t, l.targets[t])) continue;
         const double d = ((double)logp[t] - (double)a.ref_logp[t]) * (l.weights ? (double)l.weights[t] : 1.0);
-        sum += t < mid ? d : -d;
+        sum[0] += t < mid ? d : -d;
     }
-    sum = group_sum(sum, shared);
-    if (threadIdx.x == 0) all = a.beta * sum;
+    group_sums<kBlock>(sum, shared);
+    if (threadIdx.x == 0) all = a.beta * sum[0];
     __syncthreads();
     const double s = all;
     // -log sigmoid(s) = max(-s, 0) + log(1 + e^-|s|)
@@ -645,13 +665,7 @@ __global__ __launch_bounds__(kBlock) void pair_kernel(const Logits l, const Pref
         }
 }
 
-__global__ __launch_bounds__(kBlock) void pair_loss_kernel(const double* terms, const int pairs, const float scale, float* loss) {
-    __shared__ double shared[kBlock / 64];
-    double sum = 0.0;
-    for (int b = threadIdx.x; b < pairs; b += kBlock) sum += terms[b];
-    sum = group_sum(sum, shared);
-    if (threadIdx.x == 0) *loss = (float)(sum * scale);
-}
+__global__ __launch_bounds__(kBlock) void pair_loss_kernel(const PairLoss p) { join_pair_loss(p); }
 
 // ---------------------------------------------------------------- launches
 template <class E>
@@ -664,9 +678,9 @@ int64_t chunks_of(int dtype, int64_t vocab) { return dtype == STAR_F32 ? (vocab 
 struct Sections {
     int chunks_a_thread, count;   // 0: rows are not cut
 };
-Sections sections_of(int dtype, int64_t tokens, int64_t vocab) {
+Sections sections_of(int dtype, int64_t tokens, int64_t vocab, int64_t least) {
     const int64_t chunks = chunks_of(dtype, vocab);
-    if (tokens > kFewTokens || chunks < 2048) return Sections{0, 0};
+    if (tokens > kFewTokens || chunks < least) return Sections{0, 0};
     int c = 8;
     while (c > 1 && tokens * ((chunks + kSectionThreads * c - 1) / (kSectionThreads * c)) < 512) c /= 2;
     return Sections{c, (int)((chunks + kSectionThreads * c - 1) / (kSectionThreads * c))};
@@ -705,24 +719,20 @@ void launch_grad_of(RowArgs a, hipStream_t stream) {
     const int64_t chunks = chunks_of<E>(a.l);
     const unsigned rows = (unsigned)a.rows;
     a.sections = 1;
-    if (chunks <= 128) return logits_grad_kernel<E, 64, 2, 4><<<(rows + 3) / 4, 256, 0, stream>>>(a);
-    if (chunks <= 512) return logits_grad_kernel<E, 64, 8, 4><<<(rows + 3) / 4, 256, 0, stream>>>(a);
+    const unsigned fours = (rows + 3) / 4, more = a.loss.out ? 1 : 0;
+    if (chunks <= 128) return logits_grad_kernel<E, 64, 2, 4><<<fours + more, 256, 0, stream>>>(a);
+    if (chunks <= 512) return logits_grad_kernel<E, 64, 8, 4><<<fours + more, 256, 0, stream>>>(a);
     const bool few = a.rows * chunks < 512 * 2048;   // (fewer than two workgroups a unit with sections of 2048 chunks)
     a.sections = (int)(few ? (chunks + 511) / 512 : (chunks + 2047) / 2048);
-    const unsigned grid = rows * (unsigned)a.sections;
+    const unsigned grid = rows * (unsigned)a.sections + more;
     if (few) logits_grad_kernel<E, 256, 2, 1><<<grid, 256, 0, stream>>>(a);
     else logits_grad_kernel<E, 256, 8, 1><<<grid, 256, 0, stream>>>(a);
 }
 
 // Workspace of rows in sections: their results, then the targets' logits.
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
-size_t parts_bytes(int dtype, int64_t tokens, int64_t vocab) {
-    return round16(sizeof(MaxSum) * (size_t)tokens * (size_t)sections_of(dtype, tokens, vocab).count);
-}
-size_t section_bytes(int dtype, int64_t tokens, int64_t vocab) {
-    const size_t parts = parts_bytes(dtype, tokens, vocab);
-    return parts ? parts + round16(sizeof(float) * (size_t)tokens) : 0;
-}
+size_t parts_bytes(const Sections& s, int64_t tokens) { return round16(sizeof(MaxSum) * (size_t)tokens * (size_t)s.count); }
+size_t section_bytes(const Sections& s, int64_t tokens) { return s.count ? parts_bytes(s, tokens) + round16(sizeof(float) * (size_t)tokens) : 0; }
 
 // Workspace of the policy loss: ticket | sums of the workgroups | sections | log-probabilities.
 struct PolicySpace {
@@ -732,7 +742,7 @@ PolicySpace policy_space(int dtype, int64_t tokens, int64_t vocab) {
     PolicySpace s;
     s.sums = 16;
     s.parts = s.sums + sizeof(double) * 4 * kStatsGroups;
-    s.logp = s.parts + section_bytes(dtype, tokens, vocab);
+    s.logp = s.parts + section_bytes(sections_of(dtype, tokens, vocab, kPolicySections), tokens);
     s.total = s.logp + round16(sizeof(float) * (size_t)tokens);
     return s;
 }
@@ -758,7 +768,7 @@ hipError_t in_launches(RowArgs a, int64_t first, int64_t count, F&& launch) {
 }  // namespace
 
 size_t logprobs_workspace(int dtype, int64_t tokens, int64_t vocab) {
-    return section_bytes(dtype, tokens, vocab);
+    return section_bytes(sections_of(dtype, tokens, vocab, kLogprobsSections), tokens);
 }
 size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab) { return policy_space(dtype, tokens, vocab).total; }
 
@@ -767,12 +777,12 @@ hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float*
     a.l = l;
     a.logp = logp;
     a.lse = lse;
-    const Sections s = workspace ? sections_of(l.dtype, count, l.vocab) : Sections{0, 0};
+    const Sections s = workspace ? sections_of(l.dtype, count, l.vocab, kLogprobsSections) : Sections{0, 0};
     if (s.count > 1) {
         a.first = first;
         a.rows = count;
         a.parts = at<MaxSum>(workspace, 0);
-        a.picked = at<float>(workspace, parts_bytes(l.dtype, count, l.vocab));
+        a.picked = at<float>(workspace, parts_bytes(s, count));
         a.sections = s.count;
         const unsigned grid = (unsigned)(count * s.count), joins = (unsigned)((count + 63) / 64);
         auto both = [&](auto elem) {
@@ -791,14 +801,15 @@ hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float*
 }
 
 hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, const float* lse, const float* dlogp, void* dlogits,
-                                int64_t ld_out, hipStream_t stream) {
+                                int64_t ld_out, const PairLoss& loss, hipStream_t stream) {
     RowArgs a{};
     a.l = l;
     a.lse_in = lse;
     a.dlogp = dlogp;
     a.dlogits = reinterpret_cast<char*>(dlogits);
     a.ld_out = ld_out;
-    return in_launches(a, first, count, [&](const RowArgs& r) {
+    return in_launches(a, first, count, [&](RowArgs r) {
+        if (r.first + r.rows == first + count) r.loss = loss;   // the last one
         if (l.dtype == STAR_F32) launch_grad_of<ElemF32>(r, stream);
         else launch_grad_of<ElemBf16>(r, stream);
     });
@@ -814,11 +825,11 @@ hipError_t launch_policy(const Logits& l, const PolicyArgs& p, float* logp, void
     a.ld_out = ld_out;
     const PolicySpace space = policy_space(l.dtype, l.tokens, l.vocab);
     if (!a.logp && l.tokens > 0) a.logp = at<float>(workspace, space.logp);
-    const Sections s = sections_of(l.dtype, l.tokens, l.vocab);
+    const Sections s = sections_of(l.dtype, l.tokens, l.vocab, kPolicySections);
     if (s.count > 1 && l.tokens > 0 && dlogits) {
         a.rows = l.tokens;
         a.parts = at<MaxSum>(workspace, space.parts);
-        a.picked = at<float>(workspace, space.parts + parts_bytes(l.dtype, l.tokens, l.vocab));
+        a.picked = at<float>(workspace, space.parts + parts_bytes(s, l.tokens));
         a.sections = s.count;
         a.stats = stats;
         const unsigned grid = (unsigned)(l.tokens * s.count);
@@ -850,8 +861,8 @@ hipError_t launch_pairs(const Logits& l, const PreferenceArgs& a, const PairOffs
     return hipGetLastError();
 }
 
-hipError_t launch_pair_loss(const double* terms, int pairs, float scale, float* loss, hipStream_t stream) {
-    pair_loss_kernel<<<dim3(1), kBlock, 0, stream>>>(terms, pairs, scale, loss);
+hipError_t launch_pair_loss(const PairLoss& loss, hipStream_t stream) {
+    pair_loss_kernel<<<dim3(1), kBlock, 0, stream>>>(loss);
     return hipGetLastError();
 }
 

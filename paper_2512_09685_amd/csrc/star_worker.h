@@ -34,9 +34,16 @@ size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab);
 
 // logp, lse (may be null) of rows [first, first + count).  Without a workspace a row is one workgroup's.
 hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* lse, void* workspace, hipStream_t stream);
-// dlogits of rows [first, first + count) from lse and dlogp.
+// The loss of pairs from their terms (one double each).
+struct PairLoss {
+    const double* terms;
+    int pairs;
+    float scale;
+    float* out;
+};
+// dlogits of rows [first, first + count) from lse and dlogp; with a loss whose `out` is not null, that too.
 hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, const float* lse, const float* dlogp, void* dlogits,
-                                int64_t ld_out, hipStream_t stream);
+                                int64_t ld_out, const PairLoss& loss, hipStream_t stream);
 // logp (may be null), dlogits (may be null) and the four sums of the policy loss.
 hipError_t launch_policy(const Logits& l, const PolicyArgs& a, float* logp, void* dlogits, int64_t ld_out, float* stats, void* workspace,
                          hipStream_t stream);
@@ -53,7 +60,7 @@ struct PreferenceArgs {
 // Margins of `pairs` pairs, their tokens' derivatives and the terms of the loss (one double a pair).
 hipError_t launch_pairs(const Logits& l, const PreferenceArgs& a, const PairOffsets& offsets, int pairs, const float* logp, float* dlogp,
                         float* margins, double* terms, hipStream_t stream);
-hipError_t launch_pair_loss(const double* terms, int pairs, float scale, float* loss, hipStream_t stream);
+hipError_t launch_pair_loss(const PairLoss& loss, hipStream_t stream);
 
 // ---------------------------------------------------------------- saved activations
 constexpr int kActBlock = 32;    // tokens that share a scale

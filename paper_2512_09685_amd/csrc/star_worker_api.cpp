@@ -134,7 +134,7 @@ star_status star_token_logprobs_grad(const void* logits, star_dtype dtype, int64
     if (tokens == 0) return STAR_OK;
     if (!lse || !dlogp || !dlogits) return set_error(STAR_ERR_NULL, "lse, dlogp or dlogits is NULL");
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, nullptr, temperature);
-    STAR_LAUNCH(star::launch_logprobs_grad(l, 0, tokens, lse, dlogp, dlogits, ld_out, static_cast<hipStream_t>(hip_stream)));
+    STAR_LAUNCH(star::launch_logprobs_grad(l, 0, tokens, lse, dlogp, dlogits, ld_out, star::PairLoss{}, static_cast<hipStream_t>(hip_stream)));
     return STAR_OK;
 }
 
@@ -184,6 +184,8 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
     double* terms = at<double>(workspace, space.terms);
     float *lse = at<float>(workspace, space.lse), *dlogp = at<float>(workspace, space.dlogp);
     float* logp = logp_out ? logp_out : at<float>(workspace, space.logp);
+    const star::PairLoss loss{terms, pairs, params->scale, loss_out};
+    bool joined = false;
     void* rows = space.total > space.rows ? at<char>(workspace, space.rows) : nullptr;
     for (int32_t first = 0; first < pairs; first += star::kPairsPerLaunch) {
         const int n = std::min<int32_t>(star::kPairsPerLaunch, pairs - first);
@@ -193,9 +195,11 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
         STAR_LAUNCH(star::launch_logprobs(l, from, count, logp, dlogits ? lse : nullptr, count == tokens ? rows : nullptr, stream));
         STAR_LAUNCH(star::launch_pairs(l, a, o, n, logp, dlogits ? dlogp : nullptr, margins_out ? margins_out + first : nullptr, terms + first,
                                        stream));
-        if (dlogits) STAR_LAUNCH(star::launch_logprobs_grad(l, from, count, lse, dlogp, dlogits, ld_out, stream));
+        const bool last = first + n == pairs && count > 0;   // the loss is joined beside the last gradient
+        if (dlogits) STAR_LAUNCH(star::launch_logprobs_grad(l, from, count, lse, dlogp, dlogits, ld_out, last ? loss : star::PairLoss{}, stream));
+        joined = dlogits && last;
     }
-    STAR_LAUNCH(star::launch_pair_loss(terms, pairs, params->scale, loss_out, stream));
+    if (!joined) STAR_LAUNCH(star::launch_pair_loss(loss, stream));
     return STAR_OK;
 }
 
