@@ -16,7 +16,7 @@ namespace {
 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));   // (see f32x4_any)
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.925962989e-08f, kLn2 = 0.693147180559945309417f;
 // Up to this many rows are cut into sections, if they have at least so many chunks: for the policy loss, which is two launches either
 // way (48 x 32000, bf16: 11.2 against 12.7 us, 1 x 131072 11 against 19), and for log-probabilities, where the second launch
 // has to pay (1 x 131072, fp32: 9.8 against 12.6 us, bf16 9.1 against 9.9; 48 x 32000, fp32: 9.0 against 6.4).
@@ -92,12 +92,44 @@ __device__ __forceinline__ bool counts(const Logits& l, int64_t t, int64_t y) {
     return y >= 0 && y < l.vocab && (!l.weights || l.weights[t] != 0.f);
 }
 
+// A value and what rounding it to fp32 left.  Log-probabilities of size 10 are rounded by up to 5e-7, which ratios of policies and differences of
+// sums over tokens would show.
+struct Two {
+    float high, low;
+};
+__device__ __forceinline__ Two two_sum(float a, float b) {
+    const float s = a + b, t = s - a;
+    return Two{s, (a - (s - t)) + (b - t)};
+}
+__device__ __forceinline__ Two normal(float high, float low) {
+    if (!(fabsf(high) < INFINITY)) return Two{high, 0.f};
+    const float s = high + low;
+    return Two{s, low - (s - high)};
+}
+// (a - b) / temperature
+__device__ __forceinline__ Two scaled_difference(const Logits& l, float a, float b) {
+    const Two d = two_sum(a, -b);
+    const float z = d.high * l.inv_t;
+    return Two{z, __builtin_fmaf(d.high, l.inv_t, -z) + (d.high * l.inv_t_low + d.low * l.inv_t)};
+}
+// log s, for s >= 1/2: n log 2 + log f, 1 <= f < 2, with log 2 in two parts of which the first times n is exact.
+__device__ __forceinline__ Two two_log(float s) {
+    if (!(s < INFINITY)) return Two{s, 0.f};
+    const uint32_t b = __float_as_uint(s);
+    const float n = (float)((int)(b >> 23) - 127), f = __uint_as_float((b & 0x7fffffu) | 0x3f800000u);
+    return Two{n * 0x1.62ep-1f, n * 3.194618494528623e-5f + logf(f)};
+}
+__device__ __forceinline__ Two add(const Two& a, const Two& b, float sign) {
+    const Two s = two_sum(a.high, sign * b.high);
+    return normal(s.high, s.low + (a.low + sign * b.low));
+}
+
 // One token's loss, KL estimate, whether it is clipped, and its derivative by logp (unweighted).
 struct PolicyTerm {
     float loss, kl, clipped, slope;
 };
-__device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& a, int64_t t, float logp) {
-    const float A = a.advantages[t], r = expf(logp - a.old_logp[t]);
+__device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& a, int64_t t, const Two& logp) {
+    const float A = a.advantages[t], r = expf((logp.high - a.old_logp[t]) + logp.low);
     const float held = fminf(fmaxf(r, a.low), a.high);
     // (an advantage of 0 costs nothing, also where the ratio has run over)
     const float free_cost = A == 0.f ? 0.f : -A * r, held_cost = A == 0.f ? 0.f : -A * held;
@@ -107,7 +139,7 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& a, int64_t t
     p.slope = free_cost < held_cost ? 0.f : free_cost;
     p.kl = 0.f;
     if (a.kl != 0.f) {
-        const float d = a.ref_logp[t] - logp, q = expm1f(d);
+        const float d = (a.ref_logp[t] - logp.high) - logp.low, q = expm1f(d);
         p.kl = q - d;
         p.loss += a.kl * p.kl;
         p.slope -= a.kl * q;
@@ -193,18 +225,32 @@ __device__ __forceinline__ u32x4 finish_chunk(float (&v)[E::VEC], float c, int a
     return E::pack(v);
 }
 
-// dl_j = scaled * 2^((l_j - m) k), plus `c` at the target: one chunk, one element.
+// dl_j = scaled * 2^(l_j k - e), plus `c` at the target: one chunk, one element.  Where a product with k would not hold the row's values
+// (`far`), scaled * 2^((l_j - m) k).
 struct Slope {
-    float k, m, scaled, c;
+    float k, e, m, scaled, c;
     int y;
+    bool far;
+    __device__ __forceinline__ float operator()(float l) const {
+        return scaled * __builtin_amdgcn_exp2f(far ? (l - m) * k : __builtin_fmaf(l, k, -e));
+    }
 };
+__device__ __forceinline__ bool is_far(float m) { return !(fabsf(m) <= 1e30f); }
+// Of a row whose sum of 2^((l_j - m) k) is s.
+__device__ __forceinline__ Slope slope_of(float k, const MaxSum& all, float c, int64_t y) {
+    const bool far = is_far(all.m);
+    const float e = far ? 0.f : rintf(all.m * k), off = far ? 0.f : __builtin_fmaf(all.m, k, -e);
+    return Slope{k, e, all.m, -c / all.s * __builtin_amdgcn_exp2f(-off), c, (int)y, far};
+}
 template <class E>
 __device__ __forceinline__ u32x4 slope_chunk(const u32x4& x, const Slope& p, int first) {
     float v[E::VEC];
-    static_for<0, E::VEC>([&](auto I) {
-        constexpr int n = decltype(I)::value;
-        v[n] = p.scaled * __builtin_amdgcn_exp2f((E::template get<n>(x) - p.m) * p.k);
-    });
+    if (p.far)
+        static_for<0, E::VEC>([&](auto I) { v[decltype(I)::value] = p(E::template get<decltype(I)::value>(x)); });
+    else
+        static_for<0, E::VEC>([&](auto I) {
+            v[decltype(I)::value] = p.scaled * __builtin_amdgcn_exp2f(__builtin_fmaf(E::template get<decltype(I)::value>(x), p.k, -p.e));
+        });
     return finish_chunk<E>(v, p.c, p.y - first);
 }
 template <class E, int NT, int C>
@@ -219,8 +265,7 @@ __device__ __forceinline__ void store_slopes(const u32x4 (&x)[C], char* out, con
 template <class E>
 __device__ __forceinline__ void store_slope(float l, char* out, const RowSpan& sp, const Slope& p, int tid) {
     const int j = sp.edge_element(tid);
-    const float v = p.scaled * __builtin_amdgcn_exp2f((l - p.m) * p.k);
-    E::put(out, j, j == p.y ? v + p.c : v);
+    E::put(out, j, j == p.y ? p(l) + p.c : p(l));
 }
 
 // Zeros to the chunks of [from, to) by NT threads, and to the rest of the row if they begin it.
@@ -256,7 +301,7 @@ enum class RowWork { Logprobs, Policy };
 struct RowArgs {
     Logits l;
     PolicyArgs policy;
-    float *logp, *lse;
+    float *logp, *logp_low, *lse;  // the last two may be null
     char* dlogits;
     int64_t ld_out, first, rows;   // rows [first, first + rows)
     const float *lse_in, *dlogp;   // of the gradient alone
@@ -273,8 +318,16 @@ __device__ __forceinline__ const char* row_of(const RowArgs& a, int64_t t, int b
 }
 __device__ __forceinline__ float scaled_weight(const RowArgs& a, int64_t t) { return a.policy.scale * (a.l.weights ? a.l.weights[t] : 1.f); }
 
-// logp from the row's maximum and sum; `ly`: the target's logit.
-__device__ __forceinline__ float logp_of(const RowArgs& a, const MaxSum& all, float ly) { return (ly - all.m) * a.l.inv_t - logf(all.s); }
+// logp and lse from the row's maximum and log sum exp(z - max z); `ly`: the target's logit.
+__device__ __forceinline__ Two logp_of(const RowArgs& a, float m, const Two& log_s, float ly) {
+    return add(scaled_difference(a.l, ly, m), log_s, -1.f);
+}
+__device__ __forceinline__ float lse_of(const RowArgs& a, float m, const Two& log_s) { return add(scaled_difference(a.l, m, 0.f), log_s, 1.f).high; }
+__device__ __forceinline__ void put_row(const RowArgs& a, int64_t t, const Two& logp, float lse) {
+    a.logp[t] = logp.high;
+    if (a.logp_low) a.logp_low[t] = logp.low;
+    if (a.lse) a.lse[t] = lse;
+}
 
 __device__ __forceinline__ void clear_ticket(const RowArgs& a) {
     if (a.ticket && blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0u;
@@ -320,12 +373,9 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
     const int64_t t = a.first + in, y = a.l.targets[t];
     const char* row = row_of(a, t, E::BYTES);
     char* out = a.dlogits + t * a.ld_out * E::BYTES;
-    const float k = kLog2e * a.l.inv_t;
+    const float k = a.l.k;
     if (!counts(a.l, t, y)) {
-        if (tid == 0) {
-            a.logp[t] = 0.f;
-            if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = 0.f;
-        }
+        if (tid == 0) put_row(a, t, Two{0.f, 0.f}, 0.f);
         if (WORK == RowWork::Policy) zero_row<E, NT>(out, V, tid);
         return;
     }
@@ -336,7 +386,7 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
     const float ly = E::one(row, y);
     const float m = fold_row<NT>(max_of<E>(x, edge), shared[0], [](float p, float q) { return fmaxf(p, q); });
     keep_packed(x);
-    const bool far = !(fabsf(m) <= 1e30f);
+    const bool far = is_far(m);
     if (far) {
         static_for<0, C>([&](auto I) {
             float v[E::VEC];
@@ -359,11 +409,10 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
     });
     s = fold_row<NT>(s, shared[1], [](float p, float q) { return p + q; });
     // log sum exp(z - max z): the sum is that of 2^(z' - e)
-    const float log_s = logf(s) - (far ? 0.f : __builtin_fmaf(m, k, -e) * kLn2), logp = (ly - m) * a.l.inv_t - log_s;
-    if (tid == 0) {
-        a.logp[t] = logp;
-        if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = m * a.l.inv_t + log_s;
-    }
+    Two log_s = two_log(s);
+    if (!far) log_s.low -= __builtin_fmaf(m, k, -e) * kLn2;
+    const Two logp = logp_of(a, m, log_s, ly);
+    if (tid == 0) put_row(a, t, logp, lse_of(a, m, log_s));
     if constexpr (WORK == RowWork::Policy) {
         const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp).slope * a.l.inv_t, scaled = -c / s;
         if constexpr (!KEEP) keep_packed(x);
@@ -390,7 +439,7 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
 
 // Rows too long for that: a workgroup a row, H chunks a thread of its end in registers; for its gradient the rest of the row is read a second
 // time, from its end, which the caches still hold.  (2048 x 131072, fp32: 560 us with nothing in
-// registers, 523 / 467 / 443 / 447 with H = 8 / 14 / 20 / 22.)
+// registers, 523 / 467 / 443 with H = 8 / 14 / 20, whose registers no longer all fit.)
 template <class E, int NT, int H, RowWork WORK>
 __global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
     __shared__ MaxSum shared[NT / 64];
@@ -399,12 +448,9 @@ __global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
     const int64_t t = a.first + die_run(blockIdx.x), y = a.l.targets[t];
     const char* row = row_of(a, t, E::BYTES);
     char* out = a.dlogits + t * a.ld_out * E::BYTES;
-    const float k = kLog2e * a.l.inv_t;
+    const float k = a.l.k;
     if (!counts(a.l, t, y)) {
-        if (tid == 0) {
-            a.logp[t] = 0.f;
-            if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = 0.f;
-        }
+        if (tid == 0) put_row(a, t, Two{0.f, 0.f}, 0.f);
         if (WORK == RowWork::Policy) zero_row<E, NT>(out, V, tid);
         return;
     }
@@ -425,14 +471,11 @@ __global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
         mine = MaxSum{m, mine.s * __builtin_amdgcn_exp2f((mine.m - base) * k) + __builtin_amdgcn_exp2f((edge - base) * k)};
     }
     const MaxSum all = join_group<NT>(mine, k, shared);
-    const float logp = logp_of(a, all, ly);
-    if (tid == 0) {
-        a.logp[t] = logp;
-        if (WORK == RowWork::Logprobs && a.lse) a.lse[t] = all.m * a.l.inv_t + logf(all.s);
-    }
+    const Two log_s = two_log(all.s), logp = logp_of(a, all.m, log_s, ly);
+    if (tid == 0) put_row(a, t, logp, lse_of(a, all.m, log_s));
     if constexpr (WORK == RowWork::Policy) {
         const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp).slope * a.l.inv_t;
-        const Slope p{k, all.m, -c / all.s, c, (int)y};
+        const Slope p = slope_of(k, all, c, y);
         if constexpr (H > 0) {
             keep_packed(x);
             store_slopes<E, NT>(x, out, sp, p, rest + tid);
@@ -456,7 +499,7 @@ __global__ __launch_bounds__(kSectionThreads) void logits_part_kernel(const RowA
     const int64_t in = blockIdx.x / (unsigned)a.sections, t = a.first + in, y = a.l.targets[t];
     if (!counts(a.l, t, y)) return;
     const char* row = row_of(a, t, E::BYTES);
-    const float k = kLog2e * a.l.inv_t;
+    const float k = a.l.k;
     const RowSpan sp = row_span<E, NT>(row, V);
     u32x4 x[C];
     load_chunks<E, NT>(x, row, sp, section * NT * C + tid);
@@ -505,9 +548,9 @@ __global__ __launch_bounds__(64) void logits_join_kernel(const RowArgs a) {
     if (in >= a.rows) return;
     const int64_t y = a.l.targets[t];
     const bool live = counts(a.l, t, y);
-    const MaxSum all = live ? join_parts(a, in, kLog2e * a.l.inv_t) : MaxSum{0.f, 1.f};
-    a.logp[t] = live ? logp_of(a, all, a.picked[in]) : 0.f;
-    if (a.lse) a.lse[t] = live ? all.m * a.l.inv_t + logf(all.s) : 0.f;
+    const MaxSum all = live ? join_parts(a, in, a.l.k) : MaxSum{0.f, 1.f};
+    const Two log_s = two_log(all.s);
+    put_row(a, t, live ? logp_of(a, all.m, log_s, a.picked[in]) : Two{0.f, 0.f}, live ? lse_of(a, all.m, log_s) : 0.f);
 }
 
 // ---------------------------------------------------------------- sums over tokens
@@ -529,7 +572,7 @@ __global__ __launch_bounds__(kSectionThreads) void policy_section_kernel(const R
     __shared__ double shared[NT / 64][4];
     const int V = (int)a.l.vocab, tid = threadIdx.x, section = (int)(blockIdx.x % (unsigned)a.sections);
     const int64_t in = blockIdx.x / (unsigned)a.sections;
-    const float k = kLog2e * a.l.inv_t;
+    const float k = a.l.k;
     if (in >= a.rows) {
         double sum[4] = {0, 0, 0, 0};
         for (int64_t t = tid; t < a.rows; t += NT) {
@@ -537,10 +580,11 @@ __global__ __launch_bounds__(kSectionThreads) void policy_section_kernel(const R
             // count left in the workspace is not used)
             const int64_t y = a.l.targets[t];
             const double w = a.l.weights ? (double)a.l.weights[t] : 1.0;
-            const float all = logp_of(a, join_parts(a, t, k), a.picked[t]);
-            const PolicyTerm p = policy_term(a.policy, t, all);
+            const MaxSum all = join_parts(a, t, k);
+            const Two logp = logp_of(a, all.m, two_log(all.s), a.picked[t]);
+            const PolicyTerm p = policy_term(a.policy, t, logp);
             const bool live = y >= 0 && y < a.l.vocab && w != 0.0;
-            a.logp[t] = live ? all : 0.f;
+            a.logp[t] = live ? logp.high : 0.f;
             if (live) add_policy_term(sum, p, w);
         }
         group_sums<NT>(sum, shared);
@@ -562,8 +606,8 @@ __global__ __launch_bounds__(kSectionThreads) void policy_section_kernel(const R
     load_chunks<E, NT>(x, row, sp, first + tid);
     const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
     const MaxSum all = join_parts_by_wave(a, in, k);
-    const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp_of(a, all, a.picked[in])).slope * a.l.inv_t;
-    const Slope p{k, all.m, -c / all.s, c, (int)y};
+    const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp_of(a, all.m, two_log(all.s), a.picked[in])).slope * a.l.inv_t;
+    const Slope p = slope_of(k, all, c, y);
     store_slopes<E, NT>(x, out, sp, p, first + tid);
     if (section == 0 && tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
 }
@@ -597,9 +641,11 @@ __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) 
     u32x4 x[C];
     load_chunks<E, NT>(x, row, sp, first + tid);
     const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
-    // p_j = 2^((l_j - lse temperature) k): the row's maximum is not known here, nor needed
-    const float c = d * a.l.inv_t;
-    const Slope p{kLog2e * a.l.inv_t, a.lse_in[t] / a.l.inv_t, -c, c, (int)y};
+    // p_j = 2^(l_j k - lse log2 e): the row's maximum is not known here, nor needed
+    const float c = d * a.l.inv_t, lse = a.lse_in[t];
+    const bool far = is_far(lse);
+    const float e = far ? 0.f : rintf(lse * kLog2e), off = far ? 0.f : __builtin_fmaf(lse, kLog2e, -e) + lse * kLog2eLow;
+    const Slope p{a.l.k, e, lse / a.l.inv_t, -c * __builtin_amdgcn_exp2f(-off), c, (int)y, far};
     store_slopes<E, NT>(x, out, sp, p, first + tid);
     if (section == 0 && tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
 }
@@ -613,7 +659,7 @@ __global__ __launch_bounds__(kSumThreads) void policy_stats_kernel(const Logits 
     __shared__ bool last;
     double sum[4] = {0, 0, 0, 0};
     for (int64_t t = (int64_t)blockIdx.x * kSumThreads + threadIdx.x; t < l.tokens; t += (int64_t)gridDim.x * kSumThreads)
-        if (counts(l, t, l.targets[t])) add_policy_term(sum, policy_term(a, t, logp[t]), l.weights ? (double)l.weights[t] : 1.0);
+        if (counts(l, t, l.targets[t])) add_policy_term(sum, policy_term(a, t, Two{logp[t], 0.f}), l.weights ? (double)l.weights[t] : 1.0);
     group_sums<kSumThreads>(sum, shared);
     if (gridDim.x > 1) {
         // the workgroup that comes last joins all of them, in their own order
@@ -633,7 +679,7 @@ __global__ __launch_bounds__(kSumThreads) void policy_stats_kernel(const Logits 
 
 // A workgroup a pair.
 __global__ __launch_bounds__(kBlock) void pair_kernel(const Logits l, const PreferenceArgs a, const PairOffsets offsets, const float* logp,
-                                                      float* dlogp, float* margins, double* terms) {
+                                                      const float* logp_low, float* dlogp, float* margins, double* terms) {
     __shared__ double shared[kBlock / 64][1];
     __shared__ double all;
     const int b = blockIdx.x;
@@ -641,7 +687,7 @@ __global__ __launch_bounds__(kBlock) void pair_kernel(const Logits l, const Pref
     double sum[1] = {0.0};
     for (int64_t t = from + threadIdx.x; t < to; t += kBlock) {
         if (!counts(l, t, l.targets[t])) continue;
-        const double d = ((double)logp[t] - (double)a.ref_logp[t]) * (l.weights ? (double)l.weights[t] : 1.0);
+        const double d = (((double)logp[t] - (double)a.ref_logp[t]) + (double)logp_low[t]) * (l.weights ? (double)l.weights[t] : 1.0);
         sum[0] += t < mid ? d : -d;
     }
     group_sums<kBlock>(sum, shared);
@@ -708,7 +754,7 @@ void launch_rows_of(const RowArgs& a, hipStream_t stream) {
     if (chunks <= 8192) return logits_held_kernel<E, 1024, 8, 1, WORK><<<rows, 1024, 0, stream>>>(a);
     if constexpr (WORK == RowWork::Policy) {
         if (chunks <= 16384) return logits_held_kernel<E, 1024, 16, 1, WORK><<<rows, 1024, 0, stream>>>(a);
-        logits_scan_kernel<E, 1024, 20, WORK><<<rows, 1024, 0, stream>>>(a);
+        logits_scan_kernel<E, 1024, 18, WORK><<<rows, 1024, 0, stream>>>(a);
     } else {
         logits_scan_kernel<E, 512, 0, WORK><<<rows, 512, 0, stream>>>(a);
     }
@@ -772,10 +818,12 @@ size_t logprobs_workspace(int dtype, int64_t tokens, int64_t vocab) {
 }
 size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab) { return policy_space(dtype, tokens, vocab).total; }
 
-hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* lse, void* workspace, hipStream_t stream) {
+hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, void* workspace,
+                           hipStream_t stream) {
     RowArgs a{};
     a.l = l;
     a.logp = logp;
+    a.logp_low = logp_low;
     a.lse = lse;
     const Sections s = workspace ? sections_of(l.dtype, count, l.vocab, kLogprobsSections) : Sections{0, 0};
     if (s.count > 1) {
@@ -854,10 +902,10 @@ hipError_t launch_policy(const Logits& l, const PolicyArgs& p, float* logp, void
     return hipGetLastError();
 }
 
-hipError_t launch_pairs(const Logits& l, const PreferenceArgs& a, const PairOffsets& offsets, int pairs, const float* logp, float* dlogp,
-                        float* margins, double* terms, hipStream_t stream) {
+hipError_t launch_pairs(const Logits& l, const PreferenceArgs& a, const PairOffsets& offsets, int pairs, const float* logp,
+                        const float* logp_low, float* dlogp, float* margins, double* terms, hipStream_t stream) {
     if (pairs <= 0) return hipSuccess;
-    pair_kernel<<<dim3((unsigned)pairs), kBlock, 0, stream>>>(l, a, offsets, logp, dlogp, margins, terms);
+    pair_kernel<<<dim3((unsigned)pairs), kBlock, 0, stream>>>(l, a, offsets, logp, logp_low, dlogp, margins, terms);
     return hipGetLastError();
 }
 

@@ -20,7 +20,8 @@ struct Logits {
     int64_t tokens, vocab, ld;
     const int64_t* targets;
     const float* weights;  // null: all 1; a token of weight 0 does not count
-    float inv_t;           // 1 / temperature
+    float inv_t, inv_t_low;   // 1 / temperature, and what rounding it left
+    float k;                  // log2(e) / temperature
 };
 
 struct PolicyArgs {
@@ -33,7 +34,9 @@ size_t logprobs_workspace(int dtype, int64_t tokens, int64_t vocab);
 size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab);
 
 // logp, lse (may be null) of rows [first, first + count).  Without a workspace a row is one workgroup's.
-hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* lse, void* workspace, hipStream_t stream);
+// `logp_low`, if not null: what rounding the log-probabilities to `logp` left.
+hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, void* workspace,
+                           hipStream_t stream);
 // The loss of pairs from their terms (one double each).
 struct PairLoss {
     const double* terms;
@@ -58,8 +61,8 @@ struct PreferenceArgs {
     float scale, beta, smooth;
 };
 // Margins of `pairs` pairs, their tokens' derivatives and the terms of the loss (one double a pair).
-hipError_t launch_pairs(const Logits& l, const PreferenceArgs& a, const PairOffsets& offsets, int pairs, const float* logp, float* dlogp,
-                        float* margins, double* terms, hipStream_t stream);
+hipError_t launch_pairs(const Logits& l, const PreferenceArgs& a, const PairOffsets& offsets, int pairs, const float* logp,
+                        const float* logp_low, float* dlogp, float* margins, double* terms, hipStream_t stream);
 hipError_t launch_pair_loss(const PairLoss& loss, hipStream_t stream);
 
 // ---------------------------------------------------------------- saved activations

@@ -44,7 +44,7 @@ star_status check_logits(const void* logits, int dtype, int64_t tokens, int64_t 
     if (vocab < 1 || vocab > kMostVocab) return set_error(STAR_ERR_SHAPE, "vocab is below 1 or above 2^30");
     if (!rows_fit(tokens, vocab, ld)) return set_error(STAR_ERR_SHAPE, "ld is below vocab, or the logits are too large");
     if (dlogits && !rows_fit(tokens, vocab, ld_out)) return set_error(STAR_ERR_SHAPE, "ld_out is below vocab, or the gradient is too large");
-    if (!positive(temperature) || !std::isfinite(1.f / temperature)) return set_error(STAR_ERR_HPARAM, "temperature must be positive and finite");
+    if (!positive(temperature) || !std::isfinite(2.f / temperature)) return set_error(STAR_ERR_HPARAM, "temperature must be positive and finite");
     if (tokens == 0) return STAR_OK;
     if (!logits || !targets) return set_error(STAR_ERR_NULL, "logits or targets is NULL");
     if (!on_grid(logits, bytes_of(dtype)) || !on_grid(dlogits, bytes_of(dtype)) || !on_grid(targets, 8))
@@ -55,14 +55,16 @@ star_status check_logits(const void* logits, int dtype, int64_t tokens, int64_t 
 
 star::Logits make_logits(const void* x, int dtype, int64_t tokens, int64_t vocab, int64_t ld, const int64_t* targets, const float* weights,
                          float temperature) {
-    return star::Logits{x, dtype, tokens, vocab, ld, targets, weights, 1.f / temperature};
+    const double inverse = 1.0 / (double)temperature;
+    const float rounded = (float)inverse;
+    return star::Logits{x, dtype, tokens, vocab, ld, targets, weights, rounded, (float)(inverse - rounded), (float)(1.4426950408889634 * inverse)};
 }
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-// Workspace of the preference loss: terms [pairs] double, then lse, dlogp, logp [tokens] float, then that of the log-probabilities.
+// Workspace of the preference loss: terms [pairs] double, then lse, dlogp, logp, logp_low [tokens] float, then that of the log-probabilities.
 struct PreferenceSpace {
-    size_t terms, lse, dlogp, logp, rows, total;
+    size_t terms, lse, dlogp, logp, logp_low, rows, total;
 };
 PreferenceSpace preference_space(int dtype, int64_t tokens, int64_t vocab, int32_t pairs) {
     PreferenceSpace s;
@@ -71,7 +73,8 @@ PreferenceSpace preference_space(int dtype, int64_t tokens, int64_t vocab, int32
     s.lse = round16(sizeof(double) * (size_t)pairs);
     s.dlogp = s.lse + each;
     s.logp = s.dlogp + each;
-    s.rows = s.logp + each;
+    s.logp_low = s.logp + each;
+    s.rows = s.logp_low + each;
     s.total = s.rows + round16(star::logprobs_workspace(dtype, tokens, vocab));
     return s;
 }
@@ -122,7 +125,7 @@ star_status star_token_logprobs(const void* logits, star_dtype dtype, int64_t to
     if (!logp_out) return set_error(STAR_ERR_NULL, "logp_out is NULL");
     STAR_CHECK(check_workspace(workspace, workspace_bytes, star_token_logprobs_workspace(dtype, tokens, vocab)));
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, nullptr, temperature);
-    STAR_LAUNCH(star::launch_logprobs(l, 0, tokens, logp_out, lse_out, workspace, static_cast<hipStream_t>(hip_stream)));
+    STAR_LAUNCH(star::launch_logprobs(l, 0, tokens, logp_out, nullptr, lse_out, workspace, static_cast<hipStream_t>(hip_stream)));
     return STAR_OK;
 }
 
@@ -183,7 +186,7 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     double* terms = at<double>(workspace, space.terms);
     float *lse = at<float>(workspace, space.lse), *dlogp = at<float>(workspace, space.dlogp);
-    float* logp = logp_out ? logp_out : at<float>(workspace, space.logp);
+    float *logp = logp_out ? logp_out : at<float>(workspace, space.logp), *logp_low = at<float>(workspace, space.logp_low);
     const star::PairLoss loss{terms, pairs, params->scale, loss_out};
     bool joined = false;
     void* rows = space.total > space.rows ? at<char>(workspace, space.rows) : nullptr;
@@ -192,8 +195,8 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
         star::PairOffsets o{};
         for (int i = 0; i <= 2 * n; ++i) o.at[i] = offsets[2 * (int64_t)first + i];
         const int64_t from = o.at[0], count = o.at[2 * n] - from;
-        STAR_LAUNCH(star::launch_logprobs(l, from, count, logp, dlogits ? lse : nullptr, count == tokens ? rows : nullptr, stream));
-        STAR_LAUNCH(star::launch_pairs(l, a, o, n, logp, dlogits ? dlogp : nullptr, margins_out ? margins_out + first : nullptr, terms + first,
+        STAR_LAUNCH(star::launch_logprobs(l, from, count, logp, logp_low, dlogits ? lse : nullptr, count == tokens ? rows : nullptr, stream));
+        STAR_LAUNCH(star::launch_pairs(l, a, o, n, logp, logp_low, dlogits ? dlogp : nullptr, margins_out ? margins_out + first : nullptr, terms + first,
                                        stream));
         const bool last = first + n == pairs && count > 0;   // the loss is joined beside the last gradient
         if (dlogits) STAR_LAUNCH(star::launch_logprobs_grad(l, from, count, lse, dlogp, dlogits, ld_out, last ? loss : star::PairLoss{}, stream));
