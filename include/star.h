@@ -493,7 +493,7 @@ star_status star_plan_even_split(int32_t workgroups, int64_t tiles, int64_t *fir
  * token that does not count (a prompt, padding): its row is not read, its log-probability is reported as 0, its
  * gradient row is zero.  dlogits has the shape and type of the logits, rows at t * ld_out; it may be the logits
  * themselves (same address, same ld), but must not overlap them otherwise.  Addresses need the alignment of one
- * element only.  With z = logits / temperature, logp = z[target] - lse, lse = log sum exp z.  Values of -inf (banned
+ * element only.  With z = logits / temperature (1e-4 to 1e4), logp = z[target] - lse, lse = log sum exp z.  Values of -inf (banned
  * tokens) have probability 0; a row of nothing else, or one that holds NaN or +inf, has a log-probability of NaN.
  * All arithmetic is fp32 or wider; a gradient is rounded once, to its own type.  Results are the same from run to run.
  *
@@ -534,7 +534,7 @@ typedef struct {
     float scale;
     float clip_low, clip_high; /* >= 0; clip_high may be infinite                     */
     float kl_coef;             /* >= 0                                                */
-    float temperature;         /* > 0                                                 */
+    float temperature;         /* 1e-4 to 1e4                                         */
 } star_policy_params;
 
 star_status star_policy_loss(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
@@ -558,8 +558,8 @@ star_status star_policy_loss(const void *logits, star_dtype dtype, int64_t token
 typedef struct {
     float scale;
     float beta;
-    float label_smoothing; /* 0 to 1 */
-    float temperature;     /* > 0    */
+    float label_smoothing; /* 0 to 1      */
+    float temperature;     /* 1e-4 to 1e4 */
 } star_preference_params;
 
 star_status star_preference_loss(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,

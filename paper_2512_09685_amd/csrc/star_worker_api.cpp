@@ -21,7 +21,6 @@ constexpr int64_t kMostWidth = (int64_t)1 << 22;      // columns of a weight gra
 bool known(int dtype) { return dtype == STAR_F32 || dtype == STAR_BF16; }
 size_t bytes_of(int dtype) { return dtype == STAR_F32 ? 4 : 2; }
 bool on_grid(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-bool positive(float x) { return std::isfinite(x) && x > 0.f; }
 
 // `rows` rows of `length` values, `ld` apart: no size negative, no offset beyond 63 bits.
 bool rows_fit(int64_t rows, int64_t length, int64_t ld) {
@@ -44,7 +43,7 @@ star_status check_logits(const void* logits, int dtype, int64_t tokens, int64_t 
     if (vocab < 1 || vocab > kMostVocab) return set_error(STAR_ERR_SHAPE, "vocab is below 1 or above 2^30");
     if (!rows_fit(tokens, vocab, ld)) return set_error(STAR_ERR_SHAPE, "ld is below vocab, or the logits are too large");
     if (dlogits && !rows_fit(tokens, vocab, ld_out)) return set_error(STAR_ERR_SHAPE, "ld_out is below vocab, or the gradient is too large");
-    if (!positive(temperature) || !std::isfinite(2.f / temperature)) return set_error(STAR_ERR_HPARAM, "temperature must be positive and finite");
+    if (!(temperature >= 1e-4f && temperature <= 1e4f)) return set_error(STAR_ERR_HPARAM, "temperature must lie in 1e-4 to 1e4");
     if (tokens == 0) return STAR_OK;
     if (!logits || !targets) return set_error(STAR_ERR_NULL, "logits or targets is NULL");
     if (!on_grid(logits, bytes_of(dtype)) || !on_grid(dlogits, bytes_of(dtype)) || !on_grid(targets, 8))

@@ -34,7 +34,7 @@ BAD_LOGITS = [
     (dict(vocab=(1 << 30) + 1, ld=1 << 31), SHAPE), (dict(ld=9), SHAPE), (dict(ld=1 << 62), SHAPE), (dict(x=P + 1), SHAPE),
     (dict(dtype=F32, x=P + 2), SHAPE), (dict(targets=P + 4), SHAPE),
 ]
-BAD_TEMPERATURE = [0.0, -1.0, float("nan"), float("inf"), 1e-45]
+BAD_TEMPERATURE = [0.0, -1.0, float("nan"), float("inf"), 1e-45, 5e-5, 2e4]
 
 
 def _head(change):
