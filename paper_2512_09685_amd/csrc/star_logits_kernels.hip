@@ -307,7 +307,7 @@ struct RowArgs {
     const float *lse_in, *dlogp;   // of the gradient alone
     MaxSum* parts;                 // of rows that several workgroups share: [rows][sections]
     float* picked;                 // of such rows: the target's logit, which a gradient in place would be written over
-    int sections;
+    int sections, lanes;           // lanes that join a row's sections: a power of two, no more than a wave's
     float* stats;
     PairLoss loss;                 // of the pairs whose gradient this is; its output null: none
     unsigned int* ticket;          // cleared for the launch behind this one; null: it needs none
@@ -512,45 +512,42 @@ __global__ __launch_bounds__(kSectionThreads) void logits_part_kernel(const RowA
     if (tid == 0 && section == 0) a.picked[in] = E::one(row, y);
 }
 
-// The sections of a row joined by one thread, 16 of them on their way at a time; and by a wave, one a lane.
+// The sections of a row joined by `a.lanes` lanes side by side, four sections of each on their way at a time; every lane gets the whole.
+// All launches of a call join a row this way, with as many lanes: the gradient and the sums then rest on the same bits.
 __device__ __forceinline__ MaxSum join_parts(const RowArgs& a, int64_t in, float k) {
     const MaxSum* p = a.parts + in * a.sections;
-    MaxSum all{-INFINITY, 0.f};
-    for (int first = 0; first < a.sections; first += 16) {
-        MaxSum x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = first + i < a.sections ? p[first + i] : MaxSum{-INFINITY, 0.f};
-        float m = all.m;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) m = fmaxf(m, x[i].m);
-        const float base = m == -INFINITY ? 0.f : m;
-        float s = all.s * __builtin_amdgcn_exp2f((all.m - base) * k);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s += x[i].s * __builtin_amdgcn_exp2f((x[i].m - base) * k);
-        all = MaxSum{m, s};
-    }
-    return all;
-}
-__device__ __forceinline__ MaxSum join_parts_by_wave(const RowArgs& a, int64_t in, float k) {
-    const MaxSum* p = a.parts + in * a.sections;
+    const int lane = (int)threadIdx.x & (a.lanes - 1);
     MaxSum mine{-INFINITY, 0.f};
-    for (int i = threadIdx.x & 63; i < a.sections; i += 64) {
-        const MaxSum x = p[i];
-        const float m = fmaxf(mine.m, x.m), base = m == -INFINITY ? 0.f : m;
-        mine = MaxSum{m, mine.s * __builtin_amdgcn_exp2f((mine.m - base) * k) + x.s * __builtin_amdgcn_exp2f((x.m - base) * k)};
+    for (int first = lane; first < a.sections; first += 4 * a.lanes) {
+        MaxSum x[4];
+        float m = mine.m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = first + i * a.lanes < a.sections ? p[first + i * a.lanes] : MaxSum{-INFINITY, 0.f};
+            m = fmaxf(m, x[i].m);
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        mine = MaxSum{m, mine.s * __builtin_amdgcn_exp2f((mine.m - base) * k)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine.s += x[i].s * __builtin_amdgcn_exp2f((x[i].m - base) * k);
     }
-    return join_wave(mine, k);
+    float m = mine.m;
+    for (int d = a.lanes / 2; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    float s = mine.s * __builtin_amdgcn_exp2f((mine.m - (m == -INFINITY ? 0.f : m)) * k);
+    for (int d = a.lanes / 2; d; d >>= 1) s += __shfl_xor(s, d);
+    return MaxSum{m, s};
 }
 
-// Second launch of the log-probabilities: a thread a row.
-__global__ __launch_bounds__(64) void logits_join_kernel(const RowArgs a) {
-    const int64_t in = (int64_t)blockIdx.x * 64 + threadIdx.x, t = a.first + in;
+// Second launch of the log-probabilities: one workgroup, `a.lanes` lanes a row.
+__global__ __launch_bounds__(kSectionThreads) void logits_join_kernel(const RowArgs a) {
+    const int64_t in = threadIdx.x / (unsigned)a.lanes, t = a.first + in;
     if (in >= a.rows) return;
     const int64_t y = a.l.targets[t];
     const bool live = counts(a.l, t, y);
     const MaxSum all = live ? join_parts(a, in, a.l.k) : MaxSum{0.f, 1.f};
     const Two log_s = two_log(all.s);
-    put_row(a, t, live ? logp_of(a, all.m, log_s, a.picked[in]) : Two{0.f, 0.f}, live ? lse_of(a, all.m, log_s) : 0.f);
+    if ((threadIdx.x & (a.lanes - 1)) == 0)
+        put_row(a, t, live ? logp_of(a, all.m, log_s, a.picked[in]) : Two{0.f, 0.f}, live ? lse_of(a, all.m, log_s) : 0.f);
 }
 
 // ---------------------------------------------------------------- sums over tokens
@@ -575,7 +572,8 @@ __global__ __launch_bounds__(kSectionThreads) void policy_section_kernel(const R
     const float k = a.l.k;
     if (in >= a.rows) {
         double sum[4] = {0, 0, 0, 0};
-        for (int64_t t = tid; t < a.rows; t += NT) {
+        const int64_t t = tid / a.lanes;
+        if (t < a.rows) {
             // (everything is read before anything is decided: this workgroup is the one that the others wait for; what a row that does not
             // count left in the workspace is not used)
             const int64_t y = a.l.targets[t];
@@ -584,8 +582,10 @@ __global__ __launch_bounds__(kSectionThreads) void policy_section_kernel(const R
             const Two logp = logp_of(a, all.m, two_log(all.s), a.picked[t]);
             const PolicyTerm p = policy_term(a.policy, t, logp);
             const bool live = y >= 0 && y < a.l.vocab && w != 0.0;
-            a.logp[t] = live ? logp.high : 0.f;
-            if (live) add_policy_term(sum, p, w);
+            if ((tid & (a.lanes - 1)) == 0) {
+                a.logp[t] = live ? logp.high : 0.f;
+                if (live) add_policy_term(sum, p, w);
+            }
         }
         group_sums<NT>(sum, shared);
         if (tid == 0)
@@ -605,7 +605,7 @@ __global__ __launch_bounds__(kSectionThreads) void policy_section_kernel(const R
     u32x4 x[C];
     load_chunks<E, NT>(x, row, sp, first + tid);
     const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
-    const MaxSum all = join_parts_by_wave(a, in, k);
+    const MaxSum all = join_parts(a, in, k);
     const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp_of(a, all.m, two_log(all.s), a.picked[in])).slope * a.l.inv_t;
     const Slope p = slope_of(k, all, c, y);
     store_slopes<E, NT>(x, out, sp, p, first + tid);
@@ -653,13 +653,14 @@ __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) 
 // Workspace of the sums: a ticket, then four doubles a workgroup.
 constexpr int kStatsGroups = 64;
 
-__global__ __launch_bounds__(kSumThreads) void policy_stats_kernel(const Logits l, const PolicyArgs a, const float* logp, float* stats,
-                                                                   unsigned int* ticket, double* sums) {
+// (a token's ratio comes from the same two numbers as in the launch that made its gradient, so that both say the same of the clip's border)
+__global__ __launch_bounds__(kSumThreads) void policy_stats_kernel(const Logits l, const PolicyArgs a, const float* logp, const float* logp_low,
+                                                                   float* stats, unsigned int* ticket, double* sums) {
     __shared__ double shared[kSumThreads / 64][4];
     __shared__ bool last;
     double sum[4] = {0, 0, 0, 0};
     for (int64_t t = (int64_t)blockIdx.x * kSumThreads + threadIdx.x; t < l.tokens; t += (int64_t)gridDim.x * kSumThreads)
-        if (counts(l, t, l.targets[t])) add_policy_term(sum, policy_term(a, t, Two{logp[t], 0.f}), l.weights ? (double)l.weights[t] : 1.0);
+        if (counts(l, t, l.targets[t])) add_policy_term(sum, policy_term(a, t, Two{logp[t], logp_low[t]}), l.weights ? (double)l.weights[t] : 1.0);
     group_sums<kSumThreads>(sum, shared);
     if (gridDim.x > 1) {
         // the workgroup that comes last joins all of them, in their own order
@@ -732,6 +733,14 @@ Sections sections_of(int dtype, int64_t tokens, int64_t vocab, int64_t least) {
     return Sections{c, (int)((chunks + kSectionThreads * c - 1) / (kSectionThreads * c))};
 }
 
+// Lanes that join the sections of a row, where one workgroup joins all rows (kFewTokens at most).
+static_assert(kFewTokens <= kSectionThreads);
+int join_lanes(int64_t rows) {
+    int lanes = 64;
+    while (lanes > 1 && rows * lanes > kSectionThreads) lanes /= 2;
+    return lanes;
+}
+
 template <class E, class F>
 void for_section(const Sections& s, F&& launch) {
     if (s.chunks_a_thread == 8) launch(std::integral_constant<int, 8>{});
@@ -780,16 +789,17 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 size_t parts_bytes(const Sections& s, int64_t tokens) { return round16(sizeof(MaxSum) * (size_t)tokens * (size_t)s.count); }
 size_t section_bytes(const Sections& s, int64_t tokens) { return s.count ? parts_bytes(s, tokens) + round16(sizeof(float) * (size_t)tokens) : 0; }
 
-// Workspace of the policy loss: ticket | sums of the workgroups | sections | log-probabilities.
+// Workspace of the policy loss: ticket | sums of the workgroups | sections | log-probabilities, their lower parts.
 struct PolicySpace {
-    size_t sums, parts, logp, total;
+    size_t sums, parts, logp, logp_low, total;
 };
 PolicySpace policy_space(int dtype, int64_t tokens, int64_t vocab) {
     PolicySpace s;
     s.sums = 16;
     s.parts = s.sums + sizeof(double) * 4 * kStatsGroups;
     s.logp = s.parts + section_bytes(sections_of(dtype, tokens, vocab, kPolicySections), tokens);
-    s.total = s.logp + round16(sizeof(float) * (size_t)tokens);
+    s.logp_low = s.logp + round16(sizeof(float) * (size_t)tokens);
+    s.total = s.logp_low + round16(sizeof(float) * (size_t)tokens);
     return s;
 }
 template <class T>
@@ -832,11 +842,12 @@ hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float*
         a.parts = at<MaxSum>(workspace, 0);
         a.picked = at<float>(workspace, parts_bytes(s, count));
         a.sections = s.count;
-        const unsigned grid = (unsigned)(count * s.count), joins = (unsigned)((count + 63) / 64);
+        a.lanes = join_lanes(count);
+        const unsigned grid = (unsigned)(count * s.count);
         auto both = [&](auto elem) {
             typedef decltype(elem) E;
             for_section<E>(s, [&](auto C) { logits_part_kernel<E, decltype(C)::value><<<grid, kSectionThreads, 0, stream>>>(a); });
-            logits_join_kernel<<<joins, 64, 0, stream>>>(a);
+            logits_join_kernel<<<1, kSectionThreads, 0, stream>>>(a);
         };
         if (l.dtype == STAR_F32) both(ElemF32{});
         else both(ElemBf16{});
@@ -879,6 +890,7 @@ hipError_t launch_policy(const Logits& l, const PolicyArgs& p, float* logp, void
         a.parts = at<MaxSum>(workspace, space.parts);
         a.picked = at<float>(workspace, space.parts + parts_bytes(s, l.tokens));
         a.sections = s.count;
+        a.lanes = join_lanes(l.tokens);
         a.stats = stats;
         const unsigned grid = (unsigned)(l.tokens * s.count);
         auto both = [&](auto elem) {
@@ -892,12 +904,13 @@ hipError_t launch_policy(const Logits& l, const PolicyArgs& p, float* logp, void
     }
     const int64_t groups = std::min<int64_t>(kStatsGroups, (l.tokens + 4 * kSumThreads - 1) / (4 * kSumThreads));
     a.ticket = groups > 1 ? at<unsigned int>(workspace, 0) : nullptr;
+    if (l.tokens > 0) a.logp_low = at<float>(workspace, space.logp_low);
     const hipError_t e = in_launches(a, 0, l.tokens, [&](const RowArgs& r) {
         if (!dlogits) l.dtype == STAR_F32 ? launch_rows_of<ElemF32, RowWork::Logprobs>(r, stream) : launch_rows_of<ElemBf16, RowWork::Logprobs>(r, stream);
         else l.dtype == STAR_F32 ? launch_rows_of<ElemF32, RowWork::Policy>(r, stream) : launch_rows_of<ElemBf16, RowWork::Policy>(r, stream);
     });
     if (e != hipSuccess) return e;
-    policy_stats_kernel<<<dim3((unsigned)std::max<int64_t>(1, groups)), kSumThreads, 0, stream>>>(l, p, a.logp, stats, a.ticket,
+    policy_stats_kernel<<<dim3((unsigned)std::max<int64_t>(1, groups)), kSumThreads, 0, stream>>>(l, p, a.logp, a.logp_low, stats, a.ticket,
                                                                                                  groups > 1 ? at<double>(workspace, space.sums) : nullptr);
     return hipGetLastError();
 }

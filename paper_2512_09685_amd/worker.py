@@ -13,6 +13,7 @@ import numpy as np
 from .binding import BF16, F32, StarError, _stream_handle, last_error, load_library
 
 _lib = None
+_ERR_NULL = 1     # STAR_ERR_NULL
 
 
 class _PolicyParams(ctypes.Structure):
@@ -99,7 +100,7 @@ def _vector(x, dtype, n: int, what: str, device: int):
     if x.dtype is not dtype or x.dim() != 1 or x.size(0) != n or not x.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor [{n}]")
     if x.get_device() != device:
-        raise ValueError(f"{what} must be on the logits' device")
+        raise ValueError(f"{what} must be on the first tensor's device")
     return x.data_ptr()
 
 
@@ -117,6 +118,12 @@ def _logits(logits, targets, dlogits=None):
     return (x, code, tokens, vocab, ld, _vector(targets, _i64, tokens, "targets", device)), (out, ld_out), device
 
 
+def _on_gpu(device: int):
+    """A kernel must not be given the address of host memory, which it would fault on."""
+    if device < 0:
+        raise ValueError("the tensors must be in GPU memory")
+
+
 @functools.lru_cache(maxsize=4096)
 def _need(name: str, *sizes) -> int:
     """Workspace bytes of a call, by its sizes."""
@@ -126,19 +133,18 @@ def _need(name: str, *sizes) -> int:
 def _workspace(given, need: int, device: int, stream):
     """(address, bytes, the tensor to keep until the call is enqueued)."""
     if given is not None:
-        if given.element_size() != 1 or not given.is_contiguous():
-            raise ValueError("workspace must be a contiguous uint8 tensor")
+        if given.element_size() != 1 or not given.is_contiguous() or given.get_device() != device:
+            raise ValueError("workspace must be a contiguous uint8 tensor on the same device")
         return given.data_ptr(), given.numel(), given
     if need == 0:
         return None, 0, None
-    where = "cpu" if device < 0 else device
-    if stream is None or device < 0:
-        w = _torch.empty(need, dtype=_torch.uint8, device=where)
+    if stream is None:
+        w = _torch.empty(need, dtype=_torch.uint8, device=device)
     else:
         # on the call's own stream, so that the memory is not handed out again before the call has run
-        s = stream if isinstance(stream, _torch.cuda.Stream) else _torch.cuda.ExternalStream(int(stream), device=where)
+        s = stream if isinstance(stream, _torch.cuda.Stream) else _torch.cuda.ExternalStream(int(stream), device=device)
         with _torch.cuda.stream(s):
-            w = _torch.empty(need, dtype=_torch.uint8, device=where)
+            w = _torch.empty(need, dtype=_torch.uint8, device=device)
     return w.data_ptr(), need, w
 
 
@@ -151,6 +157,7 @@ def star_token_logprobs(logits, targets, logp_out, *, lse_out=None, temperature:
     head, _, device = _logits(logits, targets)
     tokens = head[2]
     logp, lse = _vector(logp_out, _f32, tokens, "logp_out", device), _vector(lse_out, _f32, tokens, "lse_out", device)
+    _on_gpu(device)
     w, size, _keep = _workspace(workspace, _need("star_token_logprobs_workspace", *head[1:4]), device, stream)
     _check(lib.star_token_logprobs(*head, temperature, logp, lse, w, size, _stream_handle(stream)))
 
@@ -161,8 +168,9 @@ def star_token_logprobs_grad(logits, targets, lse, dlogp, dlogits, *, temperatur
     lib = _library()
     head, out, device = _logits(logits, targets, dlogits)
     tokens = head[2]
-    _check(lib.star_token_logprobs_grad(*head, temperature, _vector(lse, _f32, tokens, "lse", device),
-                                        _vector(dlogp, _f32, tokens, "dlogp", device), *out, _stream_handle(stream)))
+    normaliser, slope = _vector(lse, _f32, tokens, "lse", device), _vector(dlogp, _f32, tokens, "dlogp", device)
+    _on_gpu(device)
+    _check(lib.star_token_logprobs_grad(*head, temperature, normaliser, slope, *out, _stream_handle(stream)))
 
 
 def star_policy_loss(logits, targets, old_logp, advantages, stats_out, *, dlogits=None, ref_logp=None, weights=None,
@@ -177,6 +185,9 @@ def star_policy_loss(logits, targets, old_logp, advantages, stats_out, *, dlogit
     old, ref = _vector(old_logp, _f32, n, "old_logp", device), _vector(ref_logp, _f32, n, "ref_logp", device)
     adv, wts = _vector(advantages, _f32, n, "advantages", device), _vector(weights, _f32, n, "weights", device)
     logp, stats = _vector(logp_out, _f32, n, "logp_out", device), _vector(stats_out, _f32, 4, "stats_out", device)
+    if kl_coef and ref is None:
+        raise StarError(_ERR_NULL, "ref_logp is NULL and kl_coef is not 0")
+    _on_gpu(device)
     w, size, _keep = _workspace(workspace, _need("star_policy_loss_workspace", *head[1:4]), device, stream)
     _check(lib.star_policy_loss(*head, old, ref, adv, wts, ctypes.byref(p), *out, logp, stats, w, size,
                                 _stream_handle(stream)))
@@ -199,6 +210,7 @@ def star_preference_loss(logits, targets, ref_logp, offsets, loss_out, *, dlogit
     ref, wts = _vector(ref_logp, _f32, n, "ref_logp", device), _vector(weights, _f32, n, "weights", device)
     logp, margins = _vector(logp_out, _f32, n, "logp_out", device), _vector(margins_out, _f32, pairs, "margins_out", device)
     loss = _vector(loss_out, _f32, 1, "loss_out", device)
+    _on_gpu(device)
     w, size, _keep = _workspace(workspace, _need("star_preference_loss_workspace", *head[1:4], pairs), device, stream)
     _check(lib.star_preference_loss(*head, ref, wts, pairs, at.ctypes.data, ctypes.byref(p), *out, logp, margins, loss, w,
                                     size, _stream_handle(stream)))
@@ -222,16 +234,20 @@ def star_act_pack(x, packed, *, stream=None) -> None:
     ``star_act_bytes(tokens, width)`` bytes."""
     code = _dtype(x, "x")
     p, tokens, width, ld = _matrix(x, "x")
-    _check(_library().star_act_pack(p, code, tokens, width, ld, _packed(packed, tokens, width, x.get_device()),
-                                    _stream_handle(stream)))
+    device = x.get_device()
+    to = _packed(packed, tokens, width, device)
+    _on_gpu(device)
+    _check(_library().star_act_pack(p, code, tokens, width, ld, to, _stream_handle(stream)))
 
 
 def star_act_unpack(packed, out, *, stream=None) -> None:
     """The kept values of ``packed``, into ``out`` (float32 or bfloat16 [tokens, width])."""
     code = _dtype(out, "out")
     p, tokens, width, ld = _matrix(out, "out")
-    _check(_library().star_act_unpack(_packed(packed, tokens, width, out.get_device()), tokens, width, p, code, ld,
-                                      _stream_handle(stream)))
+    device = out.get_device()
+    source = _packed(packed, tokens, width, device)
+    _on_gpu(device)
+    _check(_library().star_act_unpack(source, tokens, width, p, code, ld, _stream_handle(stream)))
 
 
 def star_act_weight_grad(dy, packed, dw, *, accumulate: bool = False, workspace=None, stream=None) -> None:
@@ -247,6 +263,8 @@ def star_act_weight_grad(dy, packed, dw, *, accumulate: bool = False, workspace=
     if dw.get_device() != device:
         raise ValueError("dw must be on dy's device")
     width = dw.size(1)
+    kept = _packed(packed, tokens, width, device)
+    _on_gpu(device)
     w, size, _keep = _workspace(workspace, _need("star_act_weight_grad_workspace", dy_code, tokens, out, width), device, stream)
-    _check(lib.star_act_weight_grad(p, dy_code, tokens, out, ld, _packed(packed, tokens, width, device), width,
-                                    dw.data_ptr(), dw_code, int(bool(accumulate)), w, size, _stream_handle(stream)))
+    _check(lib.star_act_weight_grad(p, dy_code, tokens, out, ld, kept, width, dw.data_ptr(), dw_code,
+                                    int(bool(accumulate)), w, size, _stream_handle(stream)))

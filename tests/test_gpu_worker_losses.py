@@ -374,3 +374,15 @@ def test_rows_far_into_a_long_buffer():
     star.star_policy_loss(x, i64(y), logp, f32([1, 1, 1]), stats, dlogits=x, scale=1.0)
     wd = wo.dlogits_of(p, y, live, -np.ones(T))
     close(x, wd, wo.gradient_bound(wd, p, y, live, np.ones(T), 64 * wo.U * np.ones(T), bound, "bf16"), "dlogits")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(300, 1000), (5000, 77), (6, 20000), (200, 9000)])
+def test_gradient_and_sums_agree_on_the_clip(T, V, dtype):
+    """A clip range of 0 and old log-probabilities that are the present ones: the ratios lie on the border up to what rounding the
+    log-probabilities left.  A token is counted as clipped exactly where its gradient row is zero."""
+    x, _, y, rng = make(T, V, dtype, seed=11)
+    y, logp, stats, d = i64(y), torch.zeros(T, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros_like(x)
+    star.star_token_logprobs(x, y, logp)
+    star.star_policy_loss(x, y, logp, f32(rng.choice([-1, 1], T)), stats, dlogits=d, clip_low=0.0, clip_high=0.0, scale=1.0)
+    assert float(stats[2]) == float((d == 0).all(dim=1).sum())

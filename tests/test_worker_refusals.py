@@ -206,3 +206,19 @@ def test_binding_refuses_tensors_of_other_kinds():
     with pytest.raises(star.StarError) as e:
         star.star_policy_loss(x, y, f, f, torch.zeros(4), kl_coef=0.1, stream=0)
     assert e.value.status == NULL
+
+
+def test_binding_refuses_host_memory():
+    """Tensors that are all well formed but lie on the host: no kernel gets their addresses."""
+    T, V = 4, 10
+    x, y, f = torch.zeros(T, V), torch.zeros(T, dtype=torch.int64), torch.zeros(T)
+    packed = torch.zeros(star.star_act_bytes(T, V), dtype=torch.uint8)
+    for call in (lambda: star.star_token_logprobs(x, y, f, stream=0),
+                 lambda: star.star_token_logprobs_grad(x, y, f, f, x.clone(), stream=0),
+                 lambda: star.star_policy_loss(x, y, f, f, torch.zeros(4), stream=0),
+                 lambda: star.star_preference_loss(x, y, f, [0, 2, 4], f[:1], stream=0),
+                 lambda: star.star_act_pack(x, packed, stream=0),
+                 lambda: star.star_act_unpack(packed, x, stream=0),
+                 lambda: star.star_act_weight_grad(torch.zeros(T, 6), packed, torch.zeros(6, V), stream=0)):
+        with pytest.raises(ValueError, match="GPU memory"):
+            call()
