@@ -174,14 +174,18 @@ __device__ __forceinline__ void keep_packed(u32x4 (&x)[C]) {
     for (int i = 0; i < C; ++i) asm volatile("" : "+v"(x[i]));
 }
 
-// C chunks a thread from chunk `first` on, NT apart; what is beyond the row holds -inf.
-template <class E, int NT, int C>
+// C chunks a thread from chunk `first` on, NT apart; what is beyond the row holds -inf.  What is read for the last time goes past the
+// memory-side cache, which is faster (4096 x 131072, bf16: 157 against 180 us); what is read again is left in it, which the second
+// reading gains more from (preference loss of 4096 x 32000, bf16: 107 against 126 us, of 12288 x 32768: 341 against 373; rows of the
+// scan below, policy loss of 2048 x 131072, fp32: 345 against 402).
+enum class Reading { Last, Again };
+template <class E, int NT, Reading HOW = Reading::Last, int C>
 __device__ __forceinline__ void load_chunks(u32x4 (&x)[C], const char* row, const RowSpan& sp, int first) {
     const u32x4* from = reinterpret_cast<const u32x4*>(row + sp.head * E::BYTES);
     static_for<0, C>([&](auto I) {
         constexpr int i = decltype(I)::value;
         x[i] = u32x4{E::NOTHING, E::NOTHING, E::NOTHING, E::NOTHING};
-        if (first + i * NT < sp.chunks) x[i] = __builtin_nontemporal_load(from + first + i * NT);
+        if (first + i * NT < sp.chunks) x[i] = HOW == Reading::Again ? from[first + i * NT] : __builtin_nontemporal_load(from + first + i * NT);
     });
 }
 
@@ -205,12 +209,12 @@ __device__ __forceinline__ MaxSum join_group(const MaxSum a, float k, MaxSum* sh
 }
 
 // A long row, chunk by chunk, four of them under way at a time.
-template <class E, int NT>
+template <class E, int NT, Reading HOW = Reading::Last>
 __device__ __forceinline__ MaxSum scan_chunks(const char* row, const RowSpan& sp, float k) {
     MaxSum a{-INFINITY, 0.f};
     for (int c = threadIdx.x; c < sp.chunks; c += 4 * NT) {
         u32x4 x[4];
-        load_chunks<E, NT>(x, row, sp, c);
+        load_chunks<E, NT, HOW>(x, row, sp, c);
         const float m = max_of<E>(x, a.m), base = m == -INFINITY ? 0.f : m;
         a = MaxSum{m, a.s * __builtin_amdgcn_exp2f((a.m - base) * k) + sum_from<E>(x, -INFINITY, m, k)};
     }
@@ -304,6 +308,7 @@ struct RowArgs {
     float *logp, *logp_low, *lse;  // the last two may be null
     char* dlogits;
     int64_t ld_out, first, rows;   // rows [first, first + rows)
+    bool again;                    // the rows are read again by the gradient's launch
     const float *lse_in, *dlogp;   // of the gradient alone
     MaxSum* parts;                 // of rows that several workgroups share: [rows][sections]
     float* picked;                 // of such rows: the target's logit, which a gradient in place would be written over
@@ -381,7 +386,8 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
     }
     const RowSpan sp = row_span<E, NT>(row, V);
     u32x4 x[C];
-    load_chunks<E, NT>(x, row, sp, tid);
+    if (WORK == RowWork::Logprobs && a.again) load_chunks<E, NT, Reading::Again>(x, row, sp, tid);
+    else load_chunks<E, NT>(x, row, sp, tid);
     float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
     const float ly = E::one(row, y);
     const float m = fold_row<NT>(max_of<E>(x, edge), shared[0], [](float p, float q) { return fmaxf(p, q); });
@@ -438,8 +444,8 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
 }
 
 // Rows too long for that: a workgroup a row, H chunks a thread of its end in registers; for its gradient the rest of the row is read a second
-// time, from its end, which the caches still hold.  (2048 x 131072, fp32: 560 us with nothing in
-// registers, 523 / 467 / 443 with H = 8 / 14 / 20, whose registers no longer all fit.)
+// time, from its end, which the caches still hold.  (2048 x 131072, fp32, before the first reading left the rest in the memory-side
+// cache: 560 us with nothing in registers, 523 / 467 / 443 with H = 8 / 14 / 20, whose registers no longer all fit; now 345.)
 template <class E, int NT, int H, RowWork WORK>
 __global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
     __shared__ MaxSum shared[NT / 64];
@@ -459,7 +465,7 @@ __global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
     const float ly = E::one(row, y), edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
     RowSpan before = sp;
     before.chunks = rest;
-    MaxSum mine = scan_chunks<E, NT>(row, before, k);
+    MaxSum mine = WORK == RowWork::Policy || a.again ? scan_chunks<E, NT, Reading::Again>(row, before, k) : scan_chunks<E, NT>(row, before, k);
     u32x4 x[H > 0 ? H : 1];
     if constexpr (H > 0) {
         load_chunks<E, NT>(x, row, sp, rest + tid);
@@ -502,7 +508,7 @@ __global__ __launch_bounds__(kSectionThreads) void logits_part_kernel(const RowA
     const float k = a.l.k;
     const RowSpan sp = row_span<E, NT>(row, V);
     u32x4 x[C];
-    load_chunks<E, NT>(x, row, sp, section * NT * C + tid);
+    load_chunks<E, NT, Reading::Again>(x, row, sp, section * NT * C + tid);
     const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
     MaxSum mine{max_of<E>(x, edge), 0.f};
     keep_packed(x);
@@ -621,14 +627,15 @@ __device__ __forceinline__ void join_pair_loss(const PairLoss& p) {
     if (threadIdx.x == 0) *p.out = (float)(sum[0] * p.scale);
 }
 
-// The gradient alone, which needs nothing of the rest of its row: NT threads to a section of C chunks each, ROWS rows a workgroup.
+// The gradient alone, which needs nothing of the rest of its row: NT threads to a section of C chunks each, ROWS rows a workgroup.  The
+// last rows come first: the memory-side cache may still hold them.
 template <class E, int NT, int C, int ROWS>
 __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) {
     const int V = (int)a.l.vocab, tid = threadIdx.x % NT, section = (int)(blockIdx.x % (unsigned)a.sections);
     const int64_t in = (int64_t)(blockIdx.x / (unsigned)a.sections) * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
     if (a.loss.out && blockIdx.x == gridDim.x - 1) return join_pair_loss(a.loss);   // (a workgroup more than the rows need)
     if (ROWS > 1 && in >= a.rows) return;
-    const int64_t t = a.first + in, y = a.l.targets[t];
+    const int64_t t = a.first + (a.rows - 1 - in), y = a.l.targets[t];
     const char* row = row_of(a, t, E::BYTES);
     char* out = a.dlogits + t * a.ld_out * E::BYTES;
     const float d = a.dlogp[t];
@@ -828,13 +835,14 @@ size_t logprobs_workspace(int dtype, int64_t tokens, int64_t vocab) {
 }
 size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab) { return policy_space(dtype, tokens, vocab).total; }
 
-hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, void* workspace,
-                           hipStream_t stream) {
+hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, bool again,
+                           void* workspace, hipStream_t stream) {
     RowArgs a{};
     a.l = l;
     a.logp = logp;
     a.logp_low = logp_low;
     a.lse = lse;
+    a.again = again;
     const Sections s = workspace ? sections_of(l.dtype, count, l.vocab, kLogprobsSections) : Sections{0, 0};
     if (s.count > 1) {
         a.first = first;

@@ -34,9 +34,9 @@ size_t logprobs_workspace(int dtype, int64_t tokens, int64_t vocab);
 size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab);
 
 // logp, lse (may be null) of rows [first, first + count).  Without a workspace a row is one workgroup's.
-// `logp_low`, if not null: what rounding the log-probabilities to `logp` left.
-hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, void* workspace,
-                           hipStream_t stream);
+// `logp_low`, if not null: what rounding the log-probabilities to `logp` left.  `again`: the gradient will read the logits once more soon.
+hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, bool again,
+                           void* workspace, hipStream_t stream);
 // The loss of pairs from their terms (one double each).
 struct PairLoss {
     const double* terms;
