@@ -53,6 +53,7 @@ struct Tile {
     static constexpr int E_ALL = (BLOCKS * K + 255) / 256;
     // Registers of one thread that dy passes through, 16 bytes each.
     static constexpr int ELEM = DY == Dy::F32 ? 4 : 2, VEC = 16 / ELEM, LANES = N / VEC, ROWS = THREADS / LANES, PASSES = STEP / ROWS;
+    static constexpr int GROUPS = BLOCKS * 2 * NJ;   // of products, a column of NI results each
 };
 
 // Where chunk c (16 columns, 32 bytes) of token t's row lies: a transposing read takes chunks c and c + 1 of four tokens
@@ -126,18 +127,29 @@ template <class T>
 struct InRegisters {
     u32x4 v[T::PASSES];
 };
+// Where a stage's rows of dy lie.  Whole: all of its tokens are there, and nothing that a thread reads is beyond the last row's end (what is
+// beyond a row's own end makes columns that are not written).
+struct Rows {
+    const char* from;
+    int first, next;
+    bool whole;
+};
 template <class T>
-__device__ __forceinline__ void fetch(InRegisters<T>& r, const GradArgs& a, int64_t t0, int64_t end, int64_t n0) {
+__device__ __forceinline__ Rows rows_at(const GradArgs& a, int64_t t0, int64_t end, int64_t n0) {
     const int n = (int)(threadIdx.x % T::LANES) * T::VEC, row = (int)(threadIdx.x / T::LANES);
     const int64_t all = (a.tokens - 1) * a.ld + a.out;   // elements up to the last one
-    // (what is beyond a row's end makes columns that are not written)
-    if (a.near && t0 + T::STEP <= end && (t0 + T::STEP - 1) * a.ld + n0 + T::N <= all) {
-        const char* from = a.dy + (t0 * a.ld + n0) * T::ELEM;
-        const int first = (row * (int)a.ld + n) * T::ELEM, next = T::ROWS * (int)a.ld * T::ELEM;
-#pragma unroll
-        for (int p = 0; p < T::PASSES; ++p) r.v[p] = *reinterpret_cast<const u32x4_any*>(from + (first + p * next));
-        return;
-    }
+    return Rows{a.dy + (t0 * a.ld + n0) * T::ELEM, (int)((row * a.ld + n) * T::ELEM), (int)(T::ROWS * a.ld * T::ELEM),
+                a.near && t0 + T::STEP <= end && (t0 + T::STEP - 1) * a.ld + n0 + T::N <= all};
+}
+template <class T, int P>
+__device__ __forceinline__ void fetch_pass(InRegisters<T>& r, const Rows& rows) {
+    r.v[P] = *reinterpret_cast<const u32x4_any*>(rows.from + (rows.first + P * rows.next));
+}
+// A stage that is not whole.
+template <class T>
+__device__ __forceinline__ void fetch_part(InRegisters<T>& r, const GradArgs& a, int64_t t0, int64_t end, int64_t n0) {
+    const int n = (int)(threadIdx.x % T::LANES) * T::VEC, row = (int)(threadIdx.x / T::LANES);
+    const int64_t all = (a.tokens - 1) * a.ld + a.out;
     for (int p = 0; p < T::PASSES; ++p) {
         const int64_t t = t0 + p * T::ROWS + row, at = t * a.ld + n0 + n;
         u32x4 v = u32x4{0, 0, 0, 0};
@@ -161,35 +173,45 @@ __device__ __forceinline__ void fetch(InRegisters<T>& r, const GradArgs& a, int6
     }
 }
 
-// The bf16 parts of an fp32 value, highest first, each what the ones before leave cut off (not rounded) to its upper 8 bits; inf
-// and NaN are all in the first.
+// The bf16 parts of four fp32 values, highest first, two in a word: each is what the ones before leave, cut off (not rounded) to its
+// upper 8 bits, so that nothing is lost in three.
 struct Parts {
-    uint32_t part[3];
+    u32x2 part[3];
 };
-__device__ __forceinline__ Parts parts_of(uint32_t bits) {
-    const float v = __uint_as_float(bits), rest = fabsf(v) < INFINITY ? v - __uint_as_float(bits & 0xffff0000u) : 0.f;
-    const uint32_t mid = __float_as_uint(rest) & 0xffff0000u;
-    const float last = rest - __uint_as_float(mid);
-    // (a NaN whose upper half would read as infinity stays a NaN)
-    return Parts{{v != v ? 0x7fc0u : bits >> 16, mid >> 16, __float_as_uint(last) >> 16}};
+__device__ __forceinline__ uint32_t upper_halves(uint32_t low, uint32_t high) { return __builtin_amdgcn_perm(high, low, 0x07060302u); }
+__device__ __forceinline__ Parts parts_of(const u32x4& v) {
+    u32x4 mid, last;
+    float odd = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float x = __uint_as_float(v[i]), rest = x - __uint_as_float(v[i] & 0xffff0000u);
+        mid[i] = __float_as_uint(rest);
+        last[i] = __float_as_uint(rest - __uint_as_float(mid[i] & 0xffff0000u));
+        odd = __builtin_fmaf(x, 0.f, odd);
+    }
+    u32x4 high = v;
+    if (__any(odd != odd)) {   // inf and NaN are all in the first part; a NaN whose upper half would read as infinity stays a NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = __uint_as_float(v[i]);
+            if (!(fabsf(x) < INFINITY)) mid[i] = last[i] = 0u;
+            if (x != x) high[i] = 0x7fc00000u;
+        }
+    }
+    return Parts{{u32x2{upper_halves(high[0], high[1]), upper_halves(high[2], high[3])}, u32x2{upper_halves(mid[0], mid[1]), upper_halves(mid[2], mid[3])},
+                  u32x2{upper_halves(last[0], last[1]), upper_halves(last[2], last[3])}}};
 }
 
-template <class T>
-__device__ __forceinline__ void put(lds_char* lds, const InRegisters<T>& r) {
-    const int n = (int)(threadIdx.x % T::LANES) * T::VEC;
+template <class T, int P>
+__device__ __forceinline__ void put_pass(lds_char* lds, const InRegisters<T>& r) {
+    const int n = (int)(threadIdx.x % T::LANES) * T::VEC, t = P * T::ROWS + (int)(threadIdx.x / T::LANES);
+    lds_char* to = lds + t * T::ROW + dy_chunk<T::N>(t, n >> 4) * 32 + (n & 15) * 2;
+    if constexpr (T::ELEM == 2) {
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(to) = r.v[P];
+    } else {
+        const Parts w = parts_of(r.v[P]);
 #pragma unroll
-    for (int p = 0; p < T::PASSES; ++p) {
-        const int t = p * T::ROWS + (int)(threadIdx.x / T::LANES);
-        lds_char* to = lds + t * T::ROW + dy_chunk<T::N>(t, n >> 4) * 32 + (n & 15) * 2;
-        if constexpr (T::ELEM == 2) {
-            *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(to) = r.v[p];
-        } else {
-            const Parts w[4] = {parts_of(r.v[p][0]), parts_of(r.v[p][1]), parts_of(r.v[p][2]), parts_of(r.v[p][3])};
-#pragma unroll
-            for (int q = 0; q < 3; ++q)
-                *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(to + q * T::PLANE) =
-                    u32x2{w[0].part[q] | (w[1].part[q] << 16), w[2].part[q] | (w[3].part[q] << 16)};
-        }
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(to + q * T::PLANE) = w.part[q];
     }
 }
 
@@ -208,12 +230,13 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t low, uint32_t high, float scal
 
 // One stage's products.  The instruction sums over 16 tokens, 8 in each half of the wave; which 8 is free as long as both operands agree.
 // A lane reads 16 tokens of its column of x at once, tokens 16 o .. 16 o + 15 in half o, and gives the first and then the last
-// 8 of them; dy, whose rows are tokens, is read through the transposing load, 4 tokens of 16 columns a time.
-template <class T>
-__device__ __forceinline__ void multiply(lds_char* lds, f32x16 (&sum)[T::NI][T::NJ], int wn, int wk, int lane) {
+// 8 of them; dy, whose rows are tokens, is read through the transposing load, 4 tokens of 16 columns a time.  `beside(i)` is called with
+// i = 0 .. T::GROUPS - 1 among the products.
+template <class T, class F>
+__device__ __forceinline__ void multiply(lds_char* lds, f32x16 (&sum)[T::NI][T::NJ], int wn, int wk, int lane, F&& beside) {
     const int o = lane >> 5, row = (lane & 15) >> 2, column = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-#pragma unroll
-    for (int b = 0; b < T::BLOCKS; ++b) {
+    static_for<0, T::BLOCKS>([&](auto B) {
+        constexpr int b = decltype(B)::value;
         u32x4 q[T::NJ];
         float scale[T::NJ];
 #pragma unroll
@@ -222,8 +245,8 @@ __device__ __forceinline__ void multiply(lds_char* lds, f32x16 (&sum)[T::NI][T::
             q[j] = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(lds + T::X_AT + k * kActBlock + o * 16);
             scale[j] = __uint_as_float((uint32_t) * reinterpret_cast<const __attribute__((address_space(3))) uint8_t*>(lds + T::E_AT + k) << 23);
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        static_for<0, 2>([&](auto H) {
+            constexpr int h = decltype(H)::value;
             bf16x8 d[T::PLANES][T::NI];
 #pragma unroll
             for (int p = 0; p < T::PLANES; ++p)
@@ -241,16 +264,17 @@ __device__ __forceinline__ void multiply(lds_char* lds, f32x16 (&sum)[T::NI][T::
                     }
                     d[p][i] = r.all;
                 }
-#pragma unroll
-            for (int j = 0; j < T::NJ; ++j) {
+            static_for<0, T::NJ>([&](auto J) {
+                constexpr int j = decltype(J)::value;
                 const bf16x8 x = widen8(q[j][2 * h], q[j][2 * h + 1], scale[j]);
 #pragma unroll
                 for (int p = T::PLANES - 1; p >= 0; --p)   // (the small parts first)
 #pragma unroll
                     for (int i = 0; i < T::NI; ++i) sum[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d[p][i], x, sum[i][j], 0, 0, 0);
-            }
-        }
-    }
+                beside(std::integral_constant<int, (b * 2 + h) * T::NJ + j>{});
+            });
+        });
+    });
 }
 
 // A wave's results.  Lane -> column (lane & 31), rows 8 (e / 4) + 4 (lane >> 5) + e % 4 of each 32 by 32.  What lies outside of
@@ -337,7 +361,7 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES == 8 ? 2 : (T::NI == 1 ? 4 : 2
             auto step = [&](lds_char* now, lds_char* after) {
                 stage_barrier<LOADS>();
                 load(after);
-                multiply<T>(now, sum, wn, wk, lane);
+                multiply<T>(now, sum, wn, wk, lane, [](auto) {});
             };
             for (; steps >= 3; steps -= 3) {
                 step(s0, s2);
@@ -347,19 +371,37 @@ __global__ __launch_bounds__(T::THREADS, T::WAVES == 8 ? 2 : (T::NI == 1 ? 4 : 2
             if (steps > 0) step(s0, s2);
             if (steps > 1) step(s1, s0);
         } else {
-            // Two stages: dy of the next one lies in registers when a stage begins, and is put away first.
+            // Two stages: dy of the next one lies in registers when a stage begins.  A pass of it is put away, and the stage after it
+            // asked for, behind each of the first groups of products: the vector instructions that cut fp32 into parts then run beside the
+            // matrix instructions and not in front of them (16384 x 4096 x 4096, fp32: 1378 -> 1231 us, 1.34 PFLOP/s of bf16 products).
             InRegisters<T> r;
             int64_t t = t0;
-            fetch<T>(r, a, t, end, n0);
+            auto fetch = [&] {
+                const Rows rows = rows_at<T>(a, t, end, n0);
+                if (rows.whole) static_for<0, T::PASSES>([&](auto P) { fetch_pass<T, decltype(P)::value>(r, rows); });
+                else fetch_part<T>(r, a, t, end, n0);
+            };
+            fetch();
             load(s0);
-            put<T>(s0, r);
-            fetch<T>(r, a, t += T::STEP, end, n0);
+            static_for<0, T::PASSES>([&](auto P) { put_pass<T, decltype(P)::value>(s0, r); });
+            t += T::STEP;
+            fetch();
+            constexpr int EACH = (T::PASSES + T::GROUPS - 1) / T::GROUPS;   // passes behind a group
             auto step = [&](lds_char* now, lds_char* next) {
                 stage_barrier<0>();
                 load(next);
-                put<T>(next, r);
-                fetch<T>(r, a, t += T::STEP, end, n0);
-                multiply<T>(now, sum, wn, wk, lane);
+                t += T::STEP;
+                const Rows rows = rows_at<T>(a, t, end, n0);
+                multiply<T>(now, sum, wn, wk, lane, [&](auto I) {
+                    constexpr int from = std::min(decltype(I)::value * EACH, T::PASSES), to = std::min(from + EACH, T::PASSES);
+                    static_for<from, to>([&](auto P) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        put_pass<T, decltype(P)::value>(next, r);
+                        if (rows.whole) fetch_pass<T, decltype(P)::value>(r, rows);
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                });
+                if (!rows.whole) fetch_part<T>(r, a, t, end, n0);
             };
             for (; steps >= 2; steps -= 2) {
                 step(s0, s1);
@@ -406,7 +448,8 @@ hipError_t launch_tile(GradArgs a, Dy dy, hipStream_t stream) {
 // with 1 to 16 parts on 11 shapes of 1 to 32768 tokens, predict the best of them or one within 15 % of it; bf16 rows that do
 // not lie on 16-byte addresses take longer (1.5 to 1.9 times) in much the same proportions.
 // (16384 x 8192 x 8192, tiles of 256 / 128: 1700 / 1992 us; 4096 x 2048 x 4096, 256 / 128 / 64: 82 / 68 / 100 us; 16000 x
-// 1024 x 1024, 128 with 1 / 4 / 8 / 16 parts: 121 / 46 / 42 / 49 us.)
+// 1024 x 1024, 128 with 1 / 4 / 8 / 16 parts: 121 / 46 / 42 / 49 us; dy in fp32, 4096 x 2048 x 4096, 256 with 1 / 2 / 4 parts: 288 / 188 /
+// 213 us, 128: 207 / 225 / 239, 64 with 1: 298; 1000 x 1024 x 1000, 64 with 1 / 2 parts: 23 / 23, 128 with 1 / 2 / 4: 45 / 28 / 25.)
 struct Choice {
     int tile, parts;
 };
@@ -416,8 +459,8 @@ Choice choose(int dy_dtype, int64_t tokens, int64_t out, int64_t width) {
         double alone, full;
     };
     static constexpr Cost bf16[3] = {{256, 1, 1.16, 1.66}, {128, 2, 0.48, 0.47}, {64, 4, 0.54, 0.18}};
-    static constexpr Cost f32[3] = {{256, 1, 4.95, 5.6}, {128, 2, 2.2, 1.7}, {64, 4, 1.63, 0.56}};
-    constexpr double kUnits = 256, kJoin = 3.0, kBytesPerUs = 5e6;
+    static constexpr Cost f32[3] = {{256, 1, 4.5, 4.8}, {128, 2, 2.6, 1.65}, {64, 4, 1.35, 0.57}};
+    constexpr double kUnits = 256, kJoin = 5.0, kBytesPerUs = 5e6;
     const int64_t steps = (tokens + 63) / 64;
     Choice best{64, 1};
     double least = 1e300;
