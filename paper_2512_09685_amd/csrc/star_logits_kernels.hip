@@ -910,7 +910,8 @@ hipError_t launch_policy(const Logits& l, const PolicyArgs& p, float* logp, void
         else both(ElemBf16{});
         return hipGetLastError();
     }
-    const int64_t groups = std::min<int64_t>(kStatsGroups, (l.tokens + 4 * kSumThreads - 1) / (4 * kSumThreads));
+    // (a token a thread while workgroups last: 8192 tokens 14.2 us, 16.1 with four a thread in fewer workgroups; up to 4096 it is the same)
+    const int64_t groups = std::min<int64_t>(kStatsGroups, (l.tokens + kSumThreads - 1) / kSumThreads);
     a.ticket = groups > 1 ? at<unsigned int>(workspace, 0) : nullptr;
     if (l.tokens > 0) a.logp_low = at<float>(workspace, space.logp_low);
     const hipError_t e = in_launches(a, 0, l.tokens, [&](const RowArgs& r) {
