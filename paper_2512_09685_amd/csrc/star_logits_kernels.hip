@@ -360,8 +360,8 @@ __device__ __forceinline__ int64_t die_run(unsigned id) {
 }
 
 // The whole row in registers, C chunks a thread: read once, written once.  NT threads a row, ROWS rows a workgroup.
-// Registers and not LDS, because a unit has three times as much of them; rows of up to 8 chunks a thread let two
-// workgroups of 1024 threads share a unit, of which one reads while the other writes.
+// Registers and not LDS, because a unit has three times as much of them; rows of up to 8192 chunks let two workgroups of
+// 1024 threads share a unit, of which one reads while the other writes, and rows of up to 13312 two of 512.
 // Beside the memory it is the vector instructions that count (an exponential takes four turns of the others), so an
 // exponent is one multiply-add, l k - e with e = round(max l k), a whole number that costs the sum no rounding; and
 // where the registers allow it, fp32 rows and bf16 rows of up to 4 chunks, the exponentials are kept for the gradient
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
     __shared__ float shared[2][NT / 64];
     clear_ticket(a);
     const int V = (int)a.l.vocab, tid = threadIdx.x % NT;
-    const int64_t in = NT == 1024 ? die_run(blockIdx.x) : (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
+    const int64_t in = NT >= 512 ? die_run(blockIdx.x) : (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
     if (ROWS > 1 && in >= a.rows) return;
     const int64_t t = a.first + in, y = a.l.targets[t];
     const char* row = row_of(a, t, E::BYTES);
@@ -769,6 +769,10 @@ void launch_rows_of(const RowArgs& a, hipStream_t stream) {
     if (chunks <= 4096) return logits_held_kernel<E, 1024, 4, 1, WORK><<<rows, 1024, 0, stream>>>(a);
     if (chunks <= 8192) return logits_held_kernel<E, 1024, 8, 1, WORK><<<rows, 1024, 0, stream>>>(a);
     if constexpr (WORK == RowWork::Policy) {
+        // two workgroups of 512 threads a unit, of which one reads while the other writes, against one of 1024: 4096 x 72000, bf16: 211 / 270 us,
+        // 4096 x 100000: 300 / 346; fp32, 1500 x 36000: 85 / 89, 777 x 50021: 63.5 / 66, 2000 x 50257: 152 / 147
+        if (chunks <= 10240) return logits_held_kernel<E, 512, 20, 1, WORK><<<rows, 512, 0, stream>>>(a);
+        if (chunks <= 13312 && (E::VEC == 8 || rows < 1024)) return logits_held_kernel<E, 512, 26, 1, WORK><<<rows, 512, 0, stream>>>(a);
         if (chunks <= 16384) return logits_held_kernel<E, 1024, 16, 1, WORK><<<rows, 1024, 0, stream>>>(a);
         logits_scan_kernel<E, 1024, 18, WORK><<<rows, 1024, 0, stream>>>(a);
     } else {

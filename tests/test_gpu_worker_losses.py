@@ -386,3 +386,34 @@ def test_gradient_and_sums_agree_on_the_clip(T, V, dtype):
     star.star_token_logprobs(x, y, logp)
     star.star_policy_loss(x, y, logp, f32(rng.choice([-1, 1], T)), stats, dlogits=d, clip_low=0.0, clip_high=0.0, scale=1.0)
     assert float(stats[2]) == float((d == 0).all(dim=1).sum())
+
+
+# more rows than are cut into sections, at every size where a row's place changes: 9 001 to 17 501 chunks of 16 bytes
+@pytest.mark.parametrize("V,dtype", [(36001, "f32"), (50021, "f32"), (65536, "f32"), (70001, "f32"), (72003, "bf16"), (100003, "bf16"), (131072, "bf16"),
+                                     (150001, "bf16")])
+def test_policy_loss_of_long_rows(V, dtype):
+    test_policy_loss(129, V, 1, 0.05, 0.28, dtype)
+
+
+def test_infinite_logits_in_long_rows():
+    """Rows of nothing but the lowest value, banned tokens, NaN: where a row is kept in several places all of them see it."""
+    T = 130
+    for V, dtype in ((40001, "f32"), (90001, "bf16"), (131071, "bf16"), (65535, "f32")):
+        low = torch.finfo(TYPES[dtype]).min
+        x = torch.randn(T, V, generator=torch.Generator().manual_seed(V)).to(TYPES[dtype])
+        x[0], x[1], x[2, : V - 20], x[3, 20:] = low, float("-inf"), float("-inf"), low
+        x[4, V - 1], x[5, V // 2] = float("nan"), float("inf")
+        y = np.full(T, V - 10)
+        y[3] = 10
+        y[6:] = -100
+        ref = torch.log_softmax(x[:6].double(), dim=1).numpy()
+        dev, stats, logp, d = x.cuda(), torch.zeros(4, device="cuda"), torch.zeros(T, device="cuda"), torch.full((T, V), 9.0, dtype=TYPES[dtype], device="cuda")
+        star.star_policy_loss(dev, i64(y), f32(np.zeros(T)), f32(np.ones(T)), stats, dlogits=d, logp_out=logp, scale=1.0, clip_high=float("inf"))
+        got = logp.cpu().double().numpy()
+        live = [0, 2, 3]
+        assert np.all(np.abs(got[live] - ref[live, y[live]]) <= wo.U * (V / 64 + 300)) and np.all(np.isnan(got[[1, 4, 5]])) and np.all(got[6:] == 0)
+        r = np.exp(ref[live, y[live]])
+        want = np.exp(ref[live]) * r[:, None]
+        want[np.arange(3), y[live]] -= r
+        close(d[live], want, (1e-4 + wo.HALF_STEP[dtype]) * np.abs(want) + 1e-38, "dlogits")
+        assert bool((d[6:] == 0).all()) and bool(torch.isnan(d[1]).all()) and bool(torch.isnan(d[4]).all())
