@@ -446,7 +446,7 @@ hipError_t launch_tile(GradArgs a, Dy dy, hipStream_t stream) {
 // `full` for each of them; the two differ most for the small tiles, whose steps are latency, and least for the large
 // one, of which a unit holds one.  Joining parts costs a launch and two passes over their sums.  The figures, of launches
 // with 1 to 16 parts on 11 shapes of 1 to 32768 tokens, predict the best of them or one within 15 % of it; bf16 rows that do
-// not lie on 16-byte addresses take longer (1.5 to 1.9 times) in much the same proportions.
+// not lie on 16-byte addresses take longer (1.3 to 1.9 times) in much the same proportions.
 // (16384 x 8192 x 8192, tiles of 256 / 128: 1700 / 1992 us; 4096 x 2048 x 4096, 256 / 128 / 64: 82 / 68 / 100 us; 16000 x
 // 1024 x 1024, 128 with 1 / 4 / 8 / 16 parts: 121 / 46 / 42 / 49 us; dy in fp32, 4096 x 2048 x 4096, 256 with 1 / 2 / 4 parts: 288 / 188 /
 // 213 us, 128: 207 / 225 / 239, 64 with 1: 298; 1000 x 1024 x 1000, 64 with 1 / 2 parts: 23 / 23, 128 with 1 / 2 / 4: 45 / 28 / 25.)
