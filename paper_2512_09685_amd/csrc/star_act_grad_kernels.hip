@@ -289,8 +289,8 @@ __device__ __forceinline__ void write_tile(void* dw, const GradArgs& a, const f3
 #pragma unroll
         for (int j = 0; j < T::NJ; ++j) {
             const int64_t base = (n + x * 32) * a.width + k + j * 32;
-            const __amdgpu_buffer_rsrc_t to = buffer(reinterpret_cast<char*>(dw) + base * BYTES, (int)min((a.out * a.width - base) * BYTES, (int64_t)0x40000000));
-            const int at = k + j * 32 + (lane & 31) < a.width ? ((lane >> 5) * 4 * width + (lane & 31)) * BYTES : 0x40000000;
+            const __amdgpu_buffer_rsrc_t to = buffer(reinterpret_cast<char*>(dw) + base * BYTES, block_range(a.out * a.width, base, BYTES));
+            const int at = k + j * 32 + (lane & 31) < a.width ? ((lane >> 5) * 4 * width + (lane & 31)) * BYTES : kBlockRange;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int where = at + (8 * (e / 4) + e % 4) * width * BYTES;

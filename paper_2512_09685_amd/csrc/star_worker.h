@@ -85,6 +85,15 @@ struct WeightGrad {
     int dw_dtype;
     bool accumulate;
 };
+// What a 32 by 32 block of results, whose first element is `base`, may write of a matrix of `elements`: bytes from there to the end, none for a
+// block that begins behind it (by up to 223 rows, which at the widest do not fit 31 bits), and no more than a block can reach.  What a block must
+// not write lies at kBlockRange or beyond.
+constexpr int kBlockRange = 0x40000000;
+constexpr int block_range(int64_t elements, int64_t base, int bytes) {
+    const int64_t left = elements - base;
+    return left <= 0 ? 0 : (left >= kBlockRange / bytes ? kBlockRange : (int)left * bytes);
+}
+
 // Parts that the tokens are cut into (each part's sums are written apart and joined by a second launch; 1: none).
 int weight_grad_parts(int dy_dtype, int64_t tokens, int64_t out, int64_t width);
 hipError_t launch_weight_grad(const WeightGrad& g, void* workspace, hipStream_t stream);

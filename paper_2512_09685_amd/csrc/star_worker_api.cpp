@@ -16,7 +16,7 @@ constexpr int64_t kMostVocab = (int64_t)1 << 30;
 constexpr int64_t kMostElements = (int64_t)1 << 42;   // of one tensor: no byte offset leaves 63 bits
 constexpr int64_t kMostTiles = (int64_t)1 << 22;      // of dw, 64 by 64 each
 constexpr int64_t kMostSummed = (int64_t)1 << 30;     // tokens that one weight gradient sums over
-constexpr int64_t kMostWidth = (int64_t)1 << 22;      // columns of a weight gradient: 32 rows of it stay within 31 bits of offset
+constexpr int64_t kMostWidth = (int64_t)1 << 22;      // columns of a weight gradient: 32 rows of it stay within kBlockRange
 constexpr int64_t kCacheBytes = (int64_t)1 << 28;     // of the memory-side cache
 
 bool known(int dtype) { return dtype == STAR_F32 || dtype == STAR_BF16; }

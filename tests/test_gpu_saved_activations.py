@@ -246,3 +246,21 @@ def test_in_a_graph_and_on_a_stream():
     star.star_act_weight_grad(dy, packed, dw, stream=side)
     side.synchronize()
     assert torch.equal(dw, want)
+
+
+@pytest.mark.parametrize("N,K,dy_type", [(257, 3_000_000, "f32"), (1025, 2_450_000, "bf16")])
+def test_weight_gradient_of_the_widest_layers(N, K, dy_type):
+    """The last tile's rows lie so far beyond the end of dw that the distance does not fit 31 bits: what lies behind dw stays as it is."""
+    T, behind = 32, 1 << 30
+    g = torch.Generator(device="cuda").manual_seed(N)
+    x = torch.randint(-8, 9, (T, K), generator=g, device="cuda").bfloat16()
+    dy = torch.randint(-4, 5, (T, N), generator=g, device="cuda").to(TYPES[dy_type])
+    packed = torch.zeros(star.star_act_bytes(T, K), dtype=torch.uint8, device="cuda")
+    star.star_act_pack(x, packed)
+    whole = torch.full((N * K + behind,), 7.0, device="cuda")
+    dw = whole[:N * K].view(N, K)
+    star.star_act_weight_grad(dy, packed, dw)
+    for a in range(0, N, 64):
+        assert torch.equal(dw[a:a + 64], dy[:, a:a + 64].float().t().contiguous() @ x.float()), a
+    for a in range(N * K, N * K + behind, 1 << 28):
+        assert bool((whole[a:a + (1 << 28)] == 7.0).all())

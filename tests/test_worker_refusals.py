@@ -222,3 +222,18 @@ def test_binding_refuses_host_memory():
                  lambda: star.star_act_weight_grad(torch.zeros(T, 6), packed, torch.zeros(6, V), stream=0)):
         with pytest.raises(ValueError, match="GPU memory"):
             call()
+
+
+def test_results_stay_inside_the_weight_gradient(tmp_path):
+    """The range that a block of results may write, for tiles that reach beyond the last row of the widest matrices."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = tmp_path / "grad_range_check"
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Wextra", "-fsanitize=undefined", "-fno-sanitize-recover=undefined", "-D__HIP_PLATFORM_AMD__=1",
+                        "-I", os.path.join(root, "include"), "-I", os.path.join(root, "paper_2512_09685_amd", "csrc"),
+                        "-I", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
+                        os.path.join(root, "tests", "grad_range_check.cpp"), "-o", str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0 and "blocks in range" in r.stdout, (r.stdout, r.stderr)
