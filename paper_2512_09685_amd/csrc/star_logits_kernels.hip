@@ -229,8 +229,8 @@ __device__ __forceinline__ u32x4 finish_chunk(float (&v)[E::VEC], float c, int a
     return E::pack(v);
 }
 
-// dl_j = scaled * 2^(l_j k - e), plus `c` at the target: one chunk, one element.  Where a product with k would not hold the row's values
-// (`far`), scaled * 2^((l_j - m) k).
+// dl_j = scaled * 2^(l_j k - e), plus `c` at the target: one chunk, one element.  Where a product with k would not hold the row's
+// values (`far`), scaled * 2^((l_j - m) k).
 struct Slope {
     float k, e, m, scaled, c;
     int y;
@@ -239,10 +239,13 @@ struct Slope {
         return scaled * __builtin_amdgcn_exp2f(far ? (l - m) * k : __builtin_fmaf(l, k, -e));
     }
 };
-__device__ __forceinline__ bool is_far(float m) { return !(fabsf(m) <= 1e30f); }
+// Whether a row's exponents have to be formed from differences with its maximum, `z` the maximum times k: round(z) is off by up to
+// |z| 2^-24 from m k, which up to 2^22 adds nothing to what rounding to a whole number leaves, and from 2^31 on would leave an exponent
+// that fp32 does not hold for the maximum itself.  (True also for infinities and NaN.)
+__device__ __forceinline__ bool is_far(float z) { return !(fabsf(z) <= 0x1p22f); }
 // Of a row whose sum of 2^((l_j - m) k) is s.
 __device__ __forceinline__ Slope slope_of(float k, const MaxSum& all, float c, int64_t y) {
-    const bool far = is_far(all.m);
+    const bool far = is_far(all.m * k);
     const float e = far ? 0.f : rintf(all.m * k), off = far ? 0.f : __builtin_fmaf(all.m, k, -e);
     return Slope{k, e, all.m, -c / all.s * __builtin_amdgcn_exp2f(-off), c, (int)y, far};
 }
@@ -365,8 +368,8 @@ __device__ __forceinline__ int64_t die_run(unsigned id) {
 // Beside the memory it is the vector instructions that count (an exponential takes four turns of the others), so an
 // exponent is one multiply-add, l k - e with e = round(max l k), a whole number that costs the sum no rounding; and
 // where the registers allow it, fp32 rows and bf16 rows of up to 4 chunks, the exponentials are kept for the gradient
-// in the logits' place.  Rows whose maximum is beyond 1e30 (nothing but a type's lowest value, or infinite) are taken relative to
-// it first: no product with k would hold them.
+// in the logits' place.  Rows with a maximum that no product with k would hold (is_far: nothing but a mask's value, say) are taken
+// relative to it first, which loses nothing: differences that count are exact, in bf16 too, where they are then 0.
 template <class E, int NT, int C, int ROWS, RowWork WORK>
 __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(const RowArgs a) {
     constexpr bool KEEP = WORK == RowWork::Policy && (E::VEC == 4 || C <= 4);
@@ -392,7 +395,7 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
     const float ly = E::one(row, y);
     const float m = fold_row<NT>(max_of<E>(x, edge), shared[0], [](float p, float q) { return fmaxf(p, q); });
     keep_packed(x);
-    const bool far = is_far(m);
+    const bool far = is_far(m * k);
     if (far) {
         static_for<0, C>([&](auto I) {
             float v[E::VEC];

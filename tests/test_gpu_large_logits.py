@@ -1,0 +1,96 @@
+"""Rows whose values are large against their differences: a mask's value all over, logits shifted by a constant, temperatures at the ends of
+their range.  Log-probabilities and gradients depend on differences only, and so do the bounds here: they are those of the same rows
+less their maximum (worker_oracle).  Vocabularies and rows take every way through the launches."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_09685_amd as star
+import worker_oracle as wo
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+BASES = [30.0, 1000.0, -1000.0, 1e6, -1e6, 4e6, 1e10, -1e10, 1e30, -1e30, "most", "least"]
+TEMPERATURES = [1e-4, 1e-3, 0.7, 1.0, 1e4]
+# (vocabulary, rows): a wave a row with 1, 2, 4, 8 chunks a lane, workgroups of 256 and 1024, sections (up to 128 rows), then more
+# rows than are cut into sections at every size where a row's place changes
+SHAPES = {"f32": [(37, 12), (500, 12), (1003, 12), (2001, 12), (4001, 12), (8001, 12), (16001, 130), (32001, 130), (40001, 130), (50021, 130), (65001, 130),
+                  (70001, 130), (16001, 12), (70001, 12)],
+          "bf16": [(77, 12), (1003, 12), (2001, 12), (4003, 12), (8003, 12), (16001, 12), (32003, 130), (65001, 130), (80003, 130), (104003, 130), (131003, 130),
+                   (140003, 130), (32003, 12), (140003, 12)]}
+
+
+def large_rows(V, T, dtype, seed=0):
+    """Row t: a third of it BASES[t], a third within 8 of the type's steps below, the rest far below or -inf; rows beyond the bases do not
+    count.  (device tensor, float64 values, targets among the first two thirds)"""
+    rng = np.random.default_rng([seed, V, T])
+    info = torch.finfo(TYPES[dtype])
+    x = torch.zeros(T, V, dtype=TYPES[dtype])
+    y = np.full(T, -100, np.int64)
+    for t, base in enumerate(BASES):
+        top = torch.tensor(info.max if base == "most" else info.min if base == "least" else base, dtype=TYPES[dtype])
+        bits = top.view(torch.int32 if dtype == "f32" else torch.int16)
+        steps = torch.from_numpy(rng.integers(0, 9, V)).to(bits.dtype)
+        kind = rng.random(V)
+        kind[0], kind[V - 1] = 0.0, 0.5                      # (both ends of a row hold what matters)
+        near = (bits + (steps if float(top) < 0 else -steps)).view(TYPES[dtype]) if base != "least" else top.expand(V)
+        low = torch.from_numpy(np.where(rng.random(V) < 0.5, -np.inf, info.min)).to(TYPES[dtype])
+        if base == "least":
+            low = torch.full((V,), float("-inf"), dtype=TYPES[dtype])
+        row = torch.where(torch.from_numpy(kind < 1 / 3), top, torch.where(torch.from_numpy(kind < 2 / 3), near, low))
+        x[t] = row
+        y[t] = rng.choice(np.nonzero(kind < 1 / 3)[0])
+    return x.cuda(), x.double().numpy(), y
+
+
+def expected(x64, y, temperature):
+    """(logp, lse, p, live, bound) from the rows less their maxima; lse with them."""
+    T = float(np.float32(temperature))                       # (the call takes it as such)
+    m = x64.max(axis=1)
+    with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
+        logp, log_s, p, live, bound = wo.rows(x64 - m[:, None], y, T)
+    return logp, log_s + np.where(live, m / T, 0.0), p, live, bound
+
+
+def f32(a):
+    return torch.from_numpy(np.asarray(a, np.float32)).cuda()
+
+
+def close(got, want, bound, what):
+    got = got.double().cpu().numpy()
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.size}, first at {np.argwhere(bad)[0]}: {got[bad][0]} against {want[bad][0]}, bound {np.broadcast_to(bound, got.shape)[bad][0]}"
+
+
+def close_lse(got, want, bound):
+    """One rounding to fp32 (which may run over) more than the bound."""
+    with np.errstate(over="ignore", invalid="ignore"):
+        over = np.abs(want) > float(np.finfo(np.float32).max)
+        got = got.double().cpu().numpy()
+        assert np.array_equal(got[over], np.sign(want[over]) * np.inf)
+        assert np.all(np.abs(got - want)[~over] <= (bound + 4 * wo.U * np.abs(want))[~over])
+
+
+@pytest.mark.parametrize("temperature", TEMPERATURES)
+@pytest.mark.parametrize("dtype,V,T", [(d, *s) for d in SHAPES for s in SHAPES[d]])
+def test_logprobs_and_policy_loss(dtype, V, T, temperature):
+    x, x64, y = large_rows(V, T, dtype)
+    wlogp, wlse, p, live, bound = expected(x64, y, temperature)
+    yd = torch.from_numpy(y).cuda()
+    logp, lse = torch.full((T,), 9.0, device="cuda"), torch.full((T,), 9.0, device="cuda")
+    star.star_token_logprobs(x, yd, logp, lse_out=lse, temperature=temperature)
+    close(logp, wlogp, bound, "logp")
+    close_lse(lse, wlse, bound)
+    # ratio 1, up to the rounding of old_logp; a positive advantage: the slope is -ratio
+    old = wlogp.astype(np.float32)
+    stats, d, out = torch.zeros(4, device="cuda"), torch.full_like(x, 9.0), torch.full((T,), 9.0, device="cuda")
+    star.star_policy_loss(x, yd, f32(old), f32(np.ones(T)), stats, dlogits=d, scale=1.0, temperature=temperature, logp_out=out)
+    close(out, wlogp, bound, "logp of the loss")
+    c = -np.exp(wlogp - old) * live / float(np.float32(temperature))
+    want = wo.dlogits_of(p, y, live, c)
+    close(d, want, wo.gradient_bound(want, p, y, live, c, np.abs(c) * (bound + 16 * wo.U), bound, dtype), "dlogits")
+    close(stats[0:1], np.array([-np.exp(wlogp - old)[live].sum()]), float((bound + 16 * wo.U)[live].sum()) + 4 * wo.U * len(BASES), "loss")
+    alone = torch.zeros(4, device="cuda")
+    star.star_policy_loss(x, yd, f32(old), f32(np.ones(T)), alone, scale=1.0, temperature=temperature)
+    assert torch.allclose(alone, stats, rtol=1e-5, atol=1e-6)
