@@ -76,10 +76,6 @@ __device__ __forceinline__ RowSpan row_span(const char* row, int V) {
     return r;
 }
 
-// Running maximum and sum of 2^((l - m) k).
-struct MaxSum {
-    float m, s;
-};
 __device__ __forceinline__ MaxSum join(const MaxSum a, const MaxSum b, float k) {
     const float m = fmaxf(a.m, b.m);
     // (a side that has seen nothing but -inf adds nothing; two such sides make NaN, as a row of nothing else has to)
@@ -309,10 +305,12 @@ struct RowArgs {
     Logits l;
     PolicyArgs policy;
     float *logp, *logp_low, *lse;  // the last two may be null
+    MaxSum* sums;                  // may be null
     char* dlogits;
     int64_t ld_out, first, rows;   // rows [first, first + rows)
     bool again;                    // the rows are read again by the gradient's launch
-    const float *lse_in, *dlogp;   // of the gradient alone
+    const float *lse_in, *dlogp;   // of the gradient alone, as are
+    const MaxSum* sums_in;         // the rows' maxima and sums; null: lse_in
     MaxSum* parts;                 // of rows that several workgroups share: [rows][sections]
     float* picked;                 // of such rows: the target's logit, which a gradient in place would be written over
     int sections, lanes;           // lanes that join a row's sections: a power of two, no more than a wave's
@@ -335,6 +333,9 @@ __device__ __forceinline__ void put_row(const RowArgs& a, int64_t t, const Two& 
     a.logp[t] = logp.high;
     if (a.logp_low) a.logp_low[t] = logp.low;
     if (a.lse) a.lse[t] = lse;
+}
+__device__ __forceinline__ void put_sum(const RowArgs& a, int64_t t, float m, float s) {
+    if (a.sums) a.sums[t] = MaxSum{m, s};
 }
 
 __device__ __forceinline__ void clear_ticket(const RowArgs& a) {
@@ -419,9 +420,13 @@ __global__ __launch_bounds__(NT* ROWS, C <= 8 ? 8 : 4) void logits_held_kernel(c
     s = fold_row<NT>(s, shared[1], [](float p, float q) { return p + q; });
     // log sum exp(z - max z): the sum is that of 2^(z' - e)
     Two log_s = two_log(s);
-    if (!far) log_s.low -= __builtin_fmaf(m, k, -e) * kLn2;
+    const float off = far ? 0.f : __builtin_fmaf(m, k, -e);
+    log_s.low -= off * kLn2;
     const Two logp = logp_of(a, m, log_s, ly);
-    if (tid == 0) put_row(a, t, logp, lse_of(a, m, log_s));
+    if (tid == 0) {
+        put_row(a, t, logp, lse_of(a, m, log_s));
+        if (WORK == RowWork::Logprobs) put_sum(a, t, m, s * __builtin_amdgcn_exp2f(-off));
+    }
     if constexpr (WORK == RowWork::Policy) {
         const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp).slope * a.l.inv_t, scaled = -c / s;
         if constexpr (!KEEP) keep_packed(x);
@@ -481,7 +486,10 @@ __global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
     }
     const MaxSum all = join_group<NT>(mine, k, shared);
     const Two log_s = two_log(all.s), logp = logp_of(a, all.m, log_s, ly);
-    if (tid == 0) put_row(a, t, logp, lse_of(a, all.m, log_s));
+    if (tid == 0) {
+        put_row(a, t, logp, lse_of(a, all.m, log_s));
+        if (WORK == RowWork::Logprobs) put_sum(a, t, all.m, all.s);
+    }
     if constexpr (WORK == RowWork::Policy) {
         const float c = scaled_weight(a, t) * policy_term(a.policy, t, logp).slope * a.l.inv_t;
         const Slope p = slope_of(k, all, c, y);
@@ -555,8 +563,10 @@ __global__ __launch_bounds__(kSectionThreads) void logits_join_kernel(const RowA
     const bool live = counts(a.l, t, y);
     const MaxSum all = live ? join_parts(a, in, a.l.k) : MaxSum{0.f, 1.f};
     const Two log_s = two_log(all.s);
-    if ((threadIdx.x & (a.lanes - 1)) == 0)
+    if ((threadIdx.x & (a.lanes - 1)) == 0) {
         put_row(a, t, live ? logp_of(a, all.m, log_s, a.picked[in]) : Two{0.f, 0.f}, live ? lse_of(a, all.m, log_s) : 0.f);
+        put_sum(a, t, all.m, all.s);
+    }
 }
 
 // ---------------------------------------------------------------- sums over tokens
@@ -651,11 +661,17 @@ __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) 
     u32x4 x[C];
     load_chunks<E, NT>(x, row, sp, first + tid);
     const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
-    // p_j = 2^(l_j k - lse log2 e): the row's maximum is not known here, nor needed
-    const float c = d * a.l.inv_t, lse = a.lse_in[t];
-    const bool far = is_far(lse);
-    const float e = far ? 0.f : rintf(lse * kLog2e), off = far ? 0.f : __builtin_fmaf(lse, kLog2e, -e) + lse * kLog2eLow;
-    const Slope p{a.l.k, e, lse / a.l.inv_t, -c * __builtin_amdgcn_exp2f(-off), c, (int)y, far};
+    const float c = d * a.l.inv_t;
+    Slope p;
+    if (a.sums_in) {
+        p = slope_of(a.l.k, a.sums_in[t], c, y);
+    } else {
+        // p_j = 2^(l_j k - lse log2 e): the row's maximum is not known here, nor needed
+        const float lse = a.lse_in[t];
+        const bool far = is_far(lse);
+        const float e = far ? 0.f : rintf(lse * kLog2e), off = far ? 0.f : __builtin_fmaf(lse, kLog2e, -e) + lse * kLog2eLow;
+        p = Slope{a.l.k, e, lse / a.l.inv_t, -c * __builtin_amdgcn_exp2f(-off), c, (int)y, far};
+    }
     store_slopes<E, NT>(x, out, sp, p, first + tid);
     if (section == 0 && tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
 }
@@ -842,13 +858,14 @@ size_t logprobs_workspace(int dtype, int64_t tokens, int64_t vocab) {
 }
 size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab) { return policy_space(dtype, tokens, vocab).total; }
 
-hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, bool again,
+hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, MaxSum* sums, bool again,
                            void* workspace, hipStream_t stream) {
     RowArgs a{};
     a.l = l;
     a.logp = logp;
     a.logp_low = logp_low;
     a.lse = lse;
+    a.sums = sums;
     a.again = again;
     const Sections s = workspace ? sections_of(l.dtype, count, l.vocab, kLogprobsSections) : Sections{0, 0};
     if (s.count > 1) {
@@ -874,11 +891,12 @@ hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float*
     });
 }
 
-hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, const float* lse, const float* dlogp, void* dlogits,
-                                int64_t ld_out, const PairLoss& loss, hipStream_t stream) {
+hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, const float* lse, const MaxSum* sums, const float* dlogp,
+                                void* dlogits, int64_t ld_out, const PairLoss& loss, hipStream_t stream) {
     RowArgs a{};
     a.l = l;
     a.lse_in = lse;
+    a.sums_in = sums;
     a.dlogp = dlogp;
     a.dlogits = reinterpret_cast<char*>(dlogits);
     a.ld_out = ld_out;

@@ -33,9 +33,14 @@ struct PolicyArgs {
 size_t logprobs_workspace(int dtype, int64_t tokens, int64_t vocab);
 size_t policy_workspace(int dtype, int64_t tokens, int64_t vocab);
 
+// A row's maximum m and sum of 2^((l_j - m) k).
+struct MaxSum {
+    float m, s;
+};
 // logp, lse (may be null) of rows [first, first + count).  Without a workspace a row is one workgroup's.
-// `logp_low`, if not null: what rounding the log-probabilities to `logp` left.  `again`: the gradient will read the logits once more soon.
-hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, bool again,
+// `logp_low`, if not null: what rounding the log-probabilities to `logp` left.  `sums`, if not null: the rows' maxima and sums, for the gradient.
+// `again`: the gradient will read the logits once more soon.
+hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float* logp, float* logp_low, float* lse, MaxSum* sums, bool again,
                            void* workspace, hipStream_t stream);
 // The loss of pairs from their terms (one double each).
 struct PairLoss {
@@ -44,9 +49,10 @@ struct PairLoss {
     float scale;
     float* out;
 };
-// dlogits of rows [first, first + count) from lse and dlogp; with a loss whose `out` is not null, that too.
-hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, const float* lse, const float* dlogp, void* dlogits,
-                                int64_t ld_out, const PairLoss& loss, hipStream_t stream);
+// dlogits of rows [first, first + count) from dlogp and the rows' maxima and sums or, where there are none, lse; with a loss whose `out` is not
+// null, that too.
+hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, const float* lse, const MaxSum* sums, const float* dlogp,
+                                void* dlogits, int64_t ld_out, const PairLoss& loss, hipStream_t stream);
 // logp (may be null), dlogits (may be null) and the four sums of the policy loss.
 hipError_t launch_policy(const Logits& l, const PolicyArgs& a, float* logp, void* dlogits, int64_t ld_out, float* stats, void* workspace,
                          hipStream_t stream);

@@ -62,16 +62,17 @@ star::Logits make_logits(const void* x, int dtype, int64_t tokens, int64_t vocab
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-// Workspace of the preference loss: terms [pairs] double, then lse, dlogp, logp, logp_low [tokens] float, then that of the log-probabilities.
+// Workspace of the preference loss: terms [pairs] double, then sums [tokens] MaxSum, dlogp, logp, logp_low [tokens] float, then that of the
+// log-probabilities.
 struct PreferenceSpace {
-    size_t terms, lse, dlogp, logp, logp_low, rows, total;
+    size_t terms, sums, dlogp, logp, logp_low, rows, total;
 };
 PreferenceSpace preference_space(int dtype, int64_t tokens, int64_t vocab, int32_t pairs) {
     PreferenceSpace s;
     const size_t each = round16(sizeof(float) * (size_t)tokens);
     s.terms = 0;
-    s.lse = round16(sizeof(double) * (size_t)pairs);
-    s.dlogp = s.lse + each;
+    s.sums = round16(sizeof(double) * (size_t)pairs);
+    s.dlogp = s.sums + round16(sizeof(star::MaxSum) * (size_t)tokens);
     s.logp = s.dlogp + each;
     s.logp_low = s.logp + each;
     s.rows = s.logp_low + each;
@@ -128,7 +129,7 @@ star_status star_token_logprobs(const void* logits, star_dtype dtype, int64_t to
     // A normaliser is asked for where a gradient is to follow: logits that the memory-side cache holds stay in it (1023 x 50021, fp32, both
     // calls: 97 against 102 us).  Larger ones are mostly gone by then.
     const bool again = lse_out && tokens * vocab <= kCacheBytes / (int64_t)bytes_of(dtype);
-    STAR_LAUNCH(star::launch_logprobs(l, 0, tokens, logp_out, nullptr, lse_out, again, workspace, static_cast<hipStream_t>(hip_stream)));
+    STAR_LAUNCH(star::launch_logprobs(l, 0, tokens, logp_out, nullptr, lse_out, nullptr, again, workspace, static_cast<hipStream_t>(hip_stream)));
     return STAR_OK;
 }
 
@@ -140,7 +141,7 @@ star_status star_token_logprobs_grad(const void* logits, star_dtype dtype, int64
     if (tokens == 0) return STAR_OK;
     if (!lse || !dlogp || !dlogits) return set_error(STAR_ERR_NULL, "lse, dlogp or dlogits is NULL");
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, nullptr, temperature);
-    STAR_LAUNCH(star::launch_logprobs_grad(l, 0, tokens, lse, dlogp, dlogits, ld_out, star::PairLoss{}, static_cast<hipStream_t>(hip_stream)));
+    STAR_LAUNCH(star::launch_logprobs_grad(l, 0, tokens, lse, nullptr, dlogp, dlogits, ld_out, star::PairLoss{}, static_cast<hipStream_t>(hip_stream)));
     return STAR_OK;
 }
 
@@ -188,7 +189,8 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
     const star::PreferenceArgs a{ref_logp, params->scale, params->beta, params->label_smoothing};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     double* terms = at<double>(workspace, space.terms);
-    float *lse = at<float>(workspace, space.lse), *dlogp = at<float>(workspace, space.dlogp);
+    star::MaxSum* sums = dlogits ? at<star::MaxSum>(workspace, space.sums) : nullptr;
+    float* dlogp = at<float>(workspace, space.dlogp);
     float *logp = logp_out ? logp_out : at<float>(workspace, space.logp), *logp_low = at<float>(workspace, space.logp_low);
     const star::PairLoss loss{terms, pairs, params->scale, loss_out};
     bool joined = false;
@@ -198,12 +200,12 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
         star::PairOffsets o{};
         for (int i = 0; i <= 2 * n; ++i) o.at[i] = offsets[2 * (int64_t)first + i];
         const int64_t from = o.at[0], count = o.at[2 * n] - from;
-        STAR_LAUNCH(star::launch_logprobs(l, from, count, logp, logp_low, dlogits ? lse : nullptr, dlogits != nullptr,
+        STAR_LAUNCH(star::launch_logprobs(l, from, count, logp, logp_low, nullptr, sums, dlogits != nullptr,
                                           count == tokens ? rows : nullptr, stream));
         STAR_LAUNCH(star::launch_pairs(l, a, o, n, logp, logp_low, dlogits ? dlogp : nullptr, margins_out ? margins_out + first : nullptr, terms + first,
                                        stream));
         const bool last = first + n == pairs && count > 0;   // the loss is joined beside the last gradient
-        if (dlogits) STAR_LAUNCH(star::launch_logprobs_grad(l, from, count, lse, dlogp, dlogits, ld_out, last ? loss : star::PairLoss{}, stream));
+        if (dlogits) STAR_LAUNCH(star::launch_logprobs_grad(l, from, count, nullptr, sums, dlogp, dlogits, ld_out, last ? loss : star::PairLoss{}, stream));
         joined = dlogits && last;
     }
     if (!joined) STAR_LAUNCH(star::launch_pair_loss(loss, stream));

@@ -94,3 +94,28 @@ def test_logprobs_and_policy_loss(dtype, V, T, temperature):
     alone = torch.zeros(4, device="cuda")
     star.star_policy_loss(x, yd, f32(old), f32(np.ones(T)), alone, scale=1.0, temperature=temperature)
     assert torch.allclose(alone, stats, rtol=1e-5, atol=1e-6)
+
+
+@pytest.mark.parametrize("temperature", TEMPERATURES)
+@pytest.mark.parametrize("dtype,V,T", [(d, *s) for d in SHAPES for s in SHAPES[d]])
+def test_preference_loss(dtype, V, T, temperature):
+    x, x64, y = large_rows(V, T, dtype, seed=1)
+    wlogp, _, p, live, bound = expected(x64, y, temperature)
+    rng = np.random.default_rng(V)
+    ref = (wlogp + 0.4 * rng.standard_normal(T)).astype(np.float32)
+    offsets, beta, smooth, scale = np.array([0, 3, 5, 8, T]), 0.3, 0.1, 0.7
+    yd, loss, margins = torch.from_numpy(y).cuda(), torch.zeros(1, device="cuda"), torch.zeros(2, device="cuda")
+    logp, d = torch.full((T,), 9.0, device="cuda"), torch.full_like(x, 9.0)
+    star.star_preference_loss(x, yd, f32(ref), offsets, loss, dlogits=d, scale=scale, beta=beta, label_smoothing=smooth, temperature=temperature,
+                              logp_out=logp, margins_out=margins)
+    close(logp, wlogp, bound, "logp")
+    wl, wm, c = wo.preference(wlogp, ref.astype(np.float64), live, None, offsets, beta, smooth, scale)
+    pair_err = np.array([beta * bound[offsets[2 * b]:offsets[2 * b + 2]].sum() for b in range(2)])
+    close(margins, wm, pair_err + 2 * wo.U * np.abs(wm) + 1e-30, "margins")
+    close(loss, np.array([wl]), scale * pair_err.sum() + 4 * wo.U * abs(wl), "loss")
+    c = c / float(np.float32(temperature))
+    c_err = (scale * beta * pair_err.max() / 4 + scale * beta * smooth * wo.U) / temperature + 10 * wo.U * np.abs(c)
+    want = wo.dlogits_of(p, y, live, c)
+    close(d, want, wo.gradient_bound(want, p, y, live, c, c_err, bound, dtype), "dlogits")
+    star.star_preference_loss(x, yd, f32(ref), offsets, loss, dlogits=x, scale=scale, beta=beta, label_smoothing=smooth, temperature=temperature)
+    assert torch.equal(x, d)                                   # in the logits' place
