@@ -16,7 +16,7 @@ namespace {
 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));   // (see f32x4_any)
 
-constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.925962989e-08f, kLn2 = 0.693147180559945309417f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 // Up to this many rows are cut into sections, if they have at least so many chunks: for the policy loss, which is two launches either
 // way (48 x 32000, bf16: 11.2 against 12.7 us, 1 x 131072 11 against 19), and for log-probabilities, where the second launch
 // has to pay (1 x 131072, fp32: 9.8 against 12.6 us, bf16 9.1 against 9.9; 48 x 32000, fp32: 9.0 against 6.4).
@@ -204,17 +204,23 @@ __device__ __forceinline__ MaxSum join_group(const MaxSum a, float k, MaxSum* sh
     return join_wave<NT / 64>(shared[threadIdx.x % (NT / 64)], k);   // (every wave for itself, one result a lane)
 }
 
-// A long row, chunk by chunk, four of them under way at a time.
+// A long row, chunk by chunk, four of them under way at a time, by NT threads.
 template <class E, int NT, Reading HOW = Reading::Last>
-__device__ __forceinline__ MaxSum scan_chunks(const char* row, const RowSpan& sp, float k) {
+__device__ __forceinline__ MaxSum scan_chunks(const char* row, const RowSpan& sp, float k, int tid) {
     MaxSum a{-INFINITY, 0.f};
-    for (int c = threadIdx.x; c < sp.chunks; c += 4 * NT) {
+    for (int c = tid; c < sp.chunks; c += 4 * NT) {
         u32x4 x[4];
         load_chunks<E, NT, HOW>(x, row, sp, c);
         const float m = max_of<E>(x, a.m), base = m == -INFINITY ? 0.f : m;
         a = MaxSum{m, a.s * __builtin_amdgcn_exp2f((a.m - base) * k) + sum_from<E>(x, -INFINITY, m, k)};
     }
     return a;
+}
+
+// One element more.
+__device__ __forceinline__ MaxSum with_element(const MaxSum& a, float l, float k) {
+    const float m = fmaxf(a.m, l), base = m == -INFINITY ? 0.f : m;
+    return MaxSum{m, a.s * __builtin_amdgcn_exp2f((a.m - base) * k) + __builtin_amdgcn_exp2f((l - base) * k)};
 }
 
 // One chunk of the gradient from its elements but for the target: `c` more at element `at` of it, rounded.
@@ -264,6 +270,15 @@ __device__ __forceinline__ void store_slopes(const u32x4 (&x)[C], char* out, con
         const int at = first + i * NT;
         if (at < sp.chunks) __builtin_nontemporal_store(slope_chunk<E>(x[i], p, sp.head + at * E::VEC), to + at);
     });
+}
+// The gradient of chunks that were scanned, read again from their end.
+template <class E, int NT>
+__device__ __forceinline__ void store_again(const char* row, char* out, const RowSpan& sp, const Slope& p, int tid) {
+    for (int first = (sp.chunks - 1) / (4 * NT) * (4 * NT); first >= 0; first -= 4 * NT) {
+        u32x4 z[4];
+        load_chunks<E, NT>(z, row, sp, first + tid);
+        store_slopes<E, NT>(z, out, sp, p, first + tid);
+    }
 }
 template <class E>
 __device__ __forceinline__ void store_slope(float l, char* out, const RowSpan& sp, const Slope& p, int tid) {
@@ -473,7 +488,7 @@ __global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
     const float ly = E::one(row, y), edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
     RowSpan before = sp;
     before.chunks = rest;
-    MaxSum mine = WORK == RowWork::Policy || a.again ? scan_chunks<E, NT, Reading::Again>(row, before, k) : scan_chunks<E, NT>(row, before, k);
+    MaxSum mine = WORK == RowWork::Policy || a.again ? scan_chunks<E, NT, Reading::Again>(row, before, k, tid) : scan_chunks<E, NT>(row, before, k, tid);
     u32x4 x[H > 0 ? H : 1];
     if constexpr (H > 0) {
         load_chunks<E, NT>(x, row, sp, rest + tid);
@@ -481,8 +496,7 @@ __global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
         keep_packed(x);
         mine = MaxSum{m, mine.s * __builtin_amdgcn_exp2f((mine.m - base) * k) + sum_from<E>(x, edge, m, k)};
     } else {
-        const float m = fmaxf(mine.m, edge), base = m == -INFINITY ? 0.f : m;
-        mine = MaxSum{m, mine.s * __builtin_amdgcn_exp2f((mine.m - base) * k) + __builtin_amdgcn_exp2f((edge - base) * k)};
+        mine = with_element(mine, edge, k);
     }
     const MaxSum all = join_group<NT>(mine, k, shared);
     const Two log_s = two_log(all.s), logp = logp_of(a, all.m, log_s, ly);
@@ -497,11 +511,7 @@ __global__ __launch_bounds__(NT, 4) void logits_scan_kernel(const RowArgs a) {
             keep_packed(x);
             store_slopes<E, NT>(x, out, sp, p, rest + tid);
         }
-        for (int first = (rest - 1) / (4 * NT) * (4 * NT); first >= 0; first -= 4 * NT) {
-            u32x4 z[4];
-            load_chunks<E, NT>(z, row, before, first + tid);
-            store_slopes<E, NT>(z, out, before, p, first + tid);
-        }
+        store_again<E, NT>(row, out, before, p, tid);
         if (tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
     }
 }
@@ -642,8 +652,13 @@ __device__ __forceinline__ void join_pair_loss(const PairLoss& p) {
 
 // The gradient alone, which needs nothing of the rest of its row: NT threads to a section of C chunks each, ROWS rows a workgroup.  The
 // last rows come first: the memory-side cache may still hold them.
+// A normaliser that the caller hands in is one fp32 number, which holds a row's sum the worse the larger it is: rounding it enters every p as |lse|
+// 2^-24.  From kMostLse on the row's sum is formed again, by the threads of its first section, which then take all of the row: no other ones read
+// it, so that it may be written in place.
+constexpr float kMostLse = 64.f;
 template <class E, int NT, int C, int ROWS>
 __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) {
+    __shared__ MaxSum shared[NT / 64];
     const int V = (int)a.l.vocab, tid = threadIdx.x % NT, section = (int)(blockIdx.x % (unsigned)a.sections);
     const int64_t in = (int64_t)(blockIdx.x / (unsigned)a.sections) * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
     if (a.loss.out && blockIdx.x == gridDim.x - 1) return join_pair_loss(a.loss);   // (a workgroup more than the rows need)
@@ -651,26 +666,35 @@ __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) 
     const int64_t t = a.first + (a.rows - 1 - in), y = a.l.targets[t];
     const char* row = row_of(a, t, E::BYTES);
     char* out = a.dlogits + t * a.ld_out * E::BYTES;
-    const float d = a.dlogp[t];
+    const float d = a.dlogp[t], lse = a.sums_in ? 0.f : a.lse_in[t], k = a.l.k;
+    const MaxSum sum = a.sums_in ? a.sums_in[t] : MaxSum{0.f, 1.f};
     const int first = section * NT * C;
     if (!counts(a.l, t, y) || d == 0.f) {
         zero_row<E, NT>(out, V, tid, first, section + 1 == a.sections ? 0x7fffffff : first + NT * C);
         return;
     }
     const RowSpan sp = row_span<E, NT>(row, V);
+    const float c = d * a.l.inv_t;
+    if (!(fabsf(lse) <= kMostLse)) {
+        if (section > 0) return;
+        const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
+        const MaxSum all = join_group<NT>(with_element(scan_chunks<E, NT, Reading::Again>(row, sp, k, tid), edge, k), k, shared);
+        const Slope p = slope_of(k, all, c, y);
+        store_again<E, NT>(row, out, sp, p, tid);
+        if (tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);
+        return;
+    }
     u32x4 x[C];
     load_chunks<E, NT>(x, row, sp, first + tid);
     const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
-    const float c = d * a.l.inv_t;
     Slope p;
     if (a.sums_in) {
-        p = slope_of(a.l.k, a.sums_in[t], c, y);
+        p = slope_of(k, sum, c, y);
     } else {
-        // p_j = 2^(l_j k - lse log2 e): the row's maximum is not known here, nor needed
-        const float lse = a.lse_in[t];
-        const bool far = is_far(lse);
-        const float e = far ? 0.f : rintf(lse * kLog2e), off = far ? 0.f : __builtin_fmaf(lse, kLog2e, -e) + lse * kLog2eLow;
-        p = Slope{a.l.k, e, lse / a.l.inv_t, -c * __builtin_amdgcn_exp2f(-off), c, (int)y, far};
+        // p_j = 2^((l_j - m) k - rest log2 e) with an m near lse times the temperature, and what lse is more than m / temperature: only differences
+        // are multiplied with the rounded k
+        const float m = lse / a.l.inv_t, rest = __builtin_fmaf(-m, a.l.inv_t, lse) - m * a.l.inv_t_low, e = rintf(m * k);
+        p = Slope{k, e, m, -c * __builtin_amdgcn_exp2f(-(__builtin_fmaf(m, k, -e) + rest * kLog2e)), c, (int)y, false};
     }
     store_slopes<E, NT>(x, out, sp, p, first + tid);
     if (section == 0 && tid < sp.edge) store_slope<E>(edge, out, sp, p, tid);

@@ -119,3 +119,46 @@ def test_preference_loss(dtype, V, T, temperature):
     close(d, want, wo.gradient_bound(want, p, y, live, c, c_err, bound, dtype), "dlogits")
     star.star_preference_loss(x, yd, f32(ref), offsets, loss, dlogits=x, scale=scale, beta=beta, label_smoothing=smooth, temperature=temperature)
     assert torch.equal(x, d)                                   # in the logits' place
+
+
+def check_gradient(x, x64, y, temperature, dtype):
+    """star_token_logprobs_grad from star_token_logprobs' normaliser, into other memory and in place."""
+    T = len(y)
+    wlogp, wlse, p, live, bound = expected(x64, y, temperature)
+    yd, logp, lse = torch.from_numpy(y).cuda(), torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda")
+    star.star_token_logprobs(x, yd, logp, lse_out=lse, temperature=temperature)
+    close(logp, wlogp, bound, "logp")
+    close_lse(lse, wlse, bound)
+    dlogp = np.random.default_rng(T).standard_normal(T).astype(np.float32)
+    d = torch.full_like(x, 9.0)
+    star.star_token_logprobs_grad(x, yd, lse, f32(dlogp), d, temperature=temperature)
+    c = dlogp.astype(np.float64) * live / float(np.float32(temperature))
+    want = wo.dlogits_of(p, y, live, c)
+    # up to 64 the normaliser is taken as it was rounded; beyond, the row's own sum is
+    rounded = np.where(np.abs(wlse) <= 64.001, wo.U * np.abs(wlse), 0.0)
+    close(d, want, wo.gradient_bound(want, p, y, live, c, 4 * wo.U * c, bound + rounded, dtype), "dlogits")
+    star.star_token_logprobs_grad(x, yd, lse, f32(dlogp), x, temperature=temperature)
+    assert torch.equal(x, d)
+
+
+@pytest.mark.parametrize("temperature", TEMPERATURES)
+@pytest.mark.parametrize("dtype,V,T", [(d, *s) for d in SHAPES for s in SHAPES[d]])
+def test_gradient_of_logprobs(dtype, V, T, temperature):
+    x, x64, y = large_rows(V, T, dtype, seed=2)
+    check_gradient(x, x64, y, temperature, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temperature", [0.05, 1.0])
+@pytest.mark.parametrize("T,V,pad", [(9, 77, 3), (9, 1003, 0), (9, 4001, 5), (9, 33003, 1), (9, 131075, 0), (600, 8003, 0)])
+def test_gradient_of_shifted_logits(T, V, pad, temperature, dtype):
+    """Ordinary rows, a constant added: in a launch that holds rows on both sides of 64."""
+    rng = np.random.default_rng([T, V])
+    shift = np.resize([0.0, 10.0, 30.0, 50.0, -50.0, 200.0, -1000.0, 1000.0, 3000.0], T)
+    host = torch.from_numpy((rng.standard_normal((T, V + pad)) * 2 * min(1.0, 4 * temperature) + shift[:, None]).astype(np.float32)).to(TYPES[dtype])
+    x = host.cuda()[:, :V]
+    y = rng.integers(0, V, T)
+    y[:2] = 0, V - 1
+    if T > 20:
+        y[rng.random(T) < 0.3] = -1
+    check_gradient(x, host[:, :V].double().numpy(), y.astype(np.int64), temperature, dtype)
