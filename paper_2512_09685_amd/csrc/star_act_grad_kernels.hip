@@ -105,7 +105,9 @@ template <class T, Dy DY>
 __device__ __forceinline__ void load_stage(lds_char* lds, const GradArgs& a, const Sources<T, DY>& s, Cursor& c, int64_t n0, int64_t k0, int wave) {
     if constexpr (DY == Dy::Direct) {
         const int left = min(c.tokens, T::STEP) * (int)a.ld - (int)(a.ld - a.out + n0);   // elements
-        const __amdgpu_buffer_rsrc_t dy = buffer(c.dy, left * 2);
+        // (to the end of the last element's 4-byte word: a word that lies only half in range comes as 0 all of it.  Its other half, of an odd `out`,
+        // makes a column that is not written)
+        const __amdgpu_buffer_rsrc_t dy = buffer(c.dy, (left * 2 + 3) & ~3);
 #pragma unroll
         for (int i = 0; i < T::DY_LOADS; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(dy, lds + (i * T::WAVES + wave) * 1024, 16, s.dy[i], 0, 0, 0);

@@ -264,3 +264,20 @@ def test_weight_gradient_of_the_widest_layers(N, K, dy_type):
         assert torch.equal(dw[a:a + 64], dy[:, a:a + 64].float().t().contiguous() @ x.float()), a
     for a in range(N * K, N * K + behind, 1 << 28):
         assert bool((whole[a:a + (1 << 28)] == 7.0).all())
+
+
+@pytest.mark.parametrize("T,N,ld", [(1, 1, 8), (1, 7, 8), (65, 17, 24), (64, 101, 104), (33, 127, 128), (32, 129, 136), (250, 1001, 1008), (250, 1002, 1008),
+                                    (251, 1003, 1008), (64, 1005, 1008), (64, 1007, 1008), (40, 513, 520), (64, 2051, 2056)])
+def test_weight_gradient_of_an_odd_number_of_columns(T, N, ld):
+    """bf16 rows on 16-byte addresses that end inside of 16 bytes and inside of 4: the last token's last columns, with NaN behind them."""
+    K = 80
+    dy, x = exact_case(T, N, K, "bf16", seed=12)
+    dy[T - 1] = 3.0
+    dy[T - 1, N - 1] = -2.0
+    x[T - 1] = 1.0
+    buffer = torch.full((T * ld,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    dev = buffer.view(T, ld)[:, :N]
+    dev.copy_(dy.cuda())
+    dw = torch.full((N, K), 7.0, device="cuda")
+    star.star_act_weight_grad(dev, pack(x.cuda()), dw)
+    assert np.array_equal(dw.double().cpu().numpy(), dy.double().t().numpy() @ x.double().numpy())
