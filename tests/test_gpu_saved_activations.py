@@ -281,3 +281,25 @@ def test_weight_gradient_of_an_odd_number_of_columns(T, N, ld):
     dw = torch.full((N, K), 7.0, device="cuda")
     star.star_act_weight_grad(dev, pack(x.cuda()), dw)
     assert np.array_equal(dw.double().cpu().numpy(), dy.double().t().numpy() @ x.double().numpy())
+
+
+def test_long_packed_form():
+    """A packed form of more than 2^32 bytes, whose last block is all that reaches the gradient and what is brought back."""
+    T, N, K = 2 ** 20 + 40, 24, 4096
+    x = torch.empty(T, K, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for a in range(0, T, 2 ** 17):
+        x[a:a + 2 ** 17] = torch.randint(-8, 9, (min(2 ** 17, T - a), K), generator=g, device="cuda")
+    packed = torch.full((star.star_act_bytes(T, K) + 32,), 0xAB, dtype=torch.uint8, device="cuda")
+    assert packed.numel() > 2 ** 32
+    star.star_act_pack(x, packed)
+    assert bool((packed[-32:] == 0xAB).all())
+    dy = torch.zeros(T, N, dtype=torch.bfloat16, device="cuda")
+    dy[-39:] = torch.randint(-4, 5, (39, N), generator=g, device="cuda").bfloat16()
+    dw = torch.zeros(N, K, device="cuda")
+    star.star_act_weight_grad(dy, packed, dw)
+    assert torch.equal(dw, dy[-39:].float().t().contiguous() @ x[-39:].float())
+    out = torch.zeros_like(x)
+    star.star_act_unpack(packed, out)
+    for a in range(0, T, 2 ** 17):
+        assert torch.equal(out[a:a + 2 ** 17], x[a:a + 2 ** 17]), a
