@@ -745,11 +745,11 @@ __global__ __launch_bounds__(kBlock) void pair_kernel(const Logits l, const Pref
     if (threadIdx.x == 0) all = a.beta * sum[0];
     __syncthreads();
     const double s = all;
-    // -log sigmoid(s) = max(-s, 0) + log(1 + e^-|s|)
-    const double tail = log1p(exp(-fabs(s)));
+    // -log sigmoid(s) = max(-s, 0) + log(1 + e^-|s|); the two shares are 1 together, and one of 0 costs nothing, also of an infinite margin
+    const double tail = log1p(exp(-fabs(s))), share = s >= 0.0 ? (double)a.smooth : 1.0 - (double)a.smooth;
     if (threadIdx.x == 0) {
         if (margins) margins[b] = (float)s;
-        terms[b] = (1.0 - a.smooth) * (fmax(-s, 0.0) + tail) + a.smooth * (fmax(s, 0.0) + tail);
+        terms[b] = tail + (share != 0.0 ? share * fabs(s) : 0.0);
     }
     const double sig = s >= 0 ? 1.0 / (1.0 + exp(-s)) : exp(s) / (1.0 + exp(s));
     // dl/ds = sigmoid(s) - (1 - smooth); for large s that is smooth - sigmoid(-s), without the cancellation

@@ -417,3 +417,17 @@ def test_infinite_logits_in_long_rows():
         want[np.arange(3), y[live]] -= r
         close(d[live], want, (1e-4 + wo.HALF_STEP[dtype]) * np.abs(want) + 1e-38, "dlogits")
         assert bool((d[6:] == 0).all()) and bool(torch.isnan(d[1]).all()) and bool(torch.isnan(d[4]).all())
+
+
+@pytest.mark.parametrize("smooth,banned,want", [(0.0, "other", 0.0), (1.0, "preferred", 0.0), (0.0, "preferred", float("inf")), (0.1, "other", float("inf"))])
+def test_margins_without_bounds(smooth, banned, want):
+    """An answer whose policy excludes one of its tokens: the margin is infinite, and costs nothing on the side whose share is 0."""
+    V = 40
+    x = torch.zeros(4, V, device="cuda")
+    x[2 if banned == "other" else 0, 5] = float("-inf")
+    y, ref = i64([5, 5, 5, 5]), f32([-3.7, -3.7, -3.7, -3.7])
+    loss, margins, d = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda"), torch.full((4, V), 9.0, device="cuda")
+    star.star_preference_loss(x, y, ref, [0, 2, 4], loss, dlogits=d, scale=1.0, label_smoothing=smooth, margins_out=margins)
+    assert float(margins[0]) == (float("inf") if banned == "other" else float("-inf"))
+    assert float(loss[0]) == want
+    assert bool(torch.isfinite(d).all()) and (want != 0.0 or bool((d == 0).all()))
