@@ -127,8 +127,9 @@ struct PolicyTerm {
 __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& a, int64_t t, const Two& logp) {
     const float A = a.advantages[t], r = expf((logp.high - a.old_logp[t]) + logp.low);
     const float held = fminf(fmaxf(r, a.low), a.high);
-    // (an advantage of 0 costs nothing, also where the ratio has run over)
-    const float free_cost = A == 0.f ? 0.f : -A * r, held_cost = A == 0.f ? 0.f : -A * held;
+    // (an advantage of 0 costs nothing, also where the ratio has run over; where there is no ratio there is no cost to tell)
+    const bool none = A == 0.f && r == r;
+    const float free_cost = none ? 0.f : -A * r, held_cost = none ? 0.f : -A * held;
     PolicyTerm p;
     p.clipped = free_cost < held_cost ? 1.f : 0.f;
     p.loss = free_cost < held_cost ? held_cost : free_cost;

@@ -431,3 +431,23 @@ def test_margins_without_bounds(smooth, banned, want):
     assert float(margins[0]) == (float("inf") if banned == "other" else float("-inf"))
     assert float(loss[0]) == want
     assert bool(torch.isfinite(d).all()) and (want != 0.0 or bool((d == 0).all()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(3, 100), (3, 70003), (130, 40001)])
+def test_an_advantage_of_zero_hides_no_nan(T, V, dtype):
+    """A row without a log-probability has no loss either, and no gradient, whatever its advantage."""
+    x = torch.randn(T, V, generator=torch.Generator().manual_seed(V)).to(TYPES[dtype])
+    x[1, V // 2] = float("nan")
+    y = np.full(T, 5)
+    y[3:] = -100
+    dev, old = x.cuda(), f32(np.full(T, -10.0))
+    stats, d = torch.zeros(4, device="cuda"), torch.full_like(dev, 9.0)
+    star.star_policy_loss(dev, i64(y), old, f32(np.zeros(T)), stats, dlogits=d)
+    assert bool(torch.isnan(stats[0])) and bool(torch.isnan(d[1]).all())
+    assert bool((d[0] == 0).all()) and bool((d[2:] == 0).all())
+    star.star_policy_loss(dev, i64(y), old, f32(np.zeros(T)), stats)
+    assert bool(torch.isnan(stats[0]))
+    # and nothing of it where the token does not count
+    star.star_policy_loss(dev, i64(y), old, f32(np.zeros(T)), stats, dlogits=d, weights=f32(np.arange(T) != 1))
+    assert float(stats[0]) == 0.0 and bool((d == 0).all())
