@@ -120,6 +120,13 @@ __device__ __forceinline__ Two add(const Two& a, const Two& b, float sign) {
     return normal(s.high, s.low + (a.low + sign * b.low));
 }
 
+// e^d - d - 1, `q` = e^d - 1: of small d from its series, where q - d would leave few digits and, of policies close to each other, the wrong sign.
+__device__ __forceinline__ float kl_of(float d, float q) {
+    if (!(fabsf(d) < 0.25f)) return q - d;
+    const float more = __builtin_fmaf(d, __builtin_fmaf(d, __builtin_fmaf(d, __builtin_fmaf(d, 1.f / 5040.f, 1.f / 720.f), 1.f / 120.f), 1.f / 24.f), 1.f / 6.f);
+    return d * d * __builtin_fmaf(d, more, 0.5f);
+}
+
 // One token's loss, KL estimate, whether it is clipped, and its derivative by logp (unweighted).
 struct PolicyTerm {
     float loss, kl, clipped, slope;
@@ -137,7 +144,7 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& a, int64_t t
     p.kl = 0.f;
     if (a.kl != 0.f) {
         const float d = (a.ref_logp[t] - logp.high) - logp.low, q = expm1f(d);
-        p.kl = q - d;
+        p.kl = kl_of(d, q);
         p.loss += a.kl * p.kl;
         p.slope -= a.kl * q;
     }
