@@ -162,3 +162,60 @@ def test_gradient_of_shifted_logits(T, V, pad, temperature, dtype):
     if T > 20:
         y[rng.random(T) < 0.3] = -1
     check_gradient(x, host[:, :V].double().numpy(), y.astype(np.int64), temperature, dtype)
+
+
+@pytest.mark.parametrize("dtype,V,T", [(d, *s) for d in SHAPES for s in SHAPES[d]])
+def test_rows_without_a_log_probability(dtype, V, T):
+    """Rows that hold NaN or +inf, or nothing but -inf, have a gradient of NaN; their neighbours, and pairs, none of it."""
+    x = torch.randn(T, V, generator=torch.Generator().manual_seed(V)).to(TYPES[dtype])
+    x[1, V // 2], x[2, V - 1], x[3], x[5, V // 2] = float("nan"), float("inf"), float("-inf"), float("nan")
+    y = np.full(T, -100)
+    y[:5] = [0, 1, 2, 3, V - 1]                                # (row 5 does not count)
+    dev, yd = x.cuda(), torch.from_numpy(y).cuda()
+    logp, lse, d = torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda"), torch.full_like(dev, 9.0)
+    star.star_token_logprobs(dev, yd, logp, lse_out=lse)
+    assert torch.isnan(logp[:5]).tolist() == [False, True, True, True, False] and bool((logp[5:] == 0).all())
+    star.star_token_logprobs_grad(dev, yd, lse, torch.ones(T, device="cuda"), d)
+    assert torch.isnan(d).all(dim=1)[:5].tolist() == [False, True, True, True, False]
+    assert bool(torch.isfinite(d[[0, 4]]).all()) and bool((d[5:] == 0).all())
+    want = -torch.softmax(x[[0, 4]].double(), dim=1)
+    want[[0, 1], [0, V - 1]] += 1.0
+    p = np.abs(want.numpy())
+    close(d[[0, 4]], want.numpy(), 1e-4 * p + wo.HALF_STEP[dtype] * p + 1e-6 * (p > 0.5) + 1e-38, "dlogits")
+    margins, loss = torch.zeros(2, device="cuda"), torch.zeros(1, device="cuda")
+    star.star_preference_loss(dev, yd, torch.zeros(T, device="cuda"), [0, 2, 4, 5, T], loss, dlogits=d, margins_out=margins)
+    assert torch.isnan(margins).tolist() == [True, False] and bool(torch.isnan(loss[0]))
+    assert bool(torch.isnan(d[:4]).all()) and bool(torch.isfinite(d[4]).all()) and bool((d[5:] == 0).all())
+
+
+def test_more_rows_than_one_launch_holds():
+    """2^21 rows and more go into several launches: all entry points, against torch in 64 bits on the device."""
+    T, V = 2 ** 21 + 77, 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(T, V, generator=g, device="cuda")
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    y[::7] = -1
+    live, at = y >= 0, torch.arange(T, device="cuda")
+    p = torch.softmax(x.double(), dim=1)
+    want = torch.where(live, torch.log_softmax(x.double(), dim=1)[at, y.clamp(min=0)], 0.0)
+    onehot = torch.zeros(T, V, dtype=torch.float64, device="cuda")
+    onehot[at, y.clamp(min=0)] = 1.0
+    slope = torch.where(live[:, None], onehot - p, 0.0)
+    logp, lse, d = torch.full((T,), 9.0, device="cuda"), torch.zeros(T, device="cuda"), torch.full_like(x, 9.0)
+    star.star_token_logprobs(x, y, logp, lse_out=lse)
+    assert float((logp - want).abs().max()) < 64 * wo.U
+    star.star_token_logprobs_grad(x, y, lse, torch.ones(T, device="cuda"), d)
+    assert float((d - slope).abs().max()) < 64 * wo.U
+    adv, stats, again = torch.randn(T, generator=g, device="cuda"), torch.zeros(4, device="cuda"), torch.full((T,), 9.0, device="cuda")
+    star.star_policy_loss(x, y, logp, adv, stats, dlogits=d, logp_out=again, scale=1.0)
+    assert torch.equal(logp, again)
+    # (ratios of 1, up to the rounding of log-probabilities below 16 in size)
+    assert float((d + adv[:, None].double() * slope).abs().max()) < 6 * 96 * wo.U
+    assert float(stats[0]) == pytest.approx(float(-adv.double()[live].sum()), abs=64 * wo.U * float(adv.abs().sum())) and float(stats[3]) == float(live.sum())
+    loss, margins, half = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda"), T // 2
+    star.star_preference_loss(x, y, torch.zeros(T, device="cuda"), [0, half, T], loss, dlogits=d, beta=1e-3, scale=1.0, margins_out=margins)
+    m = 1e-3 * (want[:half].sum() - want[half:].sum())
+    assert float(margins[0]) == pytest.approx(float(m), abs=1e-3 * 64 * wo.U * T)
+    c = -1e-3 / (1 + torch.exp(margins[0].double()))
+    sign = torch.where(at < half, 1.0, -1.0)[:, None]
+    assert float((d - c * sign * slope).abs().max()) < 1e-3 * 64 * wo.U

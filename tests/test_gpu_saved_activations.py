@@ -303,3 +303,40 @@ def test_long_packed_form():
     star.star_act_unpack(packed, out)
     for a in range(0, T, 2 ** 17):
         assert torch.equal(out[a:a + 2 ** 17], x[a:a + 2 ** 17]), a
+
+
+# The tiles that only large or thin outputs take: 64 for bf16 (one thin side, whole and in parts), 128 for fp32, 256 for both (whole and in parts);
+# ld: rows of dy on 16-byte addresses, or not
+@pytest.mark.parametrize("T,N,K,ld,dy_type", [
+    (70, 40, 70001, 40, "bf16"), (70, 39, 70001, 39, "bf16"), (70, 39, 70001, 40, "bf16"), (65, 70001, 40, 70008, "bf16"), (5000, 40, 30001, 40, "bf16"),
+    (5000, 33, 30001, 35, "bf16"), (70, 4090, 4001, 4096, "bf16"), (70, 4089, 4001, 4096, "bf16"), (129, 4090, 4001, 4090, "bf16"),
+    (20000, 4090, 2001, 4096, "bf16"), (20001, 4090, 2001, 4091, "bf16"), (70, 2100, 4001, 2100, "f32"), (3000, 2100, 2000, 2101, "f32"),
+    (60, 4090, 4001, 4090, "f32"), (70, 4090, 4001, 4091, "f32"), (20000, 4090, 2001, 4090, "f32")])
+@pytest.mark.parametrize("dw_type", ["f32", "bf16"])
+def test_weight_gradient_in_every_tile(T, N, K, ld, dy_type, dw_type):
+    dy, x = exact_case(T, N, K, dy_type, seed=13)
+    dy[T - 1] = 3.0
+    buffer = torch.full((T, ld), float("nan"), dtype=TYPES[dy_type], device="cuda")
+    dev, x = buffer[:, :N], x.cuda()
+    dev.copy_(dy.cuda())
+    packed = pack(x)
+    want = dev.float().t().contiguous() @ x                            # (sums that fp32 holds exactly, in any order)
+    dw = torch.full((N * K + 8,), 7.0, dtype=TYPES[dw_type], device="cuda")
+    row = dw[3:3 + N * K].view(N, K)
+    star.star_act_weight_grad(dev, packed, row)
+    assert torch.equal(row, want.to(TYPES[dw_type]))
+    before = (-(want / 2)).to(TYPES[dw_type])
+    row.copy_(before)
+    star.star_act_weight_grad(dev, packed, row, accumulate=True)
+    assert torch.equal(row, (before.float() + want).to(TYPES[dw_type]))
+    assert bool((dw[:3] == 7.0).all()) and bool((dw[3 + N * K:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_kept_values_of_a_large_matrix(dtype):
+    """More blocks of columns than are packed one to a workgroup; rows apart by an odd distance."""
+    T, K = 1001, 6007
+    x, x32 = activations(T, K, dtype, seed=14, pad=4, shift=1)
+    out = torch.zeros(T, K, device="cuda")
+    star.star_act_unpack(pack(x), out)
+    assert np.array_equal(out.double().cpu().numpy(), wo.kept(x32)[0])
