@@ -467,3 +467,11 @@ def test_kl_of_policies_close_to_each_other():
         kl = float(stats[1])
         assert kl >= 0.0 and abs(kl - want) <= 40 * wo.U * want, (d, kl, want)
         assert float(stats[0]) == kl
+
+
+# up to 128 long rows, in sections of 256 times 2, 4 and 8 chunks
+@pytest.mark.parametrize("T,V,dtype", [(20, 70003, "f32"), (40, 70003, "f32"), (128, 66001, "f32"), (20, 140003, "bf16"), (33, 140003, "bf16"), (127, 131075, "bf16"),
+                                       (128, 16389, "bf16")])
+def test_losses_of_rows_in_sections(T, V, dtype):
+    test_policy_loss(T, V, 1, 0.05, 0.28, dtype)
+    test_logprobs_and_gradient(T, V, 3, dtype)
