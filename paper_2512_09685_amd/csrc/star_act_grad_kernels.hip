@@ -26,7 +26,7 @@ struct GradArgs {
     const uint8_t *kept, *exponents;
     void* dw;
     float* partial;      // sums of this launch's parts, [parts][out][width]; null: one part, straight to dw
-    int64_t tokens, out, ld, width, columns, blocks;
+    int64_t tokens, out, ld, width, columns;
     int tiles_n, tiles_k, parts;
     int dw_bf16, accumulate, near;   // near: a stage's offsets into dy fit 31 bits
 };
@@ -486,9 +486,8 @@ hipError_t launch_choice(const WeightGrad& g, const Choice& c, void* workspace, 
     GradArgs a{};
     a.dy = reinterpret_cast<const char*>(g.dy);
     a.columns = act_columns(g.width);
-    a.blocks = act_blocks(g.tokens);
     a.kept = reinterpret_cast<const uint8_t*>(g.packed);
-    a.exponents = a.kept + a.blocks * a.columns * kActBlock;
+    a.exponents = a.kept + act_blocks(g.tokens) * a.columns * kActBlock;
     a.dw = g.dw;
     a.tokens = g.tokens;
     a.out = g.out;

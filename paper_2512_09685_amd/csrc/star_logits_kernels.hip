@@ -76,13 +76,6 @@ __device__ __forceinline__ RowSpan row_span(const char* row, int V) {
     return r;
 }
 
-__device__ __forceinline__ MaxSum join(const MaxSum a, const MaxSum b, float k) {
-    const float m = fmaxf(a.m, b.m);
-    // (a side that has seen nothing but -inf adds nothing; two such sides make NaN, as a row of nothing else has to)
-    const float fa = __builtin_amdgcn_exp2f((a.m - m) * k), fb = __builtin_amdgcn_exp2f((b.m - m) * k);
-    return MaxSum{m, a.s * fa + b.s * fb};
-}
-
 // Whether token t counts.
 __device__ __forceinline__ bool counts(const Logits& l, int64_t t, int64_t y) {
     return y >= 0 && y < l.vocab && (!l.weights || l.weights[t] != 0.f);
@@ -193,7 +186,8 @@ __device__ __forceinline__ void load_chunks(u32x4 (&x)[C], const char* row, cons
     });
 }
 
-// Over a wave; every lane gets the whole.
+// Over a wave; every lane gets the whole.  (Sides that have seen nothing but -inf add nothing.  A row of nothing else ends here with a sum of 0 and gets its
+// NaN from the difference of the taken logit, or of any other, with its maximum.)
 template <int LANES = 64>
 __device__ __forceinline__ MaxSum join_wave(const MaxSum a, float k) {
     float m = a.m;
@@ -799,7 +793,7 @@ int join_lanes(int64_t rows) {
     return lanes;
 }
 
-template <class E, class F>
+template <class F>
 void for_section(const Sections& s, F&& launch) {
     if (s.chunks_a_thread == 8) launch(std::integral_constant<int, 8>{});
     else if (s.chunks_a_thread == 4) launch(std::integral_constant<int, 4>{});
@@ -910,7 +904,7 @@ hipError_t launch_logprobs(const Logits& l, int64_t first, int64_t count, float*
         const unsigned grid = (unsigned)(count * s.count);
         auto both = [&](auto elem) {
             typedef decltype(elem) E;
-            for_section<E>(s, [&](auto C) { logits_part_kernel<E, decltype(C)::value><<<grid, kSectionThreads, 0, stream>>>(a); });
+            for_section(s, [&](auto C) { logits_part_kernel<E, decltype(C)::value><<<grid, kSectionThreads, 0, stream>>>(a); });
             logits_join_kernel<<<1, kSectionThreads, 0, stream>>>(a);
         };
         if (l.dtype == STAR_F32) both(ElemF32{});
@@ -960,8 +954,8 @@ hipError_t launch_policy(const Logits& l, const PolicyArgs& p, float* logp, void
         const unsigned grid = (unsigned)(l.tokens * s.count);
         auto both = [&](auto elem) {
             typedef decltype(elem) E;
-            for_section<E>(s, [&](auto C) { logits_part_kernel<E, decltype(C)::value><<<grid, kSectionThreads, 0, stream>>>(a); });
-            for_section<E>(s, [&](auto C) { policy_section_kernel<E, decltype(C)::value><<<grid + 1, kSectionThreads, 0, stream>>>(a); });
+            for_section(s, [&](auto C) { logits_part_kernel<E, decltype(C)::value><<<grid, kSectionThreads, 0, stream>>>(a); });
+            for_section(s, [&](auto C) { policy_section_kernel<E, decltype(C)::value><<<grid + 1, kSectionThreads, 0, stream>>>(a); });
         };
         if (l.dtype == STAR_F32) both(ElemF32{});
         else both(ElemBf16{});
