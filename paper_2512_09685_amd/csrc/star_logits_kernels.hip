@@ -18,8 +18,11 @@ typedef u32x4 u32x4_any __attribute__((aligned(2)));   // (see f32x4_any)
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 // Up to this many rows are cut into sections, if they have at least so many chunks: for the policy loss, which is two launches either
-// way (48 x 32000, bf16: 11.2 against 12.7 us, 1 x 131072 11 against 19), and for log-probabilities, where the second launch
-// has to pay (1 x 131072, fp32: 9.8 against 12.6 us, bf16 9.1 against 9.9; 48 x 32000, fp32: 9.0 against 6.4).
+// way (whole rows against sections, us: 1 x 131072, bf16: 20.6 / 10.7; 64 / 96 / 128 x 131072, bf16: 21.3 / 11.2, 21.7 / 12.5, 22.1 / 15.9, fp32:
+// 24.3 / 14.2, 30.7 / 24.4, 33.8 / 30.5; x 32000 of either type 11.8 / 11.0 at 64 and 11.1 / 10.6 at 128), and for log-probabilities, where the second
+// launch has to pay (1 x 131072, fp32: 12.6 / 9.8, bf16 9.9 / 9.1; 48 x 32000, fp32: 6.4 / 9.0).  Beyond the turn the policy loss still gains
+// a little up to 160 rows (129 x 131072, bf16: 22.3 / 18.1, 160: 23.2 / 21.6, 200: 26.8 / 27.5; fp32, 129: 36.1 / 32.4, 255: equal), but log-probabilities
+// lose (128 x 131072, bf16: 11.1 / 10.3, fp32: 14.3 / 15.8; 160: 11.8 / 13.8 and 14.9 / 18.5).
 constexpr int64_t kFewTokens = 128, kPolicySections = 2048, kLogprobsSections = 16384;
 
 // 16 bytes of a row as VEC numbers, and back.
@@ -814,10 +817,12 @@ void launch_rows_of(const RowArgs& a, hipStream_t stream) {
     if (chunks <= 4096) return logits_held_kernel<E, 1024, 4, 1, WORK><<<rows, 1024, 0, stream>>>(a);
     if (chunks <= 8192) return logits_held_kernel<E, 1024, 8, 1, WORK><<<rows, 1024, 0, stream>>>(a);
     if constexpr (WORK == RowWork::Policy) {
-        // two workgroups of 512 threads a unit, of which one reads while the other writes, against one of 1024: 4096 x 72000, bf16: 211 / 270 us,
-        // 4096 x 100000: 300 / 346; fp32, 1500 x 36000: 85 / 89, 777 x 50021: 63.5 / 66, 2000 x 50257: 152 / 147
+        // two workgroups of 512 threads a unit, of which one reads while the other writes, against one of 1024 (us, two / one): 4096 x 72000, bf16:
+        // 211 / 270, 4096 x 100000: 300 / 346; fp32, 1500 x 36000: 85 / 89.  Rows of fp32 beyond 10240 chunks gain while there are few rounds of them,
+        // 512 in each: 777 x 50021 61.9 / 67.6, 1024 x 41001 62.6 / 69.3, x 45056 67.9 / 74.6, x 53248 82.6 / 85.8, 1500 x 41001 94.4 / 99.7, x 50021 116.4 /
+        // 117.5, x 53248 122.3 / 121.7, 1536 x 45056 108.0 / 107.7, 2000 x 50021 151.5 / 150.2, 3000 x 50021 221 / 218
         if (chunks <= 10240) return logits_held_kernel<E, 512, 20, 1, WORK><<<rows, 512, 0, stream>>>(a);
-        if (chunks <= 13312 && (E::VEC == 8 || rows < 1024)) return logits_held_kernel<E, 512, 26, 1, WORK><<<rows, 512, 0, stream>>>(a);
+        if (chunks <= 13312 && (E::VEC == 8 || rows < 1536)) return logits_held_kernel<E, 512, 26, 1, WORK><<<rows, 512, 0, stream>>>(a);
         if (chunks <= 16384) return logits_held_kernel<E, 1024, 16, 1, WORK><<<rows, 1024, 0, stream>>>(a);
         logits_scan_kernel<E, 1024, 18, WORK><<<rows, 1024, 0, stream>>>(a);
     } else {

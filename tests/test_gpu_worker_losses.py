@@ -475,3 +475,26 @@ def test_kl_of_policies_close_to_each_other():
 def test_losses_of_rows_in_sections(T, V, dtype):
     test_policy_loss(T, V, 1, 0.05, 0.28, dtype)
     test_logprobs_and_gradient(T, V, 3, dtype)
+
+
+@pytest.mark.parametrize("T", [1023, 1535, 1536])
+def test_policy_loss_on_both_sides_of_a_turn(T):
+    """fp32 rows of more than 10240 chunks lie with two to a unit or alone, by their number."""
+    V = 41001
+    x = torch.randn(T, V, generator=torch.Generator(device="cuda").manual_seed(T), device="cuda")
+    y = np.arange(T) * 17 % V
+    y[::5] = -1
+    z = torch.full((T,), -11.0, device="cuda")
+    stats, d = torch.zeros(4, device="cuda"), torch.full_like(x, 9.0)
+    star.star_policy_loss(x, i64(y), z, z * 0 - 1, stats, dlogits=d, clip_low=1e3, clip_high=float("inf"), scale=1.0)
+    for a in range(0, T, 128):
+        logp = torch.log_softmax(x[a:a + 128].double(), dim=1)
+        live = torch.from_numpy(y[a:a + 128] >= 0).cuda()
+        at = torch.nonzero(live)[:, 0]
+        p = torch.exp(logp)
+        p[at, i64(y[a:a + 128])[at]] -= 1.0
+        r = torch.exp(logp[at, i64(y[a:a + 128])[at]] + 11.0)
+        want = torch.zeros_like(p)
+        want[at] = -p[at] * r[:, None]                         # slope -A r = r
+        # r and p 2^-24 times a row's chain of V / 512 + 64 additions, and what exp makes of it
+        assert bool(((d[a:a + 128] - want).abs() <= 4 * wo.U * (V / 512 + 64) * want.abs() + 1e-38).all()), a
