@@ -512,7 +512,7 @@ star_status star_token_logprobs(const void *logits, star_dtype dtype, int64_t to
 /* The gradient of any function of them: dlogits[t][j] = dlogp[t] / temperature ([j == targets[t]] - exp(z[t][j] - lse[t])).
  *   lse   : device float[tokens], as star_token_logprobs returned it for the same logits and temperature
  *           (one fp32 number: rounding it adds |lse| 2^-24 to the relative error of the probabilities; for rows of
- *           |lse| > 64, or infinite, their sum is formed again, which reads them twice)
+ *           |lse| > 64, with STAR_BF16 1024, or infinite, their sum is formed again, which reads them twice)
  *   dlogp : device float[tokens], the function's derivatives; a row whose derivative is 0 is not read */
 star_status star_token_logprobs_grad(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
                                      const int64_t *targets, float temperature, const float *lse, const float *dlogp,

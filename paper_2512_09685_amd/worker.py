@@ -164,7 +164,7 @@ def star_token_logprobs(logits, targets, logp_out, *, lse_out=None, temperature:
 
 def star_token_logprobs_grad(logits, targets, lse, dlogp, dlogits, *, temperature: float = 1.0, stream=None) -> None:
     """``dlogits`` of a function whose derivatives by the log-probabilities are ``dlogp`` (float32 [tokens]); ``lse`` as
-    ``star_token_logprobs`` left it (beyond 64 in size, where one fp32 number no longer holds it well, a row's sum is formed again).
+    ``star_token_logprobs`` left it (beyond 64 in size, of bfloat16 rows 1024, where one fp32 number no longer holds it well enough, a row's sum is formed again).
     ``dlogits`` may be ``logits``."""
     lib = _library()
     head, out, device = _logits(logits, targets, dlogits)

@@ -134,8 +134,8 @@ def check_gradient(x, x64, y, temperature, dtype):
     star.star_token_logprobs_grad(x, yd, lse, f32(dlogp), d, temperature=temperature)
     c = dlogp.astype(np.float64) * live / float(np.float32(temperature))
     want = wo.dlogits_of(p, y, live, c)
-    # up to 64 the normaliser is taken as it was rounded; beyond, the row's own sum is
-    rounded = np.where(np.abs(wlse) <= 64.001, wo.U * np.abs(wlse), 0.0)
+    # up to 64, of bf16 rows 1024, the normaliser is taken as it was rounded; beyond, the row's own sum is
+    rounded = np.where(np.abs(wlse) <= (64.001 if dtype == "f32" else 1024.01), wo.U * np.abs(wlse), 0.0)
     close(d, want, wo.gradient_bound(want, p, y, live, c, 4 * wo.U * c, bound + rounded, dtype), "dlogits")
     star.star_token_logprobs_grad(x, yd, lse, f32(dlogp), x, temperature=temperature)
     assert torch.equal(x, d)
