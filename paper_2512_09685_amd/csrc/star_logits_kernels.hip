@@ -330,7 +330,7 @@ struct RowArgs {
     int64_t ld_out, first, rows;   // rows [first, first + rows)
     bool again;                    // the rows are read again by the gradient's launch
     const float *lse_in, *dlogp;   // of the gradient alone, as are
-    const MaxSum* sums_in;         // the rows' maxima and sums; null: lse_in
+    const MaxSum* sums_in;         // the rows' maxima and sums, or lse_in (Normaliser)
     MaxSum* parts;                 // of rows that several workgroups share: [rows][sections]
     float* picked;                 // of such rows: the target's logit, which a gradient in place would be written over
     int sections, lanes;           // lanes that join a row's sections: a power of two, no more than a wave's
@@ -655,6 +655,10 @@ __device__ __forceinline__ void join_pair_loss(const PairLoss& p) {
     if (threadIdx.x == 0) *p.out = (float)(sum[0] * p.scale);
 }
 
+// What a row's probabilities are taken from: the maxima and sums that the call's own first reading left, or a normaliser that the caller hands in.
+// (Two kernels of it: one that asks took 326 against 321 us for the preference loss of 12288 x 32768, bf16.)
+enum class Normaliser { Sums, Lse };
+
 // The gradient alone, which needs nothing of the rest of its row: NT threads to a section of C chunks each, ROWS rows a workgroup.  The
 // last rows come first: the memory-side cache may still hold them.
 // A normaliser that the caller hands in is one fp32 number, which holds a row's sum the worse the larger it is: rounding it enters every p as |lse|
@@ -663,18 +667,17 @@ __device__ __forceinline__ void join_pair_loss(const PairLoss& p) {
 // fp32: 114 against 78 us; bf16, 12288 x 32768: 452 / 281, 8192 x 65536: 1166 / 379; 1 x 131072: 34 / 7.5.)
 template <class E>
 constexpr float kMostLse = E::VEC == 4 ? 64.f : 1024.f;
-template <class E, int NT, int C, int ROWS>
+template <class E, int NT, int C, int ROWS, Normaliser FROM>
 __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) {
     __shared__ MaxSum shared[NT / 64];
     const int V = (int)a.l.vocab, tid = threadIdx.x % NT, section = (int)(blockIdx.x % (unsigned)a.sections);
     const int64_t in = (int64_t)(blockIdx.x / (unsigned)a.sections) * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0);
-    if (a.loss.out && blockIdx.x == gridDim.x - 1) return join_pair_loss(a.loss);   // (a workgroup more than the rows need)
+    if (FROM == Normaliser::Sums && a.loss.out && blockIdx.x == gridDim.x - 1) return join_pair_loss(a.loss);   // (a workgroup more than the rows need)
     if (ROWS > 1 && in >= a.rows) return;
     const int64_t t = a.first + (a.rows - 1 - in), y = a.l.targets[t];
     const char* row = row_of(a, t, E::BYTES);
     char* out = a.dlogits + t * a.ld_out * E::BYTES;
-    const float d = a.dlogp[t], lse = a.sums_in ? 0.f : a.lse_in[t], k = a.l.k;
-    const MaxSum sum = a.sums_in ? a.sums_in[t] : MaxSum{0.f, 1.f};
+    const float d = a.dlogp[t], lse = FROM == Normaliser::Lse ? a.lse_in[t] : 0.f, k = a.l.k;
     const int first = section * NT * C;
     if (!counts(a.l, t, y) || d == 0.f) {
         zero_row<E, NT>(out, V, tid, first, section + 1 == a.sections ? 0x7fffffff : first + NT * C);
@@ -682,7 +685,7 @@ __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) 
     }
     const RowSpan sp = row_span<E, NT>(row, V);
     const float c = d * a.l.inv_t;
-    if (!(fabsf(lse) <= kMostLse<E>)) {
+    if (FROM == Normaliser::Lse && !(fabsf(lse) <= kMostLse<E>)) {
         if (section > 0) return;
         const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
         const MaxSum all = join_group<NT>(with_element(scan_chunks<E, NT, Reading::Again>(row, sp, k, tid), edge, k), k, shared);
@@ -695,8 +698,8 @@ __global__ __launch_bounds__(NT* ROWS) void logits_grad_kernel(const RowArgs a) 
     load_chunks<E, NT>(x, row, sp, first + tid);
     const float edge = section == 0 && tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
     Slope p;
-    if (a.sums_in) {
-        p = slope_of(k, sum, c, y);
+    if constexpr (FROM == Normaliser::Sums) {
+        p = slope_of(k, a.sums_in[t], c, y);
     } else {
         // p_j = 2^((l_j - m) k - rest log2 e) with an m near lse times the temperature, and what lse is more than m / temperature: only differences
         // are multiplied with the rounded k
@@ -832,19 +835,19 @@ void launch_rows_of(const RowArgs& a, hipStream_t stream) {
     }
 }
 
-template <class E>
+template <class E, Normaliser FROM>
 void launch_grad_of(RowArgs a, hipStream_t stream) {
     const int64_t chunks = chunks_of<E>(a.l);
     const unsigned rows = (unsigned)a.rows;
     a.sections = 1;
     const unsigned fours = (rows + 3) / 4, more = a.loss.out ? 1 : 0;
-    if (chunks <= 128) return logits_grad_kernel<E, 64, 2, 4><<<fours + more, 256, 0, stream>>>(a);
-    if (chunks <= 512) return logits_grad_kernel<E, 64, 8, 4><<<fours + more, 256, 0, stream>>>(a);
+    if (chunks <= 128) return logits_grad_kernel<E, 64, 2, 4, FROM><<<fours + more, 256, 0, stream>>>(a);
+    if (chunks <= 512) return logits_grad_kernel<E, 64, 8, 4, FROM><<<fours + more, 256, 0, stream>>>(a);
     const bool few = a.rows * chunks < 512 * 2048;   // (fewer than two workgroups a unit with sections of 2048 chunks)
     a.sections = (int)(few ? (chunks + 511) / 512 : (chunks + 2047) / 2048);
     const unsigned grid = rows * (unsigned)a.sections + more;
-    if (few) logits_grad_kernel<E, 256, 2, 1><<<grid, 256, 0, stream>>>(a);
-    else logits_grad_kernel<E, 256, 8, 1><<<grid, 256, 0, stream>>>(a);
+    if (few) logits_grad_kernel<E, 256, 2, 1, FROM><<<grid, 256, 0, stream>>>(a);
+    else logits_grad_kernel<E, 256, 8, 1, FROM><<<grid, 256, 0, stream>>>(a);
 }
 
 // Workspace of rows in sections: their results, then the targets' logits.
@@ -935,8 +938,13 @@ hipError_t launch_logprobs_grad(const Logits& l, int64_t first, int64_t count, c
     a.ld_out = ld_out;
     return in_launches(a, first, count, [&](RowArgs r) {
         if (r.first + r.rows == first + count) r.loss = loss;   // the last one
-        if (l.dtype == STAR_F32) launch_grad_of<ElemF32>(r, stream);
-        else launch_grad_of<ElemBf16>(r, stream);
+        auto of = [&](auto elem) {
+            typedef decltype(elem) E;
+            if (sums) launch_grad_of<E, Normaliser::Sums>(r, stream);
+            else launch_grad_of<E, Normaliser::Lse>(r, stream);
+        };
+        if (l.dtype == STAR_F32) of(ElemF32{});
+        else of(ElemBf16{});
     });
 }
 
