@@ -492,9 +492,12 @@ star_status star_plan_even_split(int32_t workgroups, int64_t tiles, int64_t *fir
  * row t at element t * ld (ld >= vocab).  targets[t] is the token taken at row t.  A target outside [0, vocab) marks a
  * token that does not count (a prompt, padding): its row is not read, its log-probability is reported as 0, its
  * gradient row is zero.  dlogits has the shape and type of the logits, rows at t * ld_out; it may be the logits
- * themselves (same address, same ld), but must not overlap them otherwise.  Addresses need the alignment of one
- * element only.  With z = logits / temperature (1e-4 to 1e4), logp = z[target] - lse, lse = log sum exp z.  Values of -inf (banned
- * tokens) have probability 0; a row of nothing else, or one that holds NaN or +inf, has a log-probability of NaN.
+ * themselves (same address, same ld), but must not overlap them otherwise; no other output may overlap an input or
+ * another output (logp_out over an input of as many floats is refused).  Sizes: up to 2^22 tokens and 2^30 words;
+ * no tensor beyond 2^42 elements, as its rows lie (a weight gradient: up to 2^30 tokens, 2^22 columns and 2^22
+ * blocks of 64 by 64).  Addresses need the alignment of one element only.  With z = logits / temperature (1e-4 to
+ * 1e4), logp = z[target] - lse, lse = log sum exp z.  Values of -inf (banned tokens) have probability 0; a row of
+ * nothing else, or one that holds NaN or +inf, has a log-probability of NaN.
  * All arithmetic is fp32 or wider; a gradient is rounded once, to its own type.  Results are the same from run to run.
  *
  * `workspace`: device memory of at least the bytes that the matching *_workspace function returns for the call's

@@ -23,6 +23,12 @@ bool known(int dtype) { return dtype == STAR_F32 || dtype == STAR_BF16; }
 size_t bytes_of(int dtype) { return dtype == STAR_F32 ? 4 : 2; }
 bool on_grid(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
+// Whether log-probabilities written to `out` would be written over `in`, both `tokens` floats: inputs are read again behind them.
+bool over(const float* out, const float* in, int64_t tokens) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(out), b = reinterpret_cast<uintptr_t>(in), bytes = sizeof(float) * (uintptr_t)tokens;
+    return out && in && (a < b ? b - a : a - b) < bytes;
+}
+
 // `rows` rows of `length` values, `ld` apart: no size negative, no offset beyond 63 bits.
 bool rows_fit(int64_t rows, int64_t length, int64_t ld) {
     return rows >= 0 && length >= 0 && ld >= length && ld <= kMostElements && (rows == 0 || ld == 0 || rows <= kMostElements / ld);
@@ -159,6 +165,8 @@ star_status star_policy_loss(const void* logits, star_dtype dtype, int64_t token
     if (tokens > 0) {
         if (!old_logp || !advantages) return set_error(STAR_ERR_NULL, "old_logp or advantages is NULL");
         if (!ref_logp && params->kl_coef != 0.f) return set_error(STAR_ERR_NULL, "ref_logp is NULL and kl_coef is not 0");
+        if (over(logp_out, old_logp, tokens) || over(logp_out, ref_logp, tokens) || over(logp_out, advantages, tokens) || over(logp_out, weights, tokens))
+            return set_error(STAR_ERR_SHAPE, "logp_out overlaps an input");
         STAR_CHECK(check_workspace(workspace, workspace_bytes, star_policy_loss_workspace(dtype, tokens, vocab)));
     }
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, weights, params->temperature);
@@ -183,6 +191,7 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
     if (offsets[0] != 0 || offsets[2 * (int64_t)pairs] != tokens) return set_error(STAR_ERR_GROUP, "offsets must run from 0 to tokens");
     for (int64_t i = 0; i < 2 * (int64_t)pairs; ++i)
         if (offsets[i + 1] < offsets[i]) return set_error(STAR_ERR_GROUP, "offsets decrease");
+    if (over(logp_out, ref_logp, tokens) || over(logp_out, weights, tokens)) return set_error(STAR_ERR_SHAPE, "logp_out overlaps an input");
     const PreferenceSpace space = preference_space(dtype, tokens, vocab, pairs);
     STAR_CHECK(check_workspace(workspace, workspace_bytes, space.total));
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, weights, params->temperature);

@@ -237,3 +237,18 @@ def test_results_stay_inside_the_weight_gradient(tmp_path):
     assert r.returncode == 0, r.stderr
     r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0 and "blocks in range" in r.stdout, (r.stdout, r.stderr)
+
+
+@pytest.mark.parametrize("off", [0, 8, -8])
+def test_log_probabilities_over_an_input_refused(lib, off):
+    """logp_out over what the call reads again behind it: 3 tokens, 12 bytes each."""
+    far, out, o = 4 * P, P + 64, np.array([0, 1, 3], np.int64)
+    for which in range(4):
+        v = [far, 2 * far, 3 * far, 4 * far]                     # old_logp, ref_logp, advantages, weights
+        v[which] = out + off
+        assert lib.star_policy_loss(*_head({}), *v, _policy(), None, 0, out, P, None, 0, 0) == SHAPE and "overlaps" in star.last_error()
+        v[which] = out + 12                                      # side by side: the next check's answer
+        assert lib.star_policy_loss(*_head({}), *v, _policy(), None, 0, out, P, None, 0, 0) == NULL
+    for ref, w in ((out + off, far), (far, out + off)):
+        args = [ref, w, 1, o.ctypes.data, _preference(), None, 0, out, None, P, None, 0, 0]
+        assert lib.star_preference_loss(*_head({}), *args) == SHAPE and "overlaps" in star.last_error()
