@@ -378,7 +378,8 @@ __device__ __forceinline__ float fold_row(float x, float* shared, Op&& op) {
 }
 
 // Workgroups go round the 8 dies; this gives each die a run of long rows of its own (8192 x 65536, bf16: 4 % faster, 16384 x
-// 32768: 7 %; rows of 16 KB and less are up to 5 % slower that way and stay in the order of the workgroups).
+// 32768: 7 %; rows of 16 KB and less are up to 5 % slower that way and stay in the order of the workgroups, as do rows whose number is no
+// multiple of 8).
 __device__ __forceinline__ int64_t die_run(unsigned id) {
     return gridDim.x % 8 == 0 ? (id % 8) * (gridDim.x / 8) + id / 8 : id;
 }
