@@ -1,0 +1,469 @@
+"""Measured cases of a worker that learns from a teacher: log-probabilities with entropy and the most likely
+alternatives, the distillation loss on such alternatives with its gradient, and the root-mean-square norm in front of
+the head, whose output is kept in 8 bits.
+
+``own`` false: the plain form, elementary torch operations in 32 bits (64 for long sums and differences of shares).
+``own`` true: the calls of the package.
+"""
+import math
+
+import torch
+
+own = False
+
+_BF16, _F32 = "bf16", "f32"
+_DTYPES = {_BF16: torch.bfloat16, _F32: torch.float32}
+_BLOCK = 32          # tokens that share one scale in a saved activation
+_E4M3_MAX = 448.0
+_EPS = 1e-6
+
+
+# ------------------------------------------------------------------------------------------------------------ cases
+def _logits(op, name, tokens, vocab, dtype, k, *, pad=0, masked=0.0, banned=0.0, temperature=1.0, **more):
+    return dict(op=op, name=name, tokens=tokens, vocab=vocab, dtype=dtype, k=k, pad=pad, masked=masked, banned=banned,
+                temperature=temperature, **more)
+
+
+def _norm(op, name, tokens, width, dtype, *, residual=True, packed=False, gain="f32"):
+    return dict(op=op, name=name, tokens=tokens, width=width, dtype=dtype, residual=residual, packed=packed, gain=gain)
+
+
+def listed():
+    return [
+        # a token just sampled, its log-probability reported with the 20 alternatives (latency)
+        _logits("top", "alternatives of one token", 1, 32000, _BF16, 20, targeted=True),
+        # the teacher's pass over a batch: what a student is to learn from; prompts masked out
+        _logits("top", "alternatives teacher batch", 4096, 131072, _BF16, 64, masked=0.1, targeted=True),
+        # a look at a model's certainty: fp32 logits of an odd vocabulary in padded rows, no taken tokens
+        _logits("top", "alternatives odd fp32", 1023, 50021, _F32, 5, pad=11, temperature=0.7, targeted=False),
+        # a caller's own loss with an entropy bonus and a term on the alternatives: both directions
+        _logits("top_grad", "alternatives own loss", 2048, 65536, _BF16, 8, masked=0.2, targeted=True),
+        # the last few tokens of one answer, a micro-batch that is all latency
+        _logits("distill", "distillation few tokens", 48, 32000, _BF16, 32, ce=0.0, renormalise=False),
+        # a micro-batch of a student, prompts masked out, a vocabulary padded with banned words
+        _logits("distill", "distillation batch", 8192, 65536, _BF16, 64, masked=0.25, banned=0.02, ce=0.0, renormalise=False),
+        # fp32 logits of an odd vocabulary, many alternatives taken as the whole of the teacher, taken tokens mixed in
+        _logits("distill", "distillation odd fp32", 777, 50021, _F32, 100, masked=0.1, temperature=2.0, ce=0.3, renormalise=True),
+        # rows of a large vocabulary that lie at any address
+        _logits("distill", "distillation long rows", 2000, 131075, _BF16, 20, pad=2, ce=0.5, renormalise=False),
+        # one token of a model that answers (latency)
+        _norm("norm", "norm one token", 1, 4096, _BF16),
+        # a long micro-batch, the output kept in 8 bits and brought back whole; ragged last block
+        _norm("norm", "norm kept", 16381, 4096, _BF16, packed=True),
+        # a wide layer's norm in both directions
+        _norm("norm_grad", "norm both directions", 8192, 8192, _BF16),
+        # fp32 training, odd width, the model's first norm: nothing to add
+        _norm("norm_grad", "norm odd fp32", 1000, 5003, _F32, residual=False),
+    ]
+
+
+def _between(rng, low, high):
+    return int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))
+
+
+def draw(rng):
+    op = rng.choice(["top", "top", "top_grad", "distill", "distill", "distill", "norm", "norm", "norm_grad", "norm_grad"])
+    dtype = rng.choice([_BF16, _F32])
+    if op in ("norm", "norm_grad"):
+        tokens, width = _between(rng, 1, 65536), _between(rng, 64, 16384)
+        if rng.random() < 0.5:
+            width = -(-width // 64) * 64
+        tokens = max(1, min(tokens, 2 ** 26 // width))
+        case = _norm(op, "", tokens, width, dtype, residual=rng.random() < 0.7, packed=op == "norm" and rng.random() < 0.6,
+                     gain=rng.choice([_F32, _BF16]))
+    else:
+        tokens, vocab, k = _between(rng, 1, 16384), _between(rng, 1000, 131072), _between(rng, 1, 128)
+        if rng.random() < 0.5:
+            vocab = -(-vocab // 64) * 64
+        tokens = max(1, min(tokens, 2 ** 27 // vocab))
+        case = _logits(op, "", tokens, vocab, dtype, k, pad=rng.choice([0, 0, 3, 8]), masked=rng.choice([0.0, 0.25, 0.5]),
+                       banned=rng.choice([0.0, 0.02]), temperature=rng.choice([1.0, 0.7, 2.0]))
+        if op == "distill":
+            case.update(ce=rng.choice([0.0, 0.3]), renormalise=rng.choice([False, False, True]))
+        else:
+            case.update(targeted=op == "top_grad" or rng.random() < 0.7)
+    case.pop("name", None)
+    return case
+
+
+# ----------------------------------------------------------------------------------------------------------- inputs
+def _generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed))
+    return g
+
+
+def _masked_count(case):
+    return min(int(case["tokens"] * case["masked"]), case["tokens"] - 1)
+
+
+def _allowed(case):
+    """Words that are not banned: the front of the vocabulary."""
+    return case["vocab"] - int(case["vocab"] * case["banned"])
+
+
+def _prepare_norm(case, g):
+    T, K, dtype, dev = case["tokens"], case["width"], _DTYPES[case["dtype"]], "cuda"
+    column = torch.exp(0.5 * torch.randn(K, generator=g, device=dev))
+    column[::97] *= 24.0                                         # a few columns are far larger than the rest
+    x = (torch.randn(T, K, generator=g, device=dev) * column).to(dtype)
+    state = dict(case=case, x=x, res=None, sum=None,
+                 gain=(1.0 + 0.2 * torch.randn(K, generator=g, device=dev)).to(_DTYPES[case["gain"]]),
+                 y=torch.empty_like(x), rstd=torch.empty(T, device=dev))
+    if case["residual"]:
+        state["res"] = (torch.randn(T, K, generator=g, device=dev) * column * 4.0).to(dtype)
+        state["sum"] = torch.empty_like(x)
+    if case["packed"]:
+        state["back"] = torch.empty_like(x)
+    if case["op"] == "norm_grad":
+        state["dy"] = (torch.randn(T, K, generator=g, device=dev) * 1e-3).to(dtype)
+        state["dres"] = (torch.randn(T, K, generator=g, device=dev) * 1e-3).to(dtype) if case["residual"] else None
+        state["dx"], state["dgain"] = torch.empty_like(x), torch.empty(K, device=dev)
+    return state
+
+
+def prepare(case, seed):
+    g = _generator(seed)
+    dev = "cuda"
+    if case["op"] in ("norm", "norm_grad"):
+        return _prepare_norm(case, g)
+    T, V, k, dtype, temperature = case["tokens"], case["vocab"], case["k"], _DTYPES[case["dtype"]], case["temperature"]
+    W, allowed = V + case["pad"], _allowed(case)
+    whole = torch.empty(T, W, dtype=dtype, device=dev)
+    # 48 words of a row hold most of its weight, the likelier the fewer
+    likely = torch.randint(0, allowed, (T, 48), generator=g, device=dev)
+    height = (13.0 - 2.0 * torch.log(1.0 + torch.arange(48, device=dev)))[None, :] + torch.randn(T, 48, generator=g, device=dev)
+    distill = case["op"] == "distill"
+    ids = torch.full((T, k), -1, dtype=torch.int64, device=dev)
+    logp = torch.full((T, k), -math.inf, device=dev)
+    step = max(1, 2 ** 27 // W)
+    for a in range(0, T, step):
+        n = min(step, T - a)
+        rows = torch.randn(n, W, generator=g, device=dev) * 2.0
+        rows.scatter_reduce_(1, likely[a:a + n], height[a:a + n], "amax")      # (the same word twice: the larger)
+        rows[:, allowed:V] = -math.inf
+        whole[a:a + n] = rows
+        if distill:
+            # the teacher: near the student, not the same
+            z = (rows[:, :V] + 0.7 * torch.randn(n, V, generator=g, device=dev)) / temperature
+            z[:, allowed:] = -math.inf
+            value, at = torch.topk(z, min(k, allowed), dim=1)
+            ids[a:a + n, :value.shape[1]] = at
+            logp[a:a + n, :value.shape[1]] = value - torch.logsumexp(z, dim=1, keepdim=True)
+    pick = likely.gather(1, torch.randint(0, 48, (T, 1), generator=g, device=dev))[:, 0]
+    targets = torch.where(torch.rand(T, generator=g, device=dev) < 0.7, pick, torch.randint(0, allowed, (T,), generator=g, device=dev))
+    masked = torch.randperm(T, generator=g, device=dev)[:_masked_count(case)]
+    targets[masked] = -100
+    state = dict(case=case, logits=whole[:, :V], targets=targets)
+    if distill:
+        ids[1::7, k - k // 4:] = -1                             # a teacher that reported fewer for some rows
+        logp[1::7, k - k // 4:] = -math.inf
+        state.update(ids=ids, tlogp=logp, stats=torch.empty(4, device=dev), kl=torch.empty(T, device=dev),
+                     weights=torch.full((T,), 1.0 / (T - _masked_count(case)), device=dev), dlogits=torch.empty_like(whole)[:, :V])
+        return state
+    if not case["targeted"]:
+        state["targets"] = None
+    state.update(logp=torch.empty(T, device=dev) if case["targeted"] else None, entropy=torch.empty(T, device=dev), ids=ids, top=logp)
+    if case["op"] == "top_grad":
+        state.update(dlogp=torch.randn(T, generator=g, device=dev) / T, dentropy=torch.randn(T, generator=g, device=dev) * 0.1 / T,
+                     dtop=torch.randn(T, k, generator=g, device=dev) * 0.1 / T, dlogits=torch.empty_like(whole)[:, :V])
+    return state
+
+
+# ------------------------------------------------------------------------------------------------------ plain forms
+def _softmax(logits, temperature):
+    z = logits.float() / temperature
+    m = z.amax(dim=1, keepdim=True)
+    e = torch.exp(z - m)
+    return z, m, e, e.sum(dim=1, keepdim=True)
+
+
+def _largest(logits, k):
+    """Ids of the k largest of each row, ties to the lower one: keys of 64 bits, no two of them alike."""
+    T, V = logits.shape
+    ids = torch.empty(T, k, dtype=torch.int64, device=logits.device)
+    low = 2 ** 32 - 1 - torch.arange(V, device=logits.device)
+    step = max(1, 2 ** 27 // V)
+    for a in range(0, T, step):
+        bits = (logits[a:a + step].float() + 0.0).view(torch.int32)
+        order = (bits ^ ((bits >> 31) & 0x7fffffff)).long()
+        key = torch.topk(order * 2 ** 32 + low, k, dim=1).values
+        ids[a:a + step] = 2 ** 32 - 1 - (key & (2 ** 32 - 1))
+    return ids
+
+
+def _plain_top(s, case):
+    k = case["k"]
+    z, m, e, total = _softmax(s["logits"], case["temperature"])
+    lse = m + torch.log(total)
+    gap = torch.where(e > 0, m - z, torch.zeros((), device=z.device))
+    entropy = torch.log(total[:, 0]) + (e * gap).sum(dim=1) / total[:, 0]
+    ids = _largest(s["logits"], k)
+    top = z.gather(1, ids) - lse
+    out = []
+    if s["targets"] is not None:
+        live = s["targets"] >= 0
+        logp = (z.gather(1, s["targets"].clamp(min=0)[:, None]) - lse)[:, 0]
+        out.append(torch.where(live, logp, 0.0))
+        entropy, top, ids = torch.where(live, entropy, 0.0), torch.where(live[:, None], top, 0.0), torch.where(live[:, None], ids, -1)
+    out += [entropy, ids, top]
+    if case["op"] == "top":
+        return out
+    live = s["targets"] >= 0
+    zero = torch.zeros((), device=z.device)
+    dlogp, dH = torch.where(live, s["dlogp"], zero), torch.where(live, s["dentropy"], zero)
+    dtop = torch.where(live[:, None], s["dtop"], zero)
+    whole = dlogp + dtop.sum(dim=1)
+    p = e / total
+    d = -p * (whole[:, None] + dH[:, None] * (entropy[:, None] + torch.where(e > 0, z - lse, zero)))
+    d.scatter_add_(1, ids.clamp(min=0), dtop)
+    d.scatter_add_(1, s["targets"].clamp(min=0)[:, None], dlogp[:, None])
+    s["dlogits"].copy_(d / case["temperature"])
+    return out + [s["dlogits"]]
+
+
+def _plain_distill(s, case):
+    T, V = s["logits"].shape
+    ce = case["ce"]
+    z, m, e, total = _softmax(s["logits"], case["temperature"])
+    live = s["targets"] >= 0
+    there = s["ids"] >= 0
+    at = torch.where(there, s["ids"], V)                                       # a column more for what is not there
+    other = torch.cat([e, torch.zeros(T, 1, device=e.device)], dim=1).scatter(1, at, 0.0)[:, :V]
+    rest = other.sum(dim=1)
+    logp = (z.gather(1, s["ids"].clamp(min=0)) - m - torch.log(total)).double()
+    q = torch.where(there, torch.exp(s["tlogp"].double()), 0.0)
+    share = q.sum(dim=1)
+    if case["renormalise"]:
+        q = q / share[:, None]
+        left = torch.zeros_like(share)
+    else:
+        left = (1.0 - share).clamp(min=0.0)
+    left = torch.where(rest > 0, left, 0.0)
+    kl = torch.where(q > 0, q * (torch.log(q) - logp), 0.0).sum(dim=1)
+    kl = kl + torch.where(left > 0, left * (torch.log(left) - torch.log((rest / total[:, 0]).double())), 0.0)
+    whole = q.sum(dim=1) + left
+    target_logp = (z.gather(1, s["targets"].clamp(min=0)[:, None]) - m - torch.log(total))[:, 0].double()
+    w = torch.where(live, s["weights"], 0.0)
+    kl = torch.where(live, kl, 0.0)
+    nll = torch.where(live, -target_logp, 0.0)
+    sums = [(w.double() * kl).sum(), (w.double() * nll).sum(), w.double().sum()]
+    stats = torch.stack([sums[0] + ce * sums[1]] + sums).float()
+    scale = w / case["temperature"]
+    both = (whole.float() + ce)[:, None] / total
+    d = e * both
+    d -= other * torch.where(rest > 0, left.float() / rest, 0.0)[:, None]
+    d.scatter_add_(1, s["ids"].clamp(min=0), -torch.where(there, q, 0.0).float())
+    d.scatter_add_(1, s["targets"].clamp(min=0)[:, None], torch.where(live, -ce, 0.0).float()[:, None])
+    s["dlogits"].copy_(torch.where(live[:, None], d * scale[:, None], 0.0))
+    return [stats, kl.float(), s["dlogits"]]
+
+
+def _plain_saved(x):
+    """The values that the 8-bit form stands for: blocks of 32 tokens of a column, e4m3 times a power of two."""
+    T, K = x.shape
+    blocks = -(-T // _BLOCK)
+    full = torch.zeros(blocks * _BLOCK, K, device=x.device)
+    full[:T] = x
+    full = full.view(blocks, _BLOCK, K)
+    most = full.abs().amax(dim=1, keepdim=True)
+    mantissa, exponent = torch.frexp(most / _E4M3_MAX)       # the smallest e with most <= 448 * 2^e
+    e = torch.where(mantissa == 0.5, exponent - 1, exponent).clamp(min=-117)
+    scale = torch.ldexp(torch.ones_like(most), e)
+    held = (full / scale).to(torch.float8_e4m3fn).float() * scale
+    return held.view(blocks * _BLOCK, K)[:T]
+
+
+def _plain_norm(s, case):
+    dtype, K = _DTYPES[case["dtype"]], case["width"]
+    h = s["x"].float()
+    if s["res"] is not None:
+        s["sum"].copy_(h + s["res"].float())
+        h = s["sum"].float()
+    rstd = (1.0 / torch.sqrt(h.double().square().sum(dim=1) / K + _EPS)).float()
+    gain = s["gain"].float()
+    held = h * rstd[:, None]
+    s["y"].copy_(held * gain)
+    out = ([s["sum"]] if s["res"] is not None else []) + [s["y"], rstd]
+    if case["packed"]:
+        s["back"].copy_(_plain_saved(s["y"].float()))
+        out.append(s["back"])
+    if case["op"] == "norm":
+        return out
+    dy = s["dy"].float()
+    d = dy * gain
+    mean = ((d * held).double().sum(dim=1) / K).float()
+    d = rstd[:, None] * (d - held * mean[:, None])
+    if s["dres"] is not None:
+        d = d + s["dres"].float()
+    s["dx"].copy_(d.to(dtype))
+    return out + [s["dx"], (dy * held).double().sum(dim=0).float()]
+
+
+# --------------------------------------------------------------------------------------------------------- one pass
+def run(s):
+    case = s["case"]
+    return _run_own(s, case) if own else _run_plain(s, case)
+
+
+def _run_plain(s, case):
+    return {"top": _plain_top, "top_grad": _plain_top, "distill": _plain_distill, "norm": _plain_norm,
+            "norm_grad": _plain_norm}[case["op"]](s, case)
+
+
+def _run_own(s, case):
+    import paper_2512_09685_amd as star
+
+    op = case["op"]
+    if op == "distill":
+        star.star_distill_loss(s["logits"], s["ids"], s["tlogp"], s["stats"], targets=s["targets"], dlogits=s["dlogits"],
+                               weights=s["weights"], scale=1.0, ce_coef=case["ce"], renormalise=case["renormalise"],
+                               temperature=case["temperature"], kl_out=s["kl"])
+        return [s["stats"], s["kl"], s["dlogits"]]
+    if op in ("top", "top_grad"):
+        t = case["temperature"]
+        star.star_top_logprobs(s["logits"], s["targets"], s["logp"], entropy_out=s["entropy"], top_ids=s["ids"], top_logp=s["top"],
+                               temperature=t)
+        out = ([s["logp"]] if s["logp"] is not None else []) + [s["entropy"], s["ids"], s["top"]]
+        if op == "top":
+            return out
+        star.star_top_logprobs_grad(s["logits"], s["targets"], s["dlogits"], dlogp=s["dlogp"], dentropy=s["dentropy"], top_ids=s["ids"],
+                                    dtop=s["dtop"], temperature=t)
+        return out + [s["dlogits"]]
+    T, K = s["x"].shape
+    packed = torch.empty(star.star_act_bytes(T, K), dtype=torch.uint8, device=s["x"].device) if case["packed"] else None
+    star.star_rms_norm(s["x"], s["gain"], s["y"], residual=s["res"], sum_out=s["sum"], rstd_out=s["rstd"], packed=packed, eps=_EPS)
+    out = ([s["sum"]] if s["res"] is not None else []) + [s["y"], s["rstd"]]
+    if packed is not None:
+        star.star_act_unpack(packed, s["back"])
+        out.append(s["back"])
+    if op == "norm":
+        return out
+    h = s["x"] if s["sum"] is None else s["sum"]
+    star.star_rms_norm_grad(s["dy"], h, s["gain"], s["rstd"], s["dx"], dresidual=s["dres"], dweight=s["dgain"])
+    return out + [s["dx"], s["dgain"]]
+
+
+# ------------------------------------------------------------------------------------------------------------- work
+def work(case):
+    size = {_BF16: 2, _F32: 4}
+    T = case["tokens"]
+    if case["op"] in ("norm", "norm_grad"):
+        K = case["width"]
+        one = T * K * size[case["dtype"]]
+        moved = one * (4 if case["residual"] else 2) + K * size[case["gain"]] + 4 * T
+        if case["packed"]:
+            moved += 2 * (-(-T // _BLOCK) * K * (_BLOCK + 1)) + one
+        if case["op"] == "norm_grad":
+            moved += one * (3 if case["residual"] else 2) + 4 * K
+        return {"bytes": moved, "flops": (12 if case["op"] == "norm_grad" else 5) * T * K}
+    row = case["vocab"] * size[case["dtype"]]
+    counted = T if case["op"] != "distill" and not case["targeted"] else T - _masked_count(case)
+    small = T * (12 * case["k"] + 20)
+    if case["op"] == "top_grad":
+        small += T * (4 * case["k"] + 8)
+    written = 0 if case["op"] == "top" else T * row
+    return {"bytes": counted * row + written + small, "flops": (6 if case["op"] == "top" else 10) * counted * case["vocab"]}
+
+
+# ------------------------------------------------------------------------------------------------- from the definition
+def _exact_saved(x):
+    """Round-half-even on the grid of each value's own binade, 64 bits, straight from the definition of the format."""
+    T, K = x.shape
+    b = torch.nn.functional.pad(x.double(), (0, 0, 0, -T % _BLOCK)).unflatten(0, (-1, _BLOCK))
+    most = b.abs().max(dim=1, keepdim=True).values
+    e = torch.ceil(torch.log2(most.clamp(min=1e-300) / _E4M3_MAX))
+    e = torch.where(most <= _E4M3_MAX * torch.exp2(e - 1.0), e - 1.0, e)      # (where log2 was rounded over a border)
+    e = torch.where(most > _E4M3_MAX * torch.exp2(e), e + 1.0, e).clamp(min=-117.0)
+    v = b * torch.exp2(-e)
+    step = torch.exp2(torch.floor(torch.log2(v.abs().clamp(min=2.0 ** -6))) - 3.0)
+    return (torch.round(v / step) * step * torch.exp2(e)).flatten(0, 1)[:T]
+
+
+def _exact_norm(s, case):
+    out = []
+    h = s["x"].double()
+    if s["res"] is not None:
+        out.append(h + s["res"].double())
+        h = out[0].float().to(s["x"].dtype).double()                         # the norm is that of the sum as it is stored
+    rms = torch.sqrt((h ** 2).mean(dim=1, keepdim=True) + _EPS)
+    unit, gain = h / rms, s["gain"].double()
+    out += [unit * gain, 1.0 / rms[:, 0]]
+    if case["packed"]:
+        out.append(_exact_saved((unit * gain).to(s["x"].dtype)))
+    if case["op"] == "norm":
+        return out
+    dy = s["dy"].double()
+    along = (dy * gain * unit).mean(dim=1, keepdim=True)
+    dx = (dy * gain - along * unit) / rms
+    if s["dres"] is not None:
+        dx += s["dres"].double()
+    return out + [dx, (unit * dy).sum(dim=0)]
+
+
+def _exact_top(s, case, a, b):
+    """Rows [a, b) of everything."""
+    beta, k = 1.0 / case["temperature"], case["k"]
+    x = s["logits"][a:b].double()
+    order = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :k]
+    z = torch.log_softmax(x * beta, dim=1)
+    p = torch.exp(z)
+    entropy = -(p * z.clamp(min=-1e300)).sum(dim=1)
+    live = torch.ones(b - a, dtype=torch.bool, device=x.device) if s["targets"] is None else s["targets"][a:b] >= 0
+    n = torch.arange(b - a, device=x.device)
+    top = z[n[:, None], order]
+    out = []
+    if s["targets"] is not None:
+        y = s["targets"][a:b].clamp(min=0)
+        out.append(z[n, y].masked_fill(~live, 0.0))
+    out += [entropy.masked_fill(~live, 0.0), order.masked_fill(~live[:, None], -1), top.masked_fill(~live[:, None], 0.0)]
+    if case["op"] == "top_grad":
+        dlogp, dH, dtop = s["dlogp"][a:b].double(), s["dentropy"][a:b].double(), s["dtop"][a:b].double()
+        d = -p * (dlogp + dtop.sum(dim=1))[:, None] - dH[:, None] * p * (z.clamp(min=-1e300) + entropy[:, None])
+        for i in range(k):
+            d[n, order[:, i]] += dtop[:, i]
+        d[n, y] += dlogp
+        out.append((d * beta).masked_fill(~live[:, None], 0.0))
+    return out
+
+
+def _exact_distill(s, case, a, b):
+    beta, ce = 1.0 / case["temperature"], case["ce"]
+    z = torch.log_softmax(s["logits"][a:b].double() * beta, dim=1)
+    p = torch.exp(z)
+    live, y = s["targets"][a:b] >= 0, s["targets"][a:b].clamp(min=0)
+    n = torch.arange(b - a, device=z.device)
+    there, at = s["ids"][a:b] >= 0, s["ids"][a:b].clamp(min=0)
+    q = torch.zeros_like(p)
+    named = torch.zeros_like(p, dtype=torch.bool)
+    for i in range(case["k"]):
+        on = there[:, i]
+        q[n[on], at[on, i]] = torch.exp(s["tlogp"][a:b][on, i].double())
+        named[n[on], at[on, i]] = True
+    if case["renormalise"]:
+        q = q / q.sum(dim=1, keepdim=True)
+        left = torch.zeros(b - a, dtype=torch.float64, device=z.device)
+    else:
+        left = (1.0 - q.sum(dim=1)).clamp(min=0.0)
+    other = p.masked_fill(named, 0.0)
+    rest = other.sum(dim=1)
+    kl = torch.xlogy(q, q).sum(dim=1) - (q * z.clamp(min=-1e300)).sum(dim=1) + torch.xlogy(left, left) - left * torch.log(rest)
+    d = p * (q.sum(dim=1) + left + ce)[:, None] - q - other * (left / rest)[:, None]
+    d[n, y] -= ce
+    w = s["weights"][a:b].double() * live
+    kl = kl.masked_fill(~live, 0.0)
+    sums = torch.stack([(w * kl).sum(), -(w * z[n, y])[live].sum(), w.sum()])
+    return [torch.cat([sums[0:1] + ce * sums[1:2], sums]), kl, (d * (w * beta)[:, None]).masked_fill(~live[:, None], 0.0)]
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] in ("norm", "norm_grad"):
+        return _exact_norm(s, case)
+    T, V = s["logits"].shape
+    step = max(1, 2 ** 26 // V)
+    parts = [(_exact_distill if case["op"] == "distill" else _exact_top)(s, case, a, min(a + step, T)) for a in range(0, T, step)]
+    joined = [torch.cat(column) for column in zip(*parts)]
+    if case["op"] == "distill":
+        joined[0] = torch.stack([part[0] for part in parts]).sum(dim=0)
+    return joined
