@@ -340,7 +340,7 @@ def _run_own(s, case):
     if op == "norm":
         return out
     h = s["x"] if s["sum"] is None else s["sum"]
-    star.star_rms_norm_grad(s["dy"], h, s["gain"], s["rstd"], s["dx"], dresidual=s["dres"], dweight=s["dgain"])
+    star.star_rms_norm_grad(s["dy"], h, s["gain"], s["rstd"], s["dx"], dresidual=s["dres"], dgain=s["dgain"])
     return out + [s["dx"], s["dgain"]]
 
 
