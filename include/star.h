@@ -573,6 +573,70 @@ star_status star_preference_loss(const void *logits, star_dtype dtype, int64_t t
                                  int64_t ld_out, float *logp_out, float *margins_out, float *loss_out,
                                  void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/*
+ * What a model says beside the taken token: entropies and the k most likely words of every row, as a teacher reports them to a student, or a
+ * server to its caller.
+ *   targets     : device int64[tokens], or NULL: all rows count and no token is taken
+ *   k           : 0 to 128 alternatives
+ *   logp_out    : device float[tokens] or NULL (NULL without targets): log-probability of the taken token
+ *   entropy_out : device float[tokens] or NULL: -sum_j p_j log p_j, in nats
+ *   lse_out     : device float[tokens] or NULL, as of star_token_logprobs
+ *   top_ids     : device int64[tokens][k], the most likely words, the likeliest first, of equal logits the lowest id first
+ *   top_logp    : device float[tokens][k], their log-probabilities
+ * Words of probability 0 (logits of -inf) are no alternatives: where a row has fewer than k others the rest of its ids are -1 and their
+ * log-probabilities -inf.  A row without probabilities (NaN, +inf, nothing but -inf) has ids of -1 and NaN everywhere else, a row that does not count
+ * ids of -1 and 0.
+ */
+star_status star_top_logprobs(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
+                              const int64_t *targets, float temperature, int32_t k, float *logp_out,
+                              float *entropy_out, float *lse_out, int64_t *top_ids, float *top_logp, void *workspace,
+                              size_t workspace_bytes, void *hip_stream);
+
+/* The gradient of any function of them.  With D[t] = dlogp[t] + sum_i dtop[t][i] and H the entropy,
+ *     dlogits[t][j] = (dlogp[t] [j == targets[t]] + sum_i dtop[t][i] [j == top_ids[t][i]] - p[t][j] (D[t] + dentropy[t] (log p[t][j] + H[t]))) / temperature.
+ *   dlogp, dentropy : device float[tokens], or NULL: 0; dlogp needs targets
+ *   top_ids, dtop   : device int64[tokens][k], float[tokens][k], k from 0 to 128 (NULL for k == 0).  Any words in any order, the same one
+ *                     more than once too; an id outside [0, vocab) and its derivative do not count
+ */
+star_status star_top_logprobs_grad(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
+                                   const int64_t *targets, float temperature, const float *dlogp,
+                                   const float *dentropy, int32_t k, const int64_t *top_ids, const float *dtop,
+                                   void *dlogits, int64_t ld_out, void *hip_stream);
+
+/*
+ * Distillation loss on a teacher's alternatives, and its gradient.  Row t of the teacher names k words i with log-probabilities
+ * teacher_logp[t][i], as star_top_logprobs returns them (at the same temperature).  With q_i = exp(teacher_logp) its shares, p the student's, and the
+ * words not named taken together (q_r = max(0, 1 - sum q_i), p_r the sum of their p), token t costs
+ *     l_t = sum_i q_i log(q_i / p_i) + q_r log(q_r / p_r) - ce_coef log p[targets[t]]
+ * and loss = scale sum_t weights[t] l_t.  With renormalise nonzero the named words are the whole of the teacher: q_i is divided by their sum, and
+ * q_r is 0.
+ *   teacher_ids  : device int64[tokens][k], k from 1 to 128, in any order.  An id outside [0, vocab) names nothing; of a word that is named twice the
+ *                  first counts
+ *   teacher_logp : device float[tokens][k]; -inf: a share of 0
+ *   targets      : device int64[tokens], or NULL: all rows count (then ce_coef must be 0)
+ *   weights      : device float[tokens] or NULL (all 1); a token of weight 0 does not count
+ *   dlogits      : as above, or NULL: the loss alone
+ *   kl_out       : device float[tokens] or NULL: l_t without its last term; 0 for a token that does not count
+ *   stats_out    : device float[4]: loss, and sum_t scale weights[t] times the divergence (kl_out), times -log p[targets[t]] (0 without targets), times 1
+ * Where the student gives the words not named a probability of 0 (there are none, or all are banned), they are left out: q_r is taken as 0.  A word of
+ * the teacher's that the student bans costs infinity, and has a gradient all the same.  A teacher that names nothing costs 0.  The named words' numbers are
+ * formed in 64 bits, p_r from the words that are not named.
+ */
+typedef struct {
+    float scale;
+    float ce_coef;       /* >= 0        */
+    float temperature;   /* 1e-4 to 1e4 */
+    int32_t renormalise;
+} star_distill_params;
+
+star_status star_distill_loss(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
+                              const int64_t *targets, int32_t k, const int64_t *teacher_ids, const float *teacher_logp,
+                              const float *weights, const star_distill_params *params, void *dlogits, int64_t ld_out,
+                              float *kl_out, float *stats_out, void *workspace, size_t workspace_bytes,
+                              void *hip_stream);
+
+size_t star_top_logprobs_workspace(star_dtype dtype, int64_t tokens, int64_t vocab, int32_t k);
+size_t star_distill_loss_workspace(star_dtype dtype, int64_t tokens, int64_t vocab, int32_t k);
 size_t star_token_logprobs_workspace(star_dtype dtype, int64_t tokens, int64_t vocab);
 size_t star_policy_loss_workspace(star_dtype dtype, int64_t tokens, int64_t vocab);
 size_t star_preference_loss_workspace(star_dtype dtype, int64_t tokens, int64_t vocab, int32_t pairs);
@@ -611,6 +675,43 @@ star_status star_act_weight_grad(const void *dy, star_dtype dy_dtype, int64_t to
                                  void *workspace, size_t workspace_bytes, void *hip_stream);
 
 size_t star_act_weight_grad_workspace(star_dtype dy_dtype, int64_t tokens, int64_t out, int64_t width);
+
+/*
+ * Root-mean-square norm with the residual's addition, as it stands before a projection:
+ *     h = x + residual, rounded to its type,   rstd = 1 / sqrt(mean_j h_j^2 + eps),   y_j = h_j rstd gain_j
+ * for `tokens` rows (up to 2^30) of `width` values (1 to 32768); x, residual, sum_out and y are of one type, each with its own distance of rows.
+ *   residual : device, or NULL: h = x
+ *   gain     : device, `width` values of gain_dtype, or NULL: all 1 (a stretch of the parameters or of their copy)
+ *   eps      : positive and finite
+ *   sum_out  : h, needed with a residual (its gradient reads h), NULL without one; may be x or the residual
+ *   y        : may be x or the residual
+ *   rstd_out : device float[tokens] or NULL
+ *   packed   : NULL, or star_act_bytes(tokens, width) bytes: y as star_act_pack keeps it, for star_act_weight_grad
+ * "May be" means same address and same distance of rows; overlapping otherwise is not allowed.  The mean is taken in 64 bits.  A row that holds inf or
+ * NaN gives NaN.
+ */
+star_status star_rms_norm(const void *x, star_dtype dtype, int64_t tokens, int64_t width, int64_t ld,
+                          const void *residual, int64_t ld_residual, const void *gain, star_dtype gain_dtype, float eps,
+                          void *sum_out, int64_t ld_sum, void *y, int64_t ld_y, float *rstd_out, void *packed,
+                          void *hip_stream);
+
+/*
+ * Its gradient.  With h' = h rstd,
+ *     dx_j = rstd (gain_j dy_j - h'_j mean_i(gain_i dy_i h'_i)) + dresidual_j,    dgain_j = sum_t dy[t][j] h'[t][j]
+ * (accumulate nonzero: dgain is added to what it holds).  dx is the gradient of x and of the residual.
+ *   dy, h, dresidual, dx : device, `tokens` rows of `width` values of one type; h as the norm took it (sum_out, or x); dresidual, the gradient that
+ *            comes to h past the norm, may be NULL; dx may be dy, h or dresidual (same address and distance of rows)
+ *   rstd   : device float[tokens], from star_rms_norm
+ *   dgain  : device, `width` values of dgain_dtype, contiguous -- a stretch of a worker's gradient row -- or NULL.  Sums over the tokens are taken
+ *            in fp32 by a workgroup, over the workgroups in 64 bits, in a fixed order
+ */
+star_status star_rms_norm_grad(const void *dy, star_dtype dtype, int64_t tokens, int64_t width, int64_t ld_dy,
+                               const void *h, int64_t ld_h, const void *gain, star_dtype gain_dtype, const float *rstd,
+                               const void *dresidual, int64_t ld_dresidual, void *dx, int64_t ld_dx, void *dgain,
+                               star_dtype dgain_dtype, int32_t accumulate, void *workspace, size_t workspace_bytes,
+                               void *hip_stream);
+
+size_t star_rms_norm_grad_workspace(star_dtype dtype, int64_t tokens, int64_t width);
 
 /* Bytes of internal device workspace one call of this shape uses at most (direct norm sums without an update need the
  * most: partial sums of up to 240 updates). */

@@ -13,6 +13,6 @@ from .binding import (  # noqa: F401
     star_version, star_workspace_bytes,
 )
 from .worker import (  # noqa: F401
-    star_act_bytes, star_act_pack, star_act_unpack, star_act_weight_grad, star_policy_loss, star_preference_loss,
-    star_token_logprobs, star_token_logprobs_grad,
+    star_act_bytes, star_act_pack, star_act_unpack, star_act_weight_grad, star_distill_loss, star_policy_loss, star_preference_loss,
+    star_rms_norm, star_rms_norm_grad, star_token_logprobs, star_token_logprobs_grad, star_top_logprobs, star_top_logprobs_grad,
 )

@@ -71,6 +71,51 @@ hipError_t launch_pairs(const Logits& l, const PreferenceArgs& a, const PairOffs
                         const float* logp_low, float* dlogp, float* margins, double* terms, hipStream_t stream);
 hipError_t launch_pair_loss(const PairLoss& loss, hipStream_t stream);
 
+// ---------------------------------------------------------------- named words of a row
+constexpr int kMostAlternatives = 128;
+
+// logp, entropy, lse (each may be null) of all rows and their k most likely words.
+hipError_t launch_top(const Logits& l, int k, float* logp, float* entropy, float* lse, int64_t* ids, float* top, hipStream_t stream);
+
+// k words a row: their ids [tokens][k] and, of a teacher, log-probabilities.
+struct ListedWords {
+    const int64_t* ids;
+    const float* logp;
+    int k;
+};
+struct DistillArgs {
+    float scale, ce;
+    bool renormalise;
+};
+size_t distill_workspace(int64_t tokens);
+// kl, dlogits may be null.
+hipError_t launch_distill(const Logits& l, const ListedWords& words, const DistillArgs& d, void* dlogits, int64_t ld_out, float* kl, float* stats,
+                          void* workspace, hipStream_t stream);
+// dlogits from the derivatives by the taken tokens' log-probabilities, the entropies and the words' log-probabilities [tokens][k]; each may be null.
+hipError_t launch_top_grad(const Logits& l, const ListedWords& words, const float* dlogp, const float* dentropy, const float* dtop, void* dlogits,
+                           int64_t ld_out, hipStream_t stream);
+
+// ---------------------------------------------------------------- root-mean-square norm
+constexpr int64_t kMostNormWidth = 32768;
+
+// Rows of one tensor, `ld` elements apart; x may be null.
+struct Rows {
+    const void* x;
+    int64_t ld;
+};
+struct Norm {
+    int dtype;
+    int64_t tokens, width;
+    const void* gain;      // null: all 1
+    int gain_dtype;
+};
+hipError_t launch_norm(const Norm& n, const Rows& x, const Rows& residual, float eps, void* sum, int64_t ld_sum, void* y, int64_t ld_y, float* rstd,
+                       hipStream_t stream);
+// Workgroups that each leave sums of the gain's gradient in the workspace.
+int norm_grad_groups(int dtype, int64_t tokens, int64_t width);
+hipError_t launch_norm_grad(const Norm& n, const Rows& dy, const Rows& h, const float* rstd, const Rows& dresidual, void* dx, int64_t ld_dx, void* dgain,
+                            int dgain_dtype, bool accumulate, void* workspace, hipStream_t stream);
+
 // ---------------------------------------------------------------- saved activations
 constexpr int kActBlock = 32;    // tokens that share a scale
 constexpr int kActPad = 16;      // columns of the packed form come in multiples of this

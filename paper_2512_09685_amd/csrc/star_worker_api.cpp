@@ -44,7 +44,7 @@ star_status check_workspace(const void* workspace, size_t have, size_t need) {
 
 // The checks that all calls on logits share.
 star_status check_logits(const void* logits, int dtype, int64_t tokens, int64_t vocab, int64_t ld, const int64_t* targets, float temperature,
-                         const void* dlogits, int64_t ld_out) {
+                         const void* dlogits, int64_t ld_out, bool all_rows = false) {   // all_rows: targets may be NULL
     if (!known(dtype)) return set_error(STAR_ERR_DTYPE, "unknown dtype of the logits");
     if (tokens < 0 || tokens > kMostRows) return set_error(STAR_ERR_SHAPE, "tokens is negative or above 2^22");
     if (vocab < 1 || vocab > kMostVocab) return set_error(STAR_ERR_SHAPE, "vocab is below 1 or above 2^30");
@@ -52,7 +52,7 @@ star_status check_logits(const void* logits, int dtype, int64_t tokens, int64_t 
     if (dlogits && !rows_fit(tokens, vocab, ld_out)) return set_error(STAR_ERR_SHAPE, "ld_out is below vocab, or the gradient is too large");
     if (!(temperature >= 1e-4f && temperature <= 1e4f)) return set_error(STAR_ERR_HPARAM, "temperature must lie in 1e-4 to 1e4");
     if (tokens == 0) return STAR_OK;
-    if (!logits || !targets) return set_error(STAR_ERR_NULL, "logits or targets is NULL");
+    if (!logits || (!targets && !all_rows)) return set_error(STAR_ERR_NULL, "logits or targets is NULL");
     if (!on_grid(logits, bytes_of(dtype)) || !on_grid(dlogits, bytes_of(dtype)) || !on_grid(targets, 8))
         return set_error(STAR_ERR_SHAPE, "an address is not a multiple of its element's size");
     if (dlogits == logits && dlogits && ld != ld_out) return set_error(STAR_ERR_SHAPE, "a gradient in place needs ld_out == ld");
@@ -218,6 +218,146 @@ star_status star_preference_loss(const void* logits, star_dtype dtype, int64_t t
         joined = dlogits && last;
     }
     if (!joined) STAR_LAUNCH(star::launch_pair_loss(loss, stream));
+    return STAR_OK;
+}
+
+// Words named by a row: k a row, their ids and one float each.
+static star_status check_words(int32_t k, int32_t least, const int64_t* ids, const float* numbers, int64_t tokens) {
+    if (k < least || k > star::kMostAlternatives) return set_error(STAR_ERR_SHAPE, least ? "k must lie in 1 to 128" : "k must lie in 0 to 128");
+    if (tokens == 0 || k == 0) return STAR_OK;
+    if (!ids || !numbers) return set_error(STAR_ERR_NULL, "the words' ids or numbers are NULL");
+    if (!on_grid(ids, 8) || !on_grid(numbers, 4)) return set_error(STAR_ERR_SHAPE, "an address is not a multiple of its element's size");
+    return STAR_OK;
+}
+
+size_t star_top_logprobs_workspace(star_dtype, int64_t, int64_t, int32_t) { return 0; }
+
+star_status star_top_logprobs(const void* logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld, const int64_t* targets,
+                              float temperature, int32_t k, float* logp_out, float* entropy_out, float* lse_out, int64_t* top_ids,
+                              float* top_logp, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    set_error(STAR_OK, "");
+    STAR_CHECK(check_logits(logits, dtype, tokens, vocab, ld, targets, temperature, nullptr, 0, true));
+    STAR_CHECK(check_words(k, 0, top_ids, top_logp, tokens));
+    if (logp_out && !targets && tokens > 0) return set_error(STAR_ERR_NULL, "logp_out without targets");
+    if (over(logp_out, entropy_out, tokens) || over(logp_out, lse_out, tokens) || over(entropy_out, lse_out, tokens))
+        return set_error(STAR_ERR_SHAPE, "two outputs overlap");
+    if (tokens == 0) return STAR_OK;
+    STAR_CHECK(check_workspace(workspace, workspace_bytes, star_top_logprobs_workspace(dtype, tokens, vocab, k)));
+    const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, nullptr, temperature);
+    STAR_LAUNCH(star::launch_top(l, k, logp_out, entropy_out, lse_out, top_ids, top_logp, static_cast<hipStream_t>(hip_stream)));
+    return STAR_OK;
+}
+
+star_status star_top_logprobs_grad(const void* logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld, const int64_t* targets,
+                                   float temperature, const float* dlogp, const float* dentropy, int32_t k, const int64_t* top_ids,
+                                   const float* dtop, void* dlogits, int64_t ld_out, void* hip_stream) {
+    set_error(STAR_OK, "");
+    STAR_CHECK(check_logits(logits, dtype, tokens, vocab, ld, targets, temperature, dlogits, ld_out, true));
+    STAR_CHECK(check_words(k, 0, top_ids, dtop, tokens));
+    if (tokens == 0) return STAR_OK;
+    if (!dlogits) return set_error(STAR_ERR_NULL, "dlogits is NULL");
+    if (dlogp && !targets) return set_error(STAR_ERR_NULL, "dlogp without targets");
+    const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, nullptr, temperature);
+    STAR_LAUNCH(star::launch_top_grad(l, star::ListedWords{top_ids, nullptr, k}, dlogp, dentropy, dtop, dlogits, ld_out,
+                                      static_cast<hipStream_t>(hip_stream)));
+    return STAR_OK;
+}
+
+size_t star_distill_loss_workspace(star_dtype dtype, int64_t tokens, int64_t vocab, int32_t) {
+    return tokens == 0 || logits_fit(dtype, tokens, vocab) ? star::distill_workspace(tokens) : 0;
+}
+
+star_status star_distill_loss(const void* logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld, const int64_t* targets, int32_t k,
+                              const int64_t* teacher_ids, const float* teacher_logp, const float* weights, const star_distill_params* params,
+                              void* dlogits, int64_t ld_out, float* kl_out, float* stats_out, void* workspace, size_t workspace_bytes,
+                              void* hip_stream) {
+    set_error(STAR_OK, "");
+    if (!params) return set_error(STAR_ERR_NULL, "params is NULL");
+    if (!std::isfinite(params->scale)) return set_error(STAR_ERR_HPARAM, "scale must be finite");
+    if (!(params->ce_coef >= 0.f) || !std::isfinite(params->ce_coef)) return set_error(STAR_ERR_HPARAM, "ce_coef must be finite and not negative");
+    STAR_CHECK(check_logits(logits, dtype, tokens, vocab, ld, targets, params->temperature, dlogits, ld_out, true));
+    STAR_CHECK(check_words(k, 1, teacher_ids, teacher_logp, tokens));
+    if (!stats_out) return set_error(STAR_ERR_NULL, "stats_out is NULL");
+    if (tokens > 0 && params->ce_coef != 0.f && !targets) return set_error(STAR_ERR_NULL, "ce_coef is not 0 and targets is NULL");
+    if (over(kl_out, weights, tokens)) return set_error(STAR_ERR_SHAPE, "kl_out overlaps an input");
+    STAR_CHECK(check_workspace(workspace, workspace_bytes, star_distill_loss_workspace(dtype, tokens, vocab, k)));
+    const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, weights, params->temperature);
+    const star::DistillArgs d{params->scale, params->ce_coef, params->renormalise != 0};
+    STAR_LAUNCH(star::launch_distill(l, star::ListedWords{teacher_ids, teacher_logp, k}, d, dlogits, ld_out, kl_out, stats_out, workspace,
+                                     static_cast<hipStream_t>(hip_stream)));
+    return STAR_OK;
+}
+
+// Rows of a norm's tensor.
+static star_status check_norm_rows(const void* x, int dtype, int64_t tokens, int64_t width, int64_t ld) {
+    if (!rows_fit(tokens, width, ld)) return set_error(STAR_ERR_SHAPE, "a size is negative, a distance of rows is below width, or a tensor is too large");
+    if (!x) return set_error(STAR_ERR_NULL, "a tensor is NULL");
+    if (!on_grid(x, bytes_of(dtype))) return set_error(STAR_ERR_SHAPE, "an address is not a multiple of its element's size");
+    return STAR_OK;
+}
+static star_status check_norm(int dtype, int64_t tokens, int64_t width, const void* gain, int gain_dtype) {
+    if (!known(dtype)) return set_error(STAR_ERR_DTYPE, "unknown dtype of the rows");
+    if (gain && !known(gain_dtype)) return set_error(STAR_ERR_DTYPE, "unknown dtype of the gain");
+    if (tokens < 0 || tokens > kMostSummed) return set_error(STAR_ERR_SHAPE, "tokens is negative or above 2^30");
+    if (width < 1 || width > star::kMostNormWidth) return set_error(STAR_ERR_SHAPE, "width is below 1 or above 32768");
+    if (gain && !on_grid(gain, bytes_of(gain_dtype))) return set_error(STAR_ERR_SHAPE, "an address is not a multiple of its element's size");
+    return STAR_OK;
+}
+// Whether an output over an input lies otherwise than in its place.
+static bool askew(const void* out, int64_t ld_out, const void* in, int64_t ld) { return out == in && ld_out != ld; }
+
+star_status star_rms_norm(const void* x, star_dtype dtype, int64_t tokens, int64_t width, int64_t ld, const void* residual, int64_t ld_residual,
+                          const void* gain, star_dtype gain_dtype, float eps, void* sum_out, int64_t ld_sum, void* y, int64_t ld_y,
+                          float* rstd_out, void* packed, void* hip_stream) {
+    set_error(STAR_OK, "");
+    STAR_CHECK(check_norm(dtype, tokens, width, gain, gain_dtype));
+    if (!(eps > 0.f) || !std::isfinite(eps)) return set_error(STAR_ERR_HPARAM, "eps must be positive and finite");
+    if (tokens == 0) return STAR_OK;
+    STAR_CHECK(check_norm_rows(x, dtype, tokens, width, ld));
+    STAR_CHECK(check_norm_rows(y, dtype, tokens, width, ld_y));
+    if (!residual != !sum_out) return set_error(STAR_ERR_NULL, "residual and sum_out go together");
+    if (residual) {
+        STAR_CHECK(check_norm_rows(residual, dtype, tokens, width, ld_residual));
+        STAR_CHECK(check_norm_rows(sum_out, dtype, tokens, width, ld_sum));
+        if (sum_out == y) return set_error(STAR_ERR_SHAPE, "two outputs overlap");
+        if (askew(sum_out, ld_sum, x, ld) || askew(sum_out, ld_sum, residual, ld_residual) || askew(y, ld_y, residual, ld_residual))
+            return set_error(STAR_ERR_SHAPE, "an output in an input's place needs its distance of rows");
+    }
+    if (askew(y, ld_y, x, ld)) return set_error(STAR_ERR_SHAPE, "an output in an input's place needs its distance of rows");
+    if (packed && !on_grid(packed, 16)) return set_error(STAR_ERR_SHAPE, "packed is not aligned to 16 bytes");
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    STAR_LAUNCH(star::launch_norm(star::Norm{dtype, tokens, width, gain, gain_dtype}, star::Rows{x, ld}, star::Rows{residual, ld_residual}, eps,
+                                  sum_out, ld_sum, y, ld_y, rstd_out, stream));
+    if (packed) STAR_LAUNCH(star::launch_act_pack(y, dtype, tokens, width, ld_y, packed, stream));
+    return STAR_OK;
+}
+
+size_t star_rms_norm_grad_workspace(star_dtype dtype, int64_t tokens, int64_t width) {
+    if (!known(dtype) || tokens <= 0 || tokens > kMostSummed || width < 1 || width > star::kMostNormWidth) return 0;
+    return round16(sizeof(float) * (size_t)width * (size_t)star::norm_grad_groups(dtype, tokens, width));
+}
+
+star_status star_rms_norm_grad(const void* dy, star_dtype dtype, int64_t tokens, int64_t width, int64_t ld_dy, const void* h, int64_t ld_h,
+                               const void* gain, star_dtype gain_dtype, const float* rstd, const void* dresidual, int64_t ld_dresidual, void* dx,
+                               int64_t ld_dx, void* dgain, star_dtype dgain_dtype, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                               void* hip_stream) {
+    set_error(STAR_OK, "");
+    STAR_CHECK(check_norm(dtype, tokens, width, gain, gain_dtype));
+    if (dgain && !known(dgain_dtype)) return set_error(STAR_ERR_DTYPE, "unknown dtype of dgain");
+    if (dgain && !on_grid(dgain, bytes_of(dgain_dtype))) return set_error(STAR_ERR_SHAPE, "an address is not a multiple of its element's size");
+    if (tokens > 0) {
+        STAR_CHECK(check_norm_rows(dy, dtype, tokens, width, ld_dy));
+        STAR_CHECK(check_norm_rows(h, dtype, tokens, width, ld_h));
+        STAR_CHECK(check_norm_rows(dx, dtype, tokens, width, ld_dx));
+        if (dresidual) STAR_CHECK(check_norm_rows(dresidual, dtype, tokens, width, ld_dresidual));
+        if (!rstd) return set_error(STAR_ERR_NULL, "rstd is NULL");
+        if (askew(dx, ld_dx, dy, ld_dy) || askew(dx, ld_dx, h, ld_h) || askew(dx, ld_dx, dresidual, ld_dresidual))
+            return set_error(STAR_ERR_SHAPE, "an output in an input's place needs its distance of rows");
+        if (dgain) STAR_CHECK(check_workspace(workspace, workspace_bytes, star_rms_norm_grad_workspace(dtype, tokens, width)));
+    }
+    STAR_LAUNCH(star::launch_norm_grad(star::Norm{dtype, tokens, width, gain, gain_dtype}, star::Rows{dy, ld_dy}, star::Rows{h, ld_h}, rstd,
+                                       star::Rows{dresidual, ld_dresidual}, dx, ld_dx, dgain, dgain_dtype, accumulate != 0, workspace,
+                                       static_cast<hipStream_t>(hip_stream)));
     return STAR_OK;
 }
 

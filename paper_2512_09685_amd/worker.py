@@ -1,5 +1,5 @@
-"""Binding of the worker-side entry points of libstar.so: losses on logits with their gradients, activations kept in 8
-bits and the weight gradient formed from them.  Argument marshalling only, as in ``binding``; outputs are tensors that the
+"""Binding of the worker-side entry points of libstar.so: losses on logits with their gradients, a teacher's alternatives and
+the loss on them, the root-mean-square norm, activations kept in 8 bits and the weight gradient formed from them.  Argument marshalling only, as in ``binding``; outputs are tensors that the
 caller hands in.  A workspace, where a call needs one, is taken from torch's allocator on the call's stream, or
 passed in (a uint8 tensor of at least the bytes the C header's ``*_workspace`` function returns)."""
 from __future__ import annotations
@@ -26,6 +26,11 @@ class _PreferenceParams(ctypes.Structure):
                 ("temperature", ctypes.c_float)]
 
 
+class _DistillParams(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("ce_coef", ctypes.c_float), ("temperature", ctypes.c_float),
+                ("renormalise", ctypes.c_int32)]
+
+
 def _library():
     global _lib
     if _lib is None:
@@ -41,6 +46,14 @@ def _library():
             "star_token_logprobs_workspace": (size, [st, i64, i64]),
             "star_policy_loss_workspace": (size, [st, i64, i64]),
             "star_preference_loss_workspace": (size, [st, i64, i64, i32]),
+            "star_top_logprobs": (st, logits + [f32, i32, vp, vp, vp, vp, vp, vp, size, vp]),
+            "star_top_logprobs_workspace": (size, [st, i64, i64, i32]),
+            "star_top_logprobs_grad": (st, logits + [f32, vp, vp, i32, vp, vp, vp, i64, vp]),
+            "star_distill_loss": (st, logits + [i32, vp, vp, vp, vp, vp, i64, vp, vp, vp, size, vp]),
+            "star_distill_loss_workspace": (size, [st, i64, i64, i32]),
+            "star_rms_norm": (st, [vp, st, i64, i64, i64, vp, i64, vp, st, f32, vp, i64, vp, i64, vp, vp, vp]),
+            "star_rms_norm_grad": (st, [vp, st, i64, i64, i64, vp, i64, vp, st, vp, vp, i64, vp, i64, vp, st, i32, vp, size, vp]),
+            "star_rms_norm_grad_workspace": (size, [st, i64, i64]),
             "star_act_bytes": (size, [i64, i64]),
             "star_act_pack": (st, [vp, st, i64, i64, i64, vp, vp]),
             "star_act_unpack": (st, [vp, i64, i64, vp, st, i64, vp]),
@@ -106,7 +119,7 @@ def _vector(x, dtype, n: int, what: str, device: int):
 
 def _logits(logits, targets, dlogits=None):
     """What every call on logits begins with: (address, dtype code, tokens, vocab, ld, targets), its gradient's (address,
-    ld), and the device's index."""
+    ld), and the device's index.  Where targets may be None, the caller has said so."""
     code = _dtype(logits, "logits")
     x, tokens, vocab, ld = _matrix(logits, "logits")
     device = logits.get_device()
@@ -116,6 +129,27 @@ def _logits(logits, targets, dlogits=None):
             raise TypeError("dlogits must have the logits' type and device")
         out, _, _, ld_out = _matrix(dlogits, "dlogits", tokens, vocab)
     return (x, code, tokens, vocab, ld, _vector(targets, _i64, tokens, "targets", device)), (out, ld_out), device
+
+
+def _words(ids, numbers, tokens: int, what: str, device: int):
+    """(k, addresses) of words named by a row and a number for each: contiguous int64 and float32 [tokens, k]."""
+    if ids is None and numbers is None:
+        return 0, None, None
+    if ids is None or numbers is None:
+        raise ValueError(f"{what} go together")
+    for x, dtype in ((ids, _i64), (numbers, _f32)):
+        if x.dtype is not dtype or x.dim() != 2 or x.size(0) != tokens or x.size(1) != ids.size(1) or not x.is_contiguous():
+            raise ValueError(f"{what} must be contiguous int64 and float32 tensors [{tokens}, k]")
+        if x.get_device() != device:
+            raise ValueError(f"{what} must be on the logits' device")
+    return ids.size(1), ids.data_ptr(), numbers.data_ptr()
+
+
+def _on_this_gpu(device: int, stream):
+    """As _on_gpu; a call without a stream goes to the current device's, which must be the tensors'."""
+    _on_gpu(device)
+    if stream is None and device != _torch.cuda.current_device():
+        raise ValueError(f"the tensors are on device {device}, which is not the current one")
 
 
 def _on_gpu(device: int):
@@ -215,6 +249,120 @@ def star_preference_loss(logits, targets, ref_logp, offsets, loss_out, *, dlogit
     w, size, _keep = _workspace(workspace, _need("star_preference_loss_workspace", *head[1:4], pairs), device, stream)
     _check(lib.star_preference_loss(*head, ref, wts, pairs, at.ctypes.data, ctypes.byref(p), *out, logp, margins, loss, w,
                                     size, _stream_handle(stream)))
+
+
+def star_top_logprobs(logits, targets, logp_out, *, entropy_out=None, lse_out=None, top_ids=None, top_logp=None,
+                      temperature: float = 1.0, workspace=None, stream=None) -> None:
+    """Entropies (float32 [tokens], nats) and the k most likely words of every row: ``top_ids`` int64 [tokens, k], k up to 128, the
+    likeliest first, of equal logits the lowest id first, and ``top_logp`` float32 [tokens, k].  ``logp_out`` and ``lse_out`` as of
+    ``star_token_logprobs``.  ``targets`` None: all rows count, and ``logp_out`` is None.  Rows that do not count have ids of
+    -1 and 0 elsewhere; words of probability 0 are no alternatives (ids of -1, log-probabilities of -inf in their place)."""
+    lib = _library()
+    head, _, device = _logits(logits, targets)
+    tokens = head[2]
+    logp, lse = _vector(logp_out, _f32, tokens, "logp_out", device), _vector(lse_out, _f32, tokens, "lse_out", device)
+    entropy = _vector(entropy_out, _f32, tokens, "entropy_out", device)
+    k, ids, top = _words(top_ids, top_logp, tokens, "top_ids and top_logp", device)
+    if logp is not None and targets is None:
+        raise StarError(_ERR_NULL, "logp_out without targets")
+    _on_this_gpu(device, stream)
+    w, size, _keep = _workspace(workspace, _need("star_top_logprobs_workspace", *head[1:4], k), device, stream)
+    _check(lib.star_top_logprobs(*head, temperature, k, logp, entropy, lse, ids, top, w, size, _stream_handle(stream)))
+
+
+def star_top_logprobs_grad(logits, targets, dlogits, *, dlogp=None, dentropy=None, top_ids=None, dtop=None,
+                           temperature: float = 1.0, stream=None) -> None:
+    """``dlogits`` of a function whose derivatives are ``dlogp`` (by the taken tokens' log-probabilities) and ``dentropy``, float32
+    [tokens], and ``dtop`` (by the log-probabilities of the words ``top_ids``), float32 [tokens, k]; each may be None.  Any words
+    in any order; one outside the vocabulary does not count.  ``dlogits`` may be ``logits``."""
+    lib = _library()
+    head, out, device = _logits(logits, targets, dlogits)
+    tokens = head[2]
+    slope, certain = _vector(dlogp, _f32, tokens, "dlogp", device), _vector(dentropy, _f32, tokens, "dentropy", device)
+    k, ids, top = _words(top_ids, dtop, tokens, "top_ids and dtop", device)
+    if slope is not None and targets is None:
+        raise StarError(_ERR_NULL, "dlogp without targets")
+    _on_this_gpu(device, stream)
+    _check(lib.star_top_logprobs_grad(*head, temperature, slope, certain, k, ids, top, *out, _stream_handle(stream)))
+
+
+def star_distill_loss(logits, teacher_ids, teacher_logp, stats_out, *, targets=None, dlogits=None, weights=None,
+                      scale: Optional[float] = None, ce_coef: float = 0.0, renormalise: bool = False, temperature: float = 1.0,
+                      kl_out=None, workspace=None, stream=None) -> None:
+    """Divergence of the student's ``logits`` from a teacher's alternatives (``teacher_ids`` int64 [tokens, k], ``teacher_logp``
+    float32 [tokens, k], k up to 128, as ``star_top_logprobs`` gives them), the words not named taken together, or, with
+    ``renormalise``, the named ones as the whole of the teacher; and, if ``dlogits`` is given, the gradient.  ``ce_coef`` adds
+    -log p of the ``targets``.  ``stats_out``: float32 [4]: loss, divergence, -log p, weight, each summed with ``scale *
+    weights``.  ``kl_out``: float32 [tokens].  ``scale``: None = 1 / tokens."""
+    lib = _library()
+    head, out, device = _logits(logits, targets, dlogits)
+    n = head[2]
+    p = _DistillParams(1.0 / max(n, 1) if scale is None else scale, ce_coef, temperature, int(bool(renormalise)))
+    k, ids, teacher = _words(teacher_ids, teacher_logp, n, "teacher_ids and teacher_logp", device)
+    wts, kl = _vector(weights, _f32, n, "weights", device), _vector(kl_out, _f32, n, "kl_out", device)
+    stats = _vector(stats_out, _f32, 4, "stats_out", device)
+    if ce_coef and targets is None:
+        raise StarError(_ERR_NULL, "ce_coef is not 0 and targets is NULL")
+    _on_this_gpu(device, stream)
+    w, size, _keep = _workspace(workspace, _need("star_distill_loss_workspace", *head[1:4], k), device, stream)
+    _check(lib.star_distill_loss(*head, k, ids, teacher, wts, ctypes.byref(p), *out, kl, stats, w, size, _stream_handle(stream)))
+
+
+def _same_rows(x, like, what: str, rows: int, columns: int):
+    """(address, distance of the rows) of a tensor like another, or (None, 0)."""
+    if x is None:
+        return None, 0
+    if x.dtype is not like.dtype or x.get_device() != like.get_device():
+        raise TypeError(f"{what} must have the first tensor's type and device")
+    p, _, _, ld = _matrix(x, what, rows, columns)
+    return p, ld
+
+
+def _gain(gain, width: int, what: str, device: int):
+    """(address, dtype code) of a contiguous vector of the norm's width."""
+    if gain is None:
+        return None, F32
+    code = _dtype(gain, what)
+    return _vector(gain, gain.dtype, width, what, device), code
+
+
+def star_rms_norm(x, gain, out, *, residual=None, sum_out=None, rstd_out=None, packed=None, eps: float = 1e-6, stream=None) -> None:
+    """``out`` = h / sqrt(mean(h^2) + eps) * gain for every row of h = x + residual, which goes to ``sum_out`` (or of x, without a
+    residual).  ``x``, ``residual``, ``sum_out``, ``out``: float32 or bfloat16 [tokens, width], rows at any distance; ``out`` and
+    ``sum_out`` may be ``x`` or ``residual``.  ``gain``: float32 or bfloat16 [width], or None.  ``rstd_out``: float32 [tokens], for the
+    gradient.  ``packed``: as for ``star_act_pack``: ``out`` kept in 8 bits."""
+    lib = _library()
+    code = _dtype(x, "x")
+    p, tokens, width, ld = _matrix(x, "x")
+    device = x.get_device()
+    add, total, y = (_same_rows(v, x, name, tokens, width) for v, name in ((residual, "residual"), (sum_out, "sum_out"), (out, "out")))
+    if (residual is None) != (sum_out is None):
+        raise StarError(_ERR_NULL, "residual and sum_out go together")
+    g, g_code = _gain(gain, width, "gain", device)
+    rstd = _vector(rstd_out, _f32, tokens, "rstd_out", device)
+    keep = None if packed is None else _packed(packed, tokens, width, device)
+    _on_this_gpu(device, stream)
+    _check(lib.star_rms_norm(p, code, tokens, width, ld, *add, g, g_code, eps, *total, *y, rstd, keep, _stream_handle(stream)))
+
+
+def star_rms_norm_grad(dy, h, gain, rstd, dx, *, dresidual=None, dgain=None, accumulate: bool = False, workspace=None,
+                       stream=None) -> None:
+    """``dx`` = the gradient of ``star_rms_norm``'s x and residual for the gradient ``dy`` of its output, ``dresidual`` added;
+    ``dgain`` = (or, with ``accumulate``, +=) that of its gain, for example ``row[a:a + width]`` of a worker's gradient row.  ``h``: the
+    norm's ``sum_out`` (``x`` without a residual), ``rstd`` its ``rstd_out``.  ``dx`` may be ``dy``, ``h`` or ``dresidual``."""
+    lib = _library()
+    code = _dtype(dy, "dy")
+    p, tokens, width, ld = _matrix(dy, "dy")
+    device = dy.get_device()
+    taken, more, to = (_same_rows(v, dy, name, tokens, width) for v, name in ((h, "h"), (dresidual, "dresidual"), (dx, "dx")))
+    g, g_code = _gain(gain, width, "gain", device)
+    dg, dg_code = _gain(dgain, width, "dgain", device)
+    r = _vector(rstd, _f32, tokens, "rstd", device)
+    _on_this_gpu(device, stream)
+    need = 0 if dgain is None else _need("star_rms_norm_grad_workspace", code, tokens, width)
+    w, size, _keep = _workspace(workspace, need, device, stream)
+    _check(lib.star_rms_norm_grad(p, code, tokens, width, ld, *taken, g, g_code, r, *more, *to, dg, dg_code, int(bool(accumulate)), w, size,
+                                  _stream_handle(stream)))
 
 
 def star_act_bytes(tokens: int, width: int) -> int:
