@@ -112,31 +112,6 @@ struct LeftOut {
     }
 };
 
-// Maximum, sum, and (where asked) sum of e_j x_j of what a thread has seen.
-struct Seen {
-    float m, s, w;
-};
-template <bool ENTROPY>
-__device__ __forceinline__ void see_max(Seen& a, float m, float k) {
-    const float base = m == -INFINITY ? 0.f : m, x = (a.m - base) * k, f = __builtin_amdgcn_exp2f(x);
-    if (ENTROPY) a.w = a.s == 0.f ? 0.f : (a.w + a.s * x) * f;
-    a.s *= f;
-    a.m = m;
-}
-template <bool ENTROPY>
-__device__ __forceinline__ void see(Seen& a, float l, float k) {   // a.m is no less
-    const float x = (l - (a.m == -INFINITY ? 0.f : a.m)) * k, e = __builtin_amdgcn_exp2f(x);
-    a.s += e;
-    if (ENTROPY) a.w = __builtin_fmaf(e, fmaxf(x, -1e30f), a.w);   // (0 of a value of -inf; NaN comes through e)
-}
-template <class E, bool ENTROPY, int C>
-__device__ __forceinline__ void see_chunks(Seen& a, u32x4 (&x)[C], float k) {
-    see_max<ENTROPY>(a, max_of<E>(x, a.m), k);
-    static_for<0, C>([&](auto I) {
-        static_for<0, E::VEC>([&](auto J) { see<ENTROPY>(a, E::template get<decltype(J)::value>(x[decltype(I)::value]), k); });
-    });
-}
-
 // Dense part of the gradient: e (a - b (x - mean)), with x = (l - m) k and e = 2^x.
 struct Dense {
     float m, k, a, b, mean;
@@ -144,7 +119,7 @@ struct Dense {
     __device__ __forceinline__ float of(float l) const {
         const float x = (l - m) * k, e = __builtin_amdgcn_exp2f(x);
         if (!ENTROPY) return e * a;
-        return e * (a - b * (fmaxf(x, -1e30f) - mean));
+        return e * (a - b * (fmaxf(x, kNoExponent) - mean));
     }
 };
 template <class E, int NT, bool ENTROPY, int C>

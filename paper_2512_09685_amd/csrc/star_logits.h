@@ -232,6 +232,34 @@ __device__ __forceinline__ float fold_row(float x, float* shared, Op&& op) {
     return fold_wave<NT / 64>(shared[threadIdx.x % (NT / 64)], op);
 }
 
+// 2^x is 0 from here on down; products of it with x are formed with no less, so that they are 0 too.
+constexpr float kNoExponent = -1e4f;
+
+// Maximum, sum, and (where asked) sum of e_j x_j of what a thread has seen.
+struct Seen {
+    float m, s, w;
+};
+template <bool ENTROPY>
+__device__ __forceinline__ void see_max(Seen& a, float m, float k) {
+    const float base = m == -INFINITY ? 0.f : m, x = (a.m - base) * k, f = __builtin_amdgcn_exp2f(x);
+    if (ENTROPY) a.w = (a.w + a.s * fmaxf(x, kNoExponent)) * f;
+    a.s *= f;
+    a.m = m;
+}
+template <bool ENTROPY>
+__device__ __forceinline__ void see(Seen& a, float l, float k) {   // a.m is no less
+    const float x = (l - (a.m == -INFINITY ? 0.f : a.m)) * k, e = __builtin_amdgcn_exp2f(x);
+    a.s += e;
+    if (ENTROPY) a.w = __builtin_fmaf(e, fmaxf(x, kNoExponent), a.w);   // (0 of a value of -inf; NaN comes through e)
+}
+template <class E, bool ENTROPY, int C>
+__device__ __forceinline__ void see_chunks(Seen& a, u32x4 (&x)[C], float k) {
+    see_max<ENTROPY>(a, max_of<E>(x, a.m), k);
+    static_for<0, C>([&](auto I) {
+        static_for<0, E::VEC>([&](auto J) { see<ENTROPY>(a, E::template get<decltype(J)::value>(x[decltype(I)::value]), k); });
+    });
+}
+
 // Workgroups go round the 8 dies; this gives each die a run of long rows of its own (8192 x 65536, bf16: 4 % faster, 16384 x
 // 32768: 7 %; rows of 16 KB and less are up to 5 % slower that way and stay in the order of the workgroups, as do rows whose number is no
 // multiple of 8).

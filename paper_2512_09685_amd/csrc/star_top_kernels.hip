@@ -31,21 +31,6 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 constexpr uint32_t kBanned = 0x007fffffu;   // order_of(-inf)
 __device__ __forceinline__ uint64_t key_of(uint32_t order, int j) { return (uint64_t)order << 32 | (uint32_t)~j; }
 
-// A row's maximum, sum and sum of e_j x_j.
-struct Moments {
-    float m, s, w;
-};
-// The same relative to a larger maximum.  (A side that has seen nothing but -inf adds nothing.)
-__device__ __forceinline__ Moments rebased(const Moments& a, float base, float k) {
-    const float x = (a.m - base) * k, f = __builtin_amdgcn_exp2f(x);
-    return Moments{base, a.s * f, a.s == 0.f ? 0.f : (a.w + a.s * x) * f};
-}
-__device__ __forceinline__ void add_element(Moments& a, float l, float k) {   // (a.m is finite, or all so far is -inf)
-    const float x = (l - a.m) * k, e = __builtin_amdgcn_exp2f(x);
-    a.s += e;
-    a.w = __builtin_fmaf(e, fmaxf(x, -1e30f), a.w);   // (0 of a value of -inf; NaN comes through e)
-}
-
 // f(value, id) for a thread's elements of a row.
 template <class E, int NT, class F>
 __device__ __forceinline__ void for_elements(const char* row, const RowSpan& sp, int tid, F&& f) {
@@ -57,10 +42,11 @@ __device__ __forceinline__ void for_elements(const char* row, const RowSpan& sp,
     if (tid < sp.edge) f(E::one(row, sp.edge_element(tid)), sp.edge_element(tid));
 }
 
-// Keys that a workgroup has put together, and the count of them.
+// Keys that a workgroup has put together, and the count of them (which may be more than there is room for).
+constexpr int kListed = 1024;
 struct KeyList {
     int count;
-    uint64_t key[kMostAlternatives];
+    uint64_t key[kListed];
 };
 
 // The k largest keys of the row, one digit of 8 bits at a time: a histogram of the keys that agree with the digits found so far, then the digit in
@@ -101,13 +87,57 @@ __device__ void select_by_digits(const char* row, const RowSpan& sp, int k, KeyL
     __syncthreads();
 }
 
-template <class E, int NT>
-__global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
-    __shared__ float shared[3][NT / 64];
+// Over a wave, without LDS: the maximum, in every lane.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float dpp_max(float x) {   // (lanes without a source keep their own)
+    const int b = __float_as_int(x);
+    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(b, b, CTRL, ROW_MASK, 0xf, false)));
+}
+__device__ __forceinline__ float wave_max(float x) {
+    x = dpp_max<0xB1, 0xf>(x);    // within pairs, quads, 8, 16 lanes, then the rows of 16 (see wave_sum_to_lane63)
+    x = dpp_max<0x4E, 0xf>(x);
+    x = dpp_max<0x141, 0xf>(x);
+    x = dpp_max<0x140, 0xf>(x);
+    x = dpp_max<0x142, 0xa>(x);
+    x = dpp_max<0x143, 0xc>(x);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+// The r-th largest of the lanes' values.
+__device__ __forceinline__ float wave_rth(float x, int r) {
+    float m = wave_max(x);
+    for (; r > 1 && m > -INFINITY; --r) {
+        if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)__ballot(x == m)) - 1) x = -INFINITY;
+        m = wave_max(x);
+    }
+    return m;
+}
+
+// Puts the values of x that are no less than `least` on the list.  (A lane's largest value of a chunk tells first whether any is.)
+template <class E>
+__device__ __forceinline__ void list_chunk(KeyList& list, const u32x4& x, float least, int id) {
+    u32x4 one[1] = {x};
+    if (max_of<E>(one, -INFINITY) < least) return;
+    static_for<0, E::VEC>([&](auto J) {
+        const float v = E::template get<decltype(J)::value>(x);
+        if (v >= least) {
+            const int at = atomicAdd(&list.count, 1);
+            if (at < kListed) list.key[at] = key_of(order_of(v), id + decltype(J)::value);
+        }
+    });
+}
+
+// A workgroup a row.  Its first H chunks a thread are held in registers until their largest values are known, one a thread: of these the
+// `rank`-th of every wave, and of those the least, is no more than the k-th largest value of the row.  Words that reach it go on a list, which
+// holds the alternatives and little else (about 1.3 k words of a row held whole, more in proportion of one that is not), and a word's place among them is the
+// number of larger keys.  The rest of the row goes by once.  A row that has more such words than the list holds -- of equal values, or
+// rising ones -- is searched digit by digit.
+template <class E, int NT, int H, bool ENTROPY>
+__global__ __launch_bounds__(NT, 8) void top_kernel(const TopArgs a) {
+    __shared__ float shared[4][NT / 64];
     __shared__ KeyList list;
     __shared__ int bins[256], found[2];
     const int V = (int)a.l.vocab, tid = threadIdx.x;
-    const int64_t t = a.first + blockIdx.x, y = a.l.targets ? a.l.targets[t] : 0;
+    const int64_t t = a.first + (NT >= 512 ? die_run(blockIdx.x) : (int64_t)blockIdx.x), y = a.l.targets ? a.l.targets[t] : 0;
     int64_t* ids = a.ids + t * a.k;
     float* top = a.top + t * a.k;
     if (a.l.targets && (y < 0 || y >= V)) {
@@ -125,27 +155,84 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
     const char* row = reinterpret_cast<const char*>(a.l.x) + t * a.l.ld * E::BYTES;
     const RowSpan sp = row_span<E, NT>(row, V);
     const float k = a.l.k;
-    float most = -INFINITY;
-    for_elements<E, NT>(row, sp, tid, [&](float v, int) { most = fmaxf(most, v); });
-    const float m = fold_row<NT>(most, shared[0], [](float p, float q) { return fmaxf(p, q); });
-    Moments mine{m == -INFINITY ? 0.f : m, 0.f, 0.f};
-    for_elements<E, NT>(row, sp, tid, [&](float v, int) { add_element(mine, v, k); });
-    const float s = fold_row<NT>(mine.s, shared[1], [](float p, float q) { return p + q; });
-    const float w = fold_row<NT>(mine.w, shared[2], [](float p, float q) { return p + q; });
+    u32x4 x[H];
+    load_chunks<E, NT>(x, row, sp, tid);
+    const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
+    const float ly = E::one(row, y);
+    if (tid == 0) list.count = 0;
+    const float mine = max_of<E>(x, edge);
+    keep_packed(x);
+    const float rth = a.k ? wave_rth(mine, (a.k + NT / 64 - 1) / (NT / 64)) : INFINITY, most = wave_max(mine);
+    if ((tid & 63) == 0) {
+        shared[0][tid >> 6] = most;
+        shared[1][tid >> 6] = rth;
+    }
+    __syncthreads();
+    Seen seen{-INFINITY, 0.f, 0.f};
+    float least = shared[1][0];
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) {
+        seen.m = fmaxf(seen.m, shared[0][i]);
+        least = fminf(least, shared[1][i]);
+    }
+    least = fmaxf(least, -3.402823466e38f);   // (banned words are no alternatives)
+    static_for<0, H>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        list_chunk<E>(list, x[i], least, sp.head + (tid + i * NT) * E::VEC);
+    });
+    if (edge >= least) {
+        const int at = atomicAdd(&list.count, 1);
+        if (at < kListed) list.key[at] = key_of(order_of(edge), sp.edge_element(tid));
+    }
+    keep_packed(x);
+    see<ENTROPY>(seen, edge, k);
+    static_for<0, H>([&](auto I) {
+        static_for<0, E::VEC>([&](auto J) { see<ENTROPY>(seen, E::template get<decltype(J)::value>(x[decltype(I)::value]), k); });
+    });
+    for (int c = tid + H * NT; c < sp.chunks; c += 4 * NT) {
+        u32x4 z[4];
+        load_chunks<E, NT>(z, row, sp, c);
+        const float m = max_of<E>(z, -INFINITY);
+        if (m >= least)
+            static_for<0, 4>([&](auto I) {
+                constexpr int i = decltype(I)::value;
+                list_chunk<E>(list, z[i], least, sp.head + (c + i * NT) * E::VEC);
+            });
+        if (m > seen.m) see_max<ENTROPY>(seen, m, k);
+        static_for<0, 4>([&](auto I) {
+            static_for<0, E::VEC>([&](auto J) { see<ENTROPY>(seen, E::template get<decltype(J)::value>(z[decltype(I)::value]), k); });
+        });
+    }
+    float m = seen.m;
+    if (sp.chunks > H * NT) {
+        m = wave_max(m);
+        __syncthreads();
+        if ((tid & 63) == 0) shared[0][tid >> 6] = m;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) m = fmaxf(m, shared[0][i]);
+        see_max<ENTROPY>(seen, m, k);
+    }
+    auto plus = [](float p, float q) { return p + q; };
+    const float s = fold_row<NT>(seen.s, shared[2], plus), w = ENTROPY ? fold_row<NT>(seen.w, shared[3], plus) : 0.f;
     const Two log_s = two_log(s);
     if (tid == 0) {
-        if (a.logp) a.logp[t] = add(scaled_difference(a.l, E::one(row, y), m), log_s, -1.f).high;
+        if (a.logp) a.logp[t] = add(scaled_difference(a.l, ly, m), log_s, -1.f).high;
         if (a.lse) a.lse[t] = add(scaled_difference(a.l, m, 0.f), log_s, 1.f).high;
-        if (a.entropy) a.entropy[t] = (log_s.high - kLn2 * (w / s)) + log_s.low;
+        if (ENTROPY) a.entropy[t] = (log_s.high - kLn2 * (w / s)) + log_s.low;
     }
     if (a.k == 0) return;
     const bool there = s > 0.f && s < INFINITY;   // (a row of NaN, +inf or nothing but -inf has no alternatives)
-    if (there) select_by_digits<E, NT>(row, sp, a.k, list, bins, found);
-    const int n = there ? min(list.count, a.k) : 0;
-    if (tid < n) {
-        const uint64_t key = list.key[tid];
+    if (there && list.count > kListed) {
+        __syncthreads();
+        select_by_digits<E, NT>(row, sp, a.k, list, bins, found);
+    }
+    const int listed = there ? list.count : 0, n = min(listed, a.k);
+    for (int e = tid; e < listed; e += NT) {
+        const uint64_t key = list.key[e];
         int rank = 0;
-        for (int i = 0; i < n; ++i) rank += list.key[i] > key;
+        for (int i = 0; i < listed; ++i) rank += list.key[i] > key;
+        if (rank >= a.k) continue;
         ids[rank] = (int64_t)(uint32_t)~(uint32_t)key;
         top[rank] = add(scaled_difference(a.l, value_of((uint32_t)(key >> 32)), m), log_s, -1.f).high;
     }
@@ -155,10 +242,13 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
     }
 }
 
-template <class E>
+template <class E, bool ENTROPY>
 void launch_top_of(const TopArgs& a, unsigned rows, hipStream_t stream) {
-    if (a.l.vocab <= 2048 * E::VEC) top_kernel<E, 256><<<rows, 256, 0, stream>>>(a);
-    else top_kernel<E, 1024><<<rows, 1024, 0, stream>>>(a);
+    const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;
+    if (chunks <= 512) top_kernel<E, 256, 2, ENTROPY><<<rows, 256, 0, stream>>>(a);
+    else if (chunks <= 2048) top_kernel<E, 256, 8, ENTROPY><<<rows, 256, 0, stream>>>(a);
+    else if (chunks <= 4096) top_kernel<E, 1024, 4, ENTROPY><<<rows, 1024, 0, stream>>>(a);
+    else top_kernel<E, 1024, 8, ENTROPY><<<rows, 1024, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -168,8 +258,8 @@ hipError_t launch_top(const Logits& l, int k, float* logp, float* entropy, float
     constexpr int64_t kRows = (int64_t)1 << 21;
     for (a.first = 0; a.first < l.tokens; a.first += kRows) {
         const unsigned rows = (unsigned)std::min(kRows, l.tokens - a.first);
-        if (l.dtype == STAR_F32) launch_top_of<ElemF32>(a, rows, stream);
-        else launch_top_of<ElemBf16>(a, rows, stream);
+        if (l.dtype == STAR_F32) entropy ? launch_top_of<ElemF32, true>(a, rows, stream) : launch_top_of<ElemF32, false>(a, rows, stream);
+        else entropy ? launch_top_of<ElemBf16, true>(a, rows, stream) : launch_top_of<ElemBf16, false>(a, rows, stream);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
