@@ -38,13 +38,21 @@ struct ListedArgs {
 
 constexpr int kEntries = kMostAlternatives + 1;   // the taken token is the last
 
-// The named words of a row.  An entry that names no word, or one that an earlier entry has named, is dead: its id is -1.
+// The named words of a row, which its first wave puts together.  An entry that names no word, or one that an earlier entry names, is dead: its id
+// is -1.
 template <int NT>
 struct WordList {
-    int n;
     int id[kEntries], next[kEntries], head[NT];
-    float value[kEntries];                        // what is written there
+    float logit[kEntries], value[kEntries];       // value: what is written there
+    float q[kMostAlternatives], log_q[kMostAlternatives];
 };
+
+// The wave's own LDS accesses before and behind this keep their order, also for the compiler; the hardware takes them in order.
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // Who reads and writes a word: a thread, and the thread's chunk that holds it (-1: its element outside the chunks).
 struct Owner {
@@ -58,20 +66,14 @@ __device__ __forceinline__ Owner owner_of(const RowSpan& sp, int id) {
     return c < sp.chunks ? Owner{c % NT, c} : Owner{id - (sp.V - sp.edge), -1};
 }
 
-// Chains of the first `n` entries by their owners.  Ends with a barrier.
+// The first entry that names the word of entry e.
 template <class E, int NT>
-__device__ __forceinline__ void chain_words(WordList<NT>& w, const RowSpan& sp, int n, int tid) {
-    for (int i = tid; i < NT; i += NT) w.head[i] = -1;
-    __syncthreads();
-    if (tid < n && w.id[tid] >= 0) w.next[tid] = atomicExch(&w.head[owner_of<E, NT>(sp, w.id[tid]).thread], tid);
-    __syncthreads();
-}
-// The first entry that names the word of entry i.
-template <class E, int NT>
-__device__ __forceinline__ int first_of(const WordList<NT>& w, const RowSpan& sp, int i) {
-    int least = i;
-    for (int e = w.head[owner_of<E, NT>(sp, w.id[i]).thread]; e >= 0; e = w.next[e])
-        if (w.id[e] == w.id[i]) least = min(least, e);
+__device__ __forceinline__ int first_of(const WordList<NT>& w, const RowSpan& sp, int e) {
+    const int id = w.id[e];
+    if (id < 0) return -1;
+    int least = e;
+    for (int f = w.head[owner_of<E, NT>(sp, id).thread]; f >= 0; f = w.next[f])
+        if (w.id[f] == id) least = min(least, f);
     return least;
 }
 
@@ -84,7 +86,7 @@ struct LeftOut {
     bool edge;
     __device__ __forceinline__ LeftOut(const WordList<NT>& words, const RowSpan& span, int thread) : w(words), sp(span), tid(thread), at(0x7fffffff), edge(false) {
         for (int e = w.head[tid]; e >= 0; e = w.next[e]) {
-            if (e == kMostAlternatives) continue;       // (the taken token is no word of the teacher's)
+            if (e == kMostAlternatives || w.id[e] < 0) continue;       // (the taken token is no word of the teacher's)
             const int c = owner_of<E, NT>(sp, w.id[e]).chunk;
             edge |= c < 0;
             if (c >= 0) at = min(at, c);
@@ -95,7 +97,7 @@ struct LeftOut {
         uint32_t mask = 0;
         at = 0x7fffffff;
         for (int e = w.head[tid]; e >= 0; e = w.next[e]) {
-            if (e == kMostAlternatives) continue;
+            if (e == kMostAlternatives || w.id[e] < 0) continue;
             const int chunk = owner_of<E, NT>(sp, w.id[e]).chunk;
             if (chunk == c) mask |= 1u << (w.id[e] - sp.head - c * E::VEC);
             if (chunk > c) at = min(at, chunk);
@@ -141,18 +143,165 @@ __device__ __forceinline__ double sum_wave(double x) {
     return x;
 }
 
-// What the wave that holds the list hands to the others.
+// What the first wave hands to the others.
 struct RowNumbers {
     float a, b, mean;
 };
 
+// What the first wave knows of its row before the row's sums do: sum of the teacher's shares, of the derivatives, and the entry that stands for the
+// taken token (-1: none is taken).
+struct Prelude {
+    double sum;
+    int taken;
+};
+
+// Puts the list together: entries `lane`, 64 + lane and the taken token.
+template <class E, int NT, Listed WORK>
+__device__ __forceinline__ Prelude list_words(const ListedArgs& a, WordList<NT>& w, const RowSpan& sp, const char* row, int64_t t, int64_t y) {
+    const int lane = threadIdx.x, n = a.words.k;
+    for (int i = lane; i < NT; i += 64) w.head[i] = -1;
+#pragma unroll
+    for (int e = lane; e < kEntries; e += 64) {
+        const int64_t id = e < n ? a.words.ids[t * n + e] : (e == kMostAlternatives ? y : -1);
+        const bool there = id >= 0 && id < sp.V;
+        w.id[e] = there ? (int)id : -1;
+        if (there) w.logit[e] = E::one(row, id);
+    }
+    wave_order();
+    for (int e = lane; e < kEntries; e += 64)
+        if (w.id[e] >= 0) w.next[e] = atomicExch(&w.head[owner_of<E, NT>(sp, w.id[e]).thread], e);
+    wave_order();
+    const int first = first_of<E, NT>(w, sp, lane), second = first_of<E, NT>(w, sp, 64 + lane), taken = first_of<E, NT>(w, sp, kMostAlternatives);
+    wave_order();
+    const bool again[2] = {first >= 0 && first != lane, second >= 0 && second != 64 + lane};
+    if (again[0]) w.id[lane] = -1;
+    if (again[1]) w.id[64 + lane] = -1;
+    if (taken != kMostAlternatives && lane == 0) w.id[kMostAlternatives] = -1;
+    Prelude p{0.0, taken};
+    if constexpr (WORK == Listed::Distill) {
+#pragma unroll 1
+        for (int e = lane; e < kMostAlternatives; e += 64) {
+            const bool live = e < 64 ? first == e : second == e;
+            const float log_q = live ? a.words.logp[t * n + e] : -INFINITY;
+            const double q = exp((double)log_q);
+            w.log_q[e] = log_q;
+            w.q[e] = (float)q;
+            p.sum += q;
+        }
+        p.sum = sum_wave(p.sum);
+    } else {
+        // derivatives by the words' log-probabilities, equal words' added in the order of the entries, to `q`
+        const float inv_t = a.l.inv_t;
+        double mine[2] = {0.0, 0.0};
+        if (first >= 0) mine[0] = (double)a.dtop[t * n + lane];
+        if (second >= 0) mine[1] = (double)a.dtop[t * n + 64 + lane];
+        p.sum = sum_wave(mine[0] + mine[1]);
+        if (__any(again[0] || again[1])) {
+            for (int f = 1; f < n; ++f) {
+                const int same = f < 64 ? __shfl(first, f) : __shfl(second, f - 64);
+                const double d = f < 64 ? __shfl(mine[0], f) : __shfl(mine[1], f - 64);
+                if (same != f && same == lane) mine[0] += d;
+                if (same != f && same == 64 + lane) mine[1] += d;
+            }
+        }
+        const double dy = taken >= 0 && a.dlogp ? (double)a.dlogp[t] : 0.0;
+        p.sum += dy;
+        w.q[lane] = (float)((mine[0] + (taken == lane ? dy : 0.0)) * inv_t);
+        w.q[64 + lane] = (float)((mine[1] + (taken == 64 + lane ? dy : 0.0)) * inv_t);
+    }
+    return p;
+}
+
+// e^x to the accuracy of fp32, of any x.
+__device__ __forceinline__ double near_exp(double x) {
+    const double z = fmax(x * 1.4426950408889634, -2000.0), n = rint(z);   // (NaN is dropped: whoever sums these sums the row's own as well)
+    return ldexp((double)__builtin_amdgcn_exp2f((float)(z - n)), (int)n);
+}
+
+// q f(log p - log q), f(d) = e^d - d - 1, with d = log p - log q.
+__device__ __forceinline__ double divergence_term(double q, double d, double p) {
+    if (q == 0.0) return p;
+    return fabs(d) < 0.25 ? q * (double)kl_of((float)d, 0.f) : p - q - q * d;
+}
+
+// Numbers of the distillation loss, from the maximum m and sum s of the words that are not named.
+template <int NT>
+__device__ __forceinline__ RowNumbers distill_words(const ListedArgs& a, WordList<NT>& w, const Prelude& given, int64_t t, float m, float s) {
+    const int lane = threadIdx.x, taken = given.taken;
+    const double weight = a.l.weights ? (double)a.l.weights[t] : 1.0, inv_t = (double)a.l.inv_t + a.l.inv_t_low, base = m == -INFINITY ? 0.f : m;
+    float most = m;
+    for (int e = lane; e < kMostAlternatives; e += 64)
+        if (w.id[e] >= 0) most = fmaxf(most, w.logit[e]);
+    most = fold_wave<64>(most, [](float p, float q) { return fmaxf(p, q); });
+    const double whole_base = most == -INFINITY ? 0.f : most;
+    // the sum over all words, relative to the largest: of the named ones, and of the rest (which without any word is 0)
+    double named = 0.0;
+    float sure = 0.f;   // NaN if a named word's logit is
+    for (int e = lane; e < kMostAlternatives; e += 64)
+        if (w.id[e] >= 0) {
+            named += near_exp(((double)w.logit[e] - whole_base) * inv_t);
+            sure += w.logit[e] - w.logit[e] == 0.f || w.logit[e] == -INFINITY ? 0.f : NAN;
+        }
+    named = sum_wave(named + (double)sure);
+    const bool rest = !(s == 0.f);
+    const double down = rest ? near_exp((base - whole_base) * inv_t) : 0.0, all = named + (rest ? s * down : 0.0);
+    const double none = all > 0.0 && all < INFINITY ? 0.0 : NAN;   // NaN: a row without probabilities
+    double share = given.sum, left = 0.0, divide = 1.0;
+    if (a.distill.renormalise) {
+        divide = share;
+        share = share == 0.0 ? 0.0 : share / share;
+    } else if (rest) {
+        left = share < 1.0 ? 1.0 - share : share - share;   // (0, or NaN)
+    }
+    const double logs = log(lane == 0 ? all : lane == 1 ? (double)s : lane == 2 ? left : divide);
+    const double log_all = __shfl(logs, 0), log_s = __shfl(logs, 1), log_left = __shfl(logs, 2), shift = a.distill.renormalise ? __shfl(logs, 3) : 0.0;
+    // the row's loss, and at the named words c ((Q + ce) p - q - ce [taken])
+    const double whole = share + left, ce = a.distill.ce, c = (double)a.distill.scale * weight * inv_t + none;
+    double kl = 0.0;
+#pragma unroll 1
+    for (int e = lane; e < kMostAlternatives; e += 64) {
+        if (w.id[e] < 0) continue;
+        const double log_p = ((double)w.logit[e] - whole_base) * inv_t - log_all, p = exp(log_p);
+        const double q = w.q[e] == 0.f ? 0.0 : w.q[e] / divide;
+        kl += divergence_term(q, log_p - (w.log_q[e] - shift), p);
+        w.value[e] = (float)(c * ((whole + ce) * p - q - (taken == e ? ce : 0.0)));
+    }
+    kl = sum_wave(kl);
+    if (rest) kl += divergence_term(left, log_s + (base - whole_base) * inv_t - log_all - log_left, s * down / all);
+    kl = (whole == 0.0 ? 0.0 : kl + (whole - 1.0)) + none;     // (a teacher that says nothing costs nothing)
+    // of the rest e (c (Q + ce) / sum of all - c q_r / sum of the rest)
+    const double slope = rest ? c * ((whole + ce) * down / all - left / s) : none;
+    const double ly = taken >= 0 ? (double)w.logit[kMostAlternatives] : 0.0, nll = taken >= 0 ? log_all - (ly - whole_base) * inv_t : 0.0;
+    if (lane == 0) {
+        w.value[kMostAlternatives] = (float)(slope * (rest ? exp((ly - base) * inv_t) : 0.0) - c * ce);
+        if (a.kl) a.kl[t] = (float)kl;
+        a.terms[2 * t] = kl;
+        a.terms[2 * t + 1] = nll;
+    }
+    return RowNumbers{(float)slope, 0.f, 0.f};
+}
+
+// Numbers of a function of the alternatives, from the maximum m, sum s and sum of e_j x_j of all words.
+template <int NT, bool ENTROPY>
+__device__ __forceinline__ RowNumbers alternatives_words(const ListedArgs& a, WordList<NT>& w, const Prelude& given, int64_t t, float m, float s, float sx) {
+    const int lane = threadIdx.x;
+    const double inv_t = (double)a.l.inv_t + a.l.inv_t_low;
+    const double slope = ENTROPY ? (double)a.dentropy[t] * 0.693147180559945309 * inv_t / s : 0.0;
+    const Dense dense{m == -INFINITY ? 0.f : m, a.l.k, (float)(-given.sum * inv_t / s), (float)slope, ENTROPY ? sx / s : 0.f};
+    for (int e = lane; e < kMostAlternatives; e += 64)
+        if (w.id[e] >= 0) w.value[e] = dense.of<ENTROPY>(w.logit[e]) + w.q[e];
+    if (lane == 0 && w.id[kMostAlternatives] >= 0)
+        w.value[kMostAlternatives] = dense.of<ENTROPY>(w.logit[kMostAlternatives]) + (a.dlogp ? a.dlogp[t] * a.l.inv_t : 0.f);
+    return RowNumbers{dense.a, dense.b, dense.mean};
+}
+
 // A workgroup a row; the last H chunks a thread stay in registers, those before are read a second time, from their end.
 template <class E, int NT, int H, Listed WORK, bool ENTROPY>
-__global__ __launch_bounds__(NT, H <= 8 ? 8 : 4) void listed_kernel(const ListedArgs a) {
+__global__ __launch_bounds__(NT, NT >= 512 ? 4 : 5) void listed_kernel(const ListedArgs a) {
     __shared__ WordList<NT> w;
     __shared__ float shared[3][NT / 64];
     __shared__ RowNumbers numbers;
-    const int V = (int)a.l.vocab, tid = threadIdx.x, n = a.words.k;
+    const int V = (int)a.l.vocab, tid = threadIdx.x;
     if (a.ticket && blockIdx.x == 0 && tid == 0) *a.ticket = 0u;
     const int64_t t = a.first + (NT >= 512 ? die_run(blockIdx.x) : (int64_t)blockIdx.x), y = a.l.targets ? a.l.targets[t] : -1;
     const char* row = reinterpret_cast<const char*>(a.l.x) + t * a.l.ld * E::BYTES;
@@ -168,171 +317,63 @@ __global__ __launch_bounds__(NT, H <= 8 ? 8 : 4) void listed_kernel(const Listed
     }
     const RowSpan sp = row_span<E, NT>(row, V);
     const int rest = (max(sp.chunks - H * NT, 0) + NT - 1) / NT * NT;   // (whole turns of the threads: chunk c is thread c % NT's)
-    u32x4 x[H > 0 ? H : 1];
-    if constexpr (H > 0) load_chunks<E, NT>(x, row, sp, rest + tid);
-    float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
-
-    // the list: the words of entries 0 .. n - 1, then the taken token
-    float logit = 0.f;
-    if (tid < kEntries) {
-        const int64_t id = tid < n ? a.words.ids[t * n + tid] : (tid == kMostAlternatives ? y : -1);
-        const bool there = id >= 0 && id < V;
-        w.id[tid] = there ? (int)id : -1;
-        if (there) logit = E::one(row, id);
-    }
-    chain_words<E, NT>(w, sp, kEntries, tid);
-    int same = -1;   // the entry that stands for this one's word
-    if (tid < kEntries && w.id[tid] >= 0) same = first_of<E, NT>(w, sp, tid);
+    u32x4 x[H];
+    load_chunks<E, NT>(x, row, sp, rest + tid);
+    const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
+    Prelude given{0.0, -1};
+    if (tid < 64) given = list_words<E, NT, WORK>(a, w, sp, row, t, y);
+    __syncthreads();
 
     Seen seen{-INFINITY, 0.f, 0.f};
     float edge_left = edge;
     RowSpan before = sp;
     before.chunks = rest;
-    if constexpr (WORK == Listed::Distill) {
+    {
         LeftOut<E, NT> left(w, sp, tid);
-        if (left.edge) edge_left = -INFINITY;
+        if (WORK == Listed::Alternatives) left.at = 0x7fffffff;
+        else if (left.edge) edge_left = -INFINITY;
         for (int c = tid; c < rest; c += 4 * NT) {
             u32x4 z[4];
             load_chunks<E, NT, Reading::Again>(z, row, before, c);
             static_for<0, 4>([&](auto I) {
                 constexpr int i = decltype(I)::value;
-                if (c + i * NT == left.at && c + i * NT < rest) left.take(z[i], c + i * NT);
+                if (WORK == Listed::Distill && c + i * NT == left.at && c + i * NT < rest) left.take(z[i], c + i * NT);
             });
-            see_chunks<E, false>(seen, z, k);
-        }
-        if constexpr (H > 0)
-            static_for<0, H>([&](auto I) {
-                constexpr int i = decltype(I)::value;
-                if (rest + tid + i * NT == left.at) left.take(x[i], rest + tid + i * NT);
-            });
-    } else {
-        for (int c = tid; c < rest; c += 4 * NT) {
-            u32x4 z[4];
-            load_chunks<E, NT, Reading::Again>(z, row, before, c);
             see_chunks<E, ENTROPY>(seen, z, k);
         }
+        static_for<0, H>([&](auto I) {
+            constexpr int i = decltype(I)::value;
+            if (WORK == Listed::Distill && rest + tid + i * NT == left.at) left.take(x[i], rest + tid + i * NT);
+        });
     }
-    see_max<ENTROPY>(seen, fmaxf(seen.m, edge_left), k);
-    see<ENTROPY>(seen, edge_left, k);
-    if constexpr (H > 0) see_chunks<E, ENTROPY>(seen, x, k);
-    const float m = fold_row<NT>(seen.m, shared[0], [](float p, float q) { return fmaxf(p, q); }), base = m == -INFINITY ? 0.f : m;
+    const float most = max_of<E>(x, fmaxf(seen.m, edge_left));
+    keep_packed(x);
+    const float m = fold_row<NT>(most, shared[0], [](float p, float q) { return fmaxf(p, q); });
     see_max<ENTROPY>(seen, m, k);
+    see<ENTROPY>(seen, edge_left, k);
+    static_for<0, H>([&](auto I) {
+        static_for<0, E::VEC>([&](auto J) { see<ENTROPY>(seen, E::template get<decltype(J)::value>(x[decltype(I)::value]), k); });
+        // (a chunk after the other: the compiler would put a sum off to where it is used, and keep all of its terms till then)
+        asm volatile("" : "+v"(seen.s), "+v"(seen.w));
+    });
+    keep_packed(x);
     auto plus = [](float p, float q) { return p + q; };
     const float s = fold_row<NT>(seen.s, shared[1], plus);
     const float sx = ENTROPY ? fold_row<NT>(seen.w, shared[2], plus) : 0.f;
 
-    // the list's numbers, by the first wave: entries `lane`, 64 + lane, and the taken token by all of it
-    // (the logits lie with the threads that read them: they go through LDS)
-    if (tid < kEntries) w.value[tid] = logit;
-    __shared__ int stands[kEntries];
-    if (tid < kEntries) stands[tid] = same;
-    __syncthreads();
     if (tid < 64) {
-        const double weight = a.l.weights ? (double)a.l.weights[t] : 1.0, inv_t = (double)a.l.inv_t + a.l.inv_t_low;
-        const int ye = stands[kMostAlternatives];   // entry that stands for the taken token, or -1
-        const double ly = ye >= 0 ? (double)w.value[kMostAlternatives] : 0.0;
-        float value[2] = {0.f, 0.f}, y_value = 0.f;
-        bool live[2];
-        float l[2];
-        for (int i = 0; i < 2; ++i) {
-            const int e = tid + 64 * i;
-            live[i] = e < n && stands[e] == e;
-            l[i] = w.value[e];
-        }
-        if constexpr (WORK == Listed::Distill) {
-            double logq[2], q[2], share = 0.0;
-            float lm = -INFINITY;
-            for (int i = 0; i < 2; ++i) {
-                logq[i] = live[i] ? (double)a.words.logp[t * n + tid + 64 * i] : -INFINITY;
-                q[i] = exp(logq[i]);
-                share += q[i];
-                if (live[i]) lm = fmaxf(lm, l[i]);
-            }
-            share = sum_wave(share);
-            lm = fold_wave<64>(lm, [](float p, float r) { return fmaxf(p, r); });
-            const float whole_m = fmaxf(m, lm), whole_base = whole_m == -INFINITY ? 0.f : whole_m;
-            // sum over all words, relative to the largest: that of the rest, that of the named
-            double named = 0.0;
-            for (int i = 0; i < 2; ++i)
-                if (live[i]) named += exp(((double)l[i] - whole_base) * inv_t);
-            named = sum_wave(named);
-            const double down = exp(((double)base - whole_base) * inv_t);   // (a rest without any word has s = 0)
-            const double all = named + (s == 0.f ? 0.0 : s * down), log_all = log(all);
-            double left = 0.0, shift = 0.0;
-            if (a.distill.renormalise) {
-                shift = log(share);
-                for (int i = 0; i < 2; ++i) q[i] /= share;
-                if (share == 0.0) q[0] = q[1] = 0.0;
-                share = share == 0.0 ? 0.0 : 1.0;
-            } else if (!(s == 0.f)) {
-                left = fmax(0.0, 1.0 - share);
-                if (share != share) left = share;
-            }
-            const double whole = share + left, none = all > 0.0 && all < INFINITY ? 0.0 : NAN;   // (NAN: a row without probabilities)
-            // KL = sum q f(log p - log q) + Q - 1
-            auto term = [](double q_, double log_q, double log_p) -> double {
-                const double p = exp(log_p);
-                if (q_ == 0.0) return p;
-                const double d = log_p - log_q;
-                if (!(d < 1.0)) return p - q_ - q_ * d;
-                const float df = (float)d;
-                return q_ * (double)kl_of(df, expm1f(df));
-            };
-            double kl = 0.0, log_p[2];
-            for (int i = 0; i < 2; ++i) {
-                log_p[i] = ((double)l[i] - whole_base) * inv_t - log_all;
-                if (live[i]) kl += term(q[i], logq[i] - shift, log_p[i]);
-            }
-            kl = sum_wave(kl);
-            const double log_rest = s == 0.f ? -INFINITY : log((double)s) + ((double)base - whole_base) * inv_t - log_all;
-            kl += term(left, log(left), log_rest) + (whole - 1.0);
-            if (whole == 0.0) kl = 0.0;     // (a teacher that says nothing)
-            kl += none;
-            const double ce = a.distill.ce, ly_p = (ly - whole_base) * inv_t - log_all;
-            const double nll = ye >= 0 ? -ly_p : 0.0;
-            const double c = (double)a.distill.scale * weight * inv_t + none;
-            // at named words c ((Q + ce) p - q - ce [taken]), of the rest e (c (Q + ce) / sum - c q_r / sum of the rest)
-            for (int i = 0; i < 2; ++i)
-                value[i] = (float)(c * ((whole + ce) * exp(log_p[i]) - q[i] - (ye == tid + 64 * i ? ce : 0.0)));
-            const double slope = s == 0.f ? none : c * ((whole + ce) * down / all - left / s);
-            y_value = (float)(slope * exp((ly - base) * inv_t) - c * ce);
-            if (tid == 0) {
-                numbers = RowNumbers{(float)slope, 0.f, 0.f};
-                if (a.kl) a.kl[t] = (float)kl;
-                a.terms[2 * t] = kl;
-                a.terms[2 * t + 1] = nll;
-            }
-        } else {
-            // derivatives by the words' log-probabilities, equal words' added in the order of the entries
-            double d[2] = {0.0, 0.0}, all_d = 0.0, yd = 0.0;
-            const double dy = ye >= 0 && a.dlogp ? (double)a.dlogp[t] : 0.0;
-            bool again = false;
-            for (int i = 0; i < 2; ++i) {
-                const int e = tid + 64 * i;
-                if (e < n && stands[e] >= 0) all_d += d[i] = (double)a.dtop[t * n + e];
-                again |= e < n && stands[e] >= 0 && !live[i];
-            }
-            if (__any(again))
-                for (int i = 0; i < 2; ++i)
-                    for (int f = tid + 64 * i + 1; live[i] && f < n; ++f)
-                        if (stands[f] == tid + 64 * i) d[i] += (double)a.dtop[t * n + f];
-            for (int i = 0; i < 2; ++i)
-                if (ye == tid + 64 * i) d[i] += dy;
-            all_d = sum_wave(all_d) + dy;
-            if (ye == kMostAlternatives) yd = dy;
-            const double dH = a.dentropy ? (double)a.dentropy[t] * 0.693147180559945309 : 0.0, mean = ENTROPY ? (double)sx / s : 0.0;
-            const Dense dense{base, k, (float)(-all_d * inv_t / s), (float)(dH * inv_t / s), (float)mean};
-            for (int i = 0; i < 2; ++i) value[i] = dense.of<ENTROPY>(l[i]) + (float)(d[i] * inv_t);
-            y_value = dense.of<ENTROPY>((float)ly) + (float)(yd * inv_t);
-            if (tid == 0) numbers = RowNumbers{dense.a, dense.b, dense.mean};
-        }
-        for (int i = 0; i < 2; ++i) w.value[tid + 64 * i] = value[i];
-        if (tid == 0) w.value[kMostAlternatives] = y_value;
+        RowNumbers r;
+        if constexpr (WORK == Listed::Distill) r = distill_words<NT>(a, w, given, t, m, s);
+        else r = alternatives_words<NT, ENTROPY>(a, w, given, t, m, s, sx);
+        if (tid == 0) numbers = r;
     }
     __syncthreads();
     if (!out) return;
-    const Dense dense{base, k, numbers.a, numbers.b, numbers.mean};
-    if constexpr (H > 0) store_dense<E, NT, ENTROPY>(x, out, sp, dense, rest + tid);
+    keep_packed(x);
+    int mine = tid;
+    asm volatile("" : "+v"(mine));   // (the addresses are formed again: kept since the loads, they would not fit the registers)
+    const Dense dense{m == -INFINITY ? 0.f : m, k, numbers.a, numbers.b, numbers.mean};
+    store_dense<E, NT, ENTROPY>(x, out, sp, dense, rest + mine);
     for (int first = (rest - 1) / (4 * NT) * (4 * NT); rest > 0 && first >= 0; first -= 4 * NT) {
         u32x4 z[4];
         load_chunks<E, NT>(z, row, before, first + tid);
@@ -341,7 +382,7 @@ __global__ __launch_bounds__(NT, H <= 8 ? 8 : 4) void listed_kernel(const Listed
     if (tid < sp.edge) E::put(out, sp.edge_element(tid), dense.of<ENTROPY>(edge));
     // (a wave's own stores to one word keep their order)
     for (int e = w.head[tid]; e >= 0; e = w.next[e])
-        if (stands[e] == e) E::put(out, w.id[e], w.value[e]);
+        if (w.id[e] >= 0) E::put(out, w.id[e], w.value[e]);
 }
 
 constexpr int kSumThreads = 1024, kSumGroups = 64;
@@ -388,7 +429,7 @@ void launch_listed_of(const ListedArgs& a, hipStream_t stream) {
     const unsigned rows = (unsigned)a.rows;
     if (chunks <= 512) return listed_kernel<E, 256, 2, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
     if (chunks <= 2048) return listed_kernel<E, 256, 8, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
-    if (chunks <= 8192) return listed_kernel<E, 1024, 8, WORK, ENTROPY><<<rows, 1024, 0, stream>>>(a);
+    if (chunks <= 8192) return listed_kernel<E, 512, 16, WORK, ENTROPY><<<rows, 512, 0, stream>>>(a);
     listed_kernel<E, 1024, 16, WORK, ENTROPY><<<rows, 1024, 0, stream>>>(a);
 }
 
