@@ -429,8 +429,7 @@ void launch_listed_of(const ListedArgs& a, hipStream_t stream) {
     const unsigned rows = (unsigned)a.rows;
     if (chunks <= 512) return listed_kernel<E, 256, 2, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
     if (chunks <= 2048) return listed_kernel<E, 256, 8, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
-    if (chunks <= 8192) return listed_kernel<E, 512, 16, WORK, ENTROPY><<<rows, 512, 0, stream>>>(a);
-    listed_kernel<E, 1024, 16, WORK, ENTROPY><<<rows, 1024, 0, stream>>>(a);
+    listed_kernel<E, 512, 16, WORK, ENTROPY><<<rows, 512, 0, stream>>>(a);
 }
 
 template <Listed WORK>
