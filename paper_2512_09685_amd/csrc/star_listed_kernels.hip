@@ -38,13 +38,25 @@ struct ListedArgs {
 
 constexpr int kEntries = kMostAlternatives + 1;   // the taken token is the last
 
+// What the first wave knows of its row before the row's sums do: sum of the teacher's shares, or of the derivatives; the entry that stands for the
+// taken token (-1: none is taken); of the teacher's words the largest logit, and the sum of exp(z - that one's).
+struct Prelude {
+    double sum, named;
+    float most;
+    int taken;
+};
+
 // The named words of a row, which its first wave puts together.  An entry that names no word, or one that an earlier entry names, is dead: its id
-// is -1.
-template <int NT>
+// is -1.  Words that the sums leave out are marked, a byte for each of a thread's held chunks.
+template <int NT, int H>
 struct WordList {
+    static constexpr int MARKS = (H + 3) / 4;
     int id[kEntries], next[kEntries], head[NT];
+    __align__(16) uint32_t marks[NT * MARKS];
+    uint32_t edge_marks[4];                       // (fewer than 128 elements lie outside the chunks)
     float logit[kEntries], value[kEntries];       // value: what is written there
     float q[kMostAlternatives], log_q[kMostAlternatives];
+    Prelude given;
 };
 
 // The wave's own LDS accesses before and behind this keep their order, also for the compiler; the hardware takes them in order.
@@ -67,8 +79,8 @@ __device__ __forceinline__ Owner owner_of(const RowSpan& sp, int id) {
 }
 
 // The first entry that names the word of entry e.
-template <class E, int NT>
-__device__ __forceinline__ int first_of(const WordList<NT>& w, const RowSpan& sp, int e) {
+template <class E, int NT, class Words>
+__device__ __forceinline__ int first_of(const Words& w, const RowSpan& sp, int e) {
     const int id = w.id[e];
     if (id < 0) return -1;
     int least = e;
@@ -77,129 +89,175 @@ __device__ __forceinline__ int first_of(const WordList<NT>& w, const RowSpan& sp
     return least;
 }
 
-// A thread's words that its sums leave out, from its first chunk on: `at` is the next chunk that holds any.
-template <class E, int NT>
+// Takes the words that `mask` names out of a chunk.
+template <class E>
+__device__ __forceinline__ void take_out(u32x4& x, uint32_t mask) {
+    static_for<0, 4>([&](auto I) {
+        constexpr int i = decltype(I)::value;
+        uint32_t out;
+        if constexpr (E::VEC == 4) out = (uint32_t)__builtin_amdgcn_sbfe((int)mask, i, 1);
+        else out = ((uint32_t)__builtin_amdgcn_sbfe((int)mask, 2 * i, 1) & 0xffffu) | ((uint32_t)__builtin_amdgcn_sbfe((int)mask, 2 * i + 1, 1) & 0xffff0000u);
+        x[i] = (x[i] & ~out) | (E::NOTHING & out);
+    });
+}
+
+// A thread's words in the chunks that are not held: `at` is the next chunk that holds any.
+template <class E, int NT, class Words>
 struct LeftOut {
-    const WordList<NT>& w;
+    const Words& w;
     const RowSpan& sp;
-    int tid, at;
-    bool edge;
-    __device__ __forceinline__ LeftOut(const WordList<NT>& words, const RowSpan& span, int thread) : w(words), sp(span), tid(thread), at(0x7fffffff), edge(false) {
-        for (int e = w.head[tid]; e >= 0; e = w.next[e]) {
-            if (e == kMostAlternatives || w.id[e] < 0) continue;       // (the taken token is no word of the teacher's)
-            const int c = owner_of<E, NT>(sp, w.id[e]).chunk;
-            edge |= c < 0;
-            if (c >= 0) at = min(at, c);
-        }
+    int tid, rest, at;
+    __device__ __forceinline__ LeftOut(const Words& words, const RowSpan& span, int thread, int not_held) : w(words), sp(span), tid(thread), rest(not_held) {
+        find(-1);
     }
-    // Takes the words of chunk c, which is `at`, out of x.
-    __device__ __forceinline__ void take(u32x4& x, int c) {
+    __device__ __forceinline__ uint32_t find(int c) {   // the words of chunk c; `at` becomes the one behind it
         uint32_t mask = 0;
         at = 0x7fffffff;
-        for (int e = w.head[tid]; e >= 0; e = w.next[e]) {
-            if (e == kMostAlternatives || w.id[e] < 0) continue;
+        for (int e = rest > 0 ? w.head[tid] : -1; e >= 0; e = w.next[e]) {
+            if (e == kMostAlternatives || w.id[e] < 0) continue;   // (the taken token is no word of the teacher's)
             const int chunk = owner_of<E, NT>(sp, w.id[e]).chunk;
-            if (chunk == c) mask |= 1u << (w.id[e] - sp.head - c * E::VEC);
-            if (chunk > c) at = min(at, chunk);
+            if (chunk == c && chunk >= 0) mask |= 1u << (w.id[e] - sp.head - c * E::VEC);
+            if (chunk > c && chunk < rest) at = min(at, chunk);
         }
-        static_for<0, 4>([&](auto I) {
-            constexpr int i = decltype(I)::value;
-            if constexpr (E::VEC == 4) {
-                if (mask >> i & 1) x[i] = E::NOTHING;
-            } else {
-                if (mask >> (2 * i) & 1) x[i] = (x[i] & 0xffff0000u) | (E::NOTHING & 0xffffu);
-                if (mask >> (2 * i + 1) & 1) x[i] = (x[i] & 0xffffu) | (E::NOTHING & 0xffff0000u);
-            }
-        });
+        return mask;
     }
 };
 
 // Dense part of the gradient: e (a - b (x - mean)), with x = (l - m) k and e = 2^x.
 struct Dense {
-    float m, k, a, b, mean;
+    float a, b, mean;
     template <bool ENTROPY>
-    __device__ __forceinline__ float of(float l) const {
-        const float x = (l - m) * k, e = __builtin_amdgcn_exp2f(x);
-        if (!ENTROPY) return e * a;
-        return e * (a - b * (fmaxf(x, kNoExponent) - mean));
+    __device__ __forceinline__ float at(float x) const {
+        const float e = __builtin_amdgcn_exp2f(x);
+        return ENTROPY ? e * (a - b * (fmaxf(x, kNoExponent) - mean)) : e * a;
     }
 };
+// Its chunks; `p` as they were summed.
 template <class E, int NT, bool ENTROPY, int C>
-__device__ __forceinline__ void store_dense(const u32x4 (&x)[C], char* out, const RowSpan& sp, const Dense& d, int first) {
+__device__ __forceinline__ void store_dense(const u32x4 (&x)[C], char* out, const RowSpan& sp, const Dense& d, const Exponent& p, int first) {
     u32x4_any* to = reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES);
-    static_for<0, C>([&](auto I) {
-        constexpr int i = decltype(I)::value;
-        const int at = first + i * NT;
-        if (at < sp.chunks) {
-            float v[E::VEC];
-            static_for<0, E::VEC>([&](auto J) { v[decltype(J)::value] = d.of<ENTROPY>(E::template get<decltype(J)::value>(x[i])); });
-            __builtin_nontemporal_store(E::pack(v), to + at);
-        }
-    });
+    const float f = __builtin_amdgcn_exp2f(-p.off);
+    const Dense here{d.a * f, d.b * f, d.mean + p.off};
+    auto all = [&](auto far) {
+        static_for<0, C>([&](auto I) {
+            constexpr int i = decltype(I)::value;
+            const int at = first + i * NT;
+            if (at < sp.chunks) {
+                float v[E::VEC];
+                static_for<0, E::VEC>([&](auto J) {
+                    v[decltype(J)::value] = here.at<ENTROPY>(p.of<decltype(far)::value>(E::template get<decltype(J)::value>(x[i])));
+                });
+                __builtin_nontemporal_store(E::pack(v), to + at);
+            }
+        });
+    };
+    if (p.far) all(std::true_type{});
+    else all(std::false_type{});
 }
 
+// Over a wave, in every lane.
 __device__ __forceinline__ double sum_wave(double x) {
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-    return x;
+    x = wave_sum_to_lane63(x);
+    const unsigned long long b = (unsigned long long)__double_as_longlong(x);
+    const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63), high = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63);
+    return __longlong_as_double((long long)((unsigned long long)high << 32 | low));
 }
 
-// What the first wave hands to the others.
-struct RowNumbers {
-    float a, b, mean;
-};
-
-// What the first wave knows of its row before the row's sums do: sum of the teacher's shares, of the derivatives, and the entry that stands for the
-// taken token (-1: none is taken).
-struct Prelude {
-    double sum;
-    int taken;
-};
+// e^x in 64 bits: n log 2 taken out, then the series up to the twelfth power, which at most log 2 / 2 leaves 2e-16 of.
+__device__ __forceinline__ double exp_of(double x) {
+    x = x < -760.0 ? -760.0 : x > 760.0 ? 760.0 : x;
+    const double n = rint(x * 1.4426950408889634), y = __builtin_fma(-n, 0.69314718055994531, x);
+    double r = 1.0 / 479001600.0;
+    constexpr double c[12] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880, 1.0 / 3628800, 1.0 / 39916800};
+#pragma unroll
+    for (int i = 11; i >= 0; --i) r = __builtin_fma(r, y, c[i]);
+    return ldexp(r, (int)n);
+}
+// log v: of the mantissa in fp32, then one step of Newton's, which squares its error.
+__device__ __forceinline__ double log_of(double v) {
+    int n;
+    const double f = frexp(v, &n), near = (double)logf((float)f) + n * 0.69314718055994531;
+    return v > 0.0 && v < INFINITY ? near + (v * exp_of(-near) - 1.0) : near;
+}
 
 // Puts the list together: entries `lane`, 64 + lane and the taken token.
-template <class E, int NT, Listed WORK>
-__device__ __forceinline__ Prelude list_words(const ListedArgs& a, WordList<NT>& w, const RowSpan& sp, const char* row, int64_t t, int64_t y) {
+template <class E, int NT, Listed WORK, class Words>
+__device__ __forceinline__ void list_words(const ListedArgs& a, Words& w, const RowSpan& sp, const char* row, int64_t t, int64_t y, int rest) {
     const int lane = threadIdx.x, n = a.words.k;
-    for (int i = lane; i < NT; i += 64) w.head[i] = -1;
+    float logit[2] = {-INFINITY, -INFINITY}, number[2] = {0.f, 0.f};
 #pragma unroll
-    for (int e = lane; e < kEntries; e += 64) {
-        const int64_t id = e < n ? a.words.ids[t * n + e] : (e == kMostAlternatives ? y : -1);
+    for (int i = 0; i < 2; ++i) {
+        const int e = lane + 64 * i;
+        const int64_t id = e < n ? a.words.ids[t * n + e] : -1;
         const bool there = id >= 0 && id < sp.V;
         w.id[e] = there ? (int)id : -1;
-        if (there) w.logit[e] = E::one(row, id);
+        if (there) logit[i] = E::one(row, id);
+        if (there) number[i] = WORK == Listed::Distill ? a.words.logp[t * n + e] : a.dtop[t * n + e];
+    }
+    if (lane == 0) {
+        w.id[kMostAlternatives] = y >= 0 && y < sp.V ? (int)y : -1;
+        w.logit[kMostAlternatives] = y >= 0 && y < sp.V ? E::one(row, y) : 0.f;
+    }
+    for (int i = lane; i < NT; i += 64) w.head[i] = -1;
+    if (WORK == Listed::Distill) {
+        for (int i = lane; i < NT * Words::MARKS / 4; i += 64) reinterpret_cast<u32x4*>(w.marks)[i] = u32x4{0, 0, 0, 0};
+        if (lane < 4) w.edge_marks[lane] = 0;
     }
     wave_order();
     for (int e = lane; e < kEntries; e += 64)
-        if (w.id[e] >= 0) w.next[e] = atomicExch(&w.head[owner_of<E, NT>(sp, w.id[e]).thread], e);
+        if (w.id[e] >= 0) {
+            const Owner o = owner_of<E, NT>(sp, w.id[e]);
+            w.next[e] = atomicExch(&w.head[o.thread], e);
+            if (WORK == Listed::Distill && e != kMostAlternatives) {
+                const int turn = (o.chunk - rest) / NT;
+                if (o.chunk >= rest)
+                    atomicOr(&w.marks[o.thread * Words::MARKS + turn / 4], 1u << (8 * (turn % 4) + (w.id[e] - sp.head) % E::VEC));
+                else if (o.chunk < 0)
+                    atomicOr(&w.edge_marks[o.thread / 32], 1u << (o.thread % 32));
+            }
+        }
     wave_order();
-    const int first = first_of<E, NT>(w, sp, lane), second = first_of<E, NT>(w, sp, 64 + lane), taken = first_of<E, NT>(w, sp, kMostAlternatives);
+    const int first[2] = {first_of<E, NT>(w, sp, lane), first_of<E, NT>(w, sp, 64 + lane)}, taken = first_of<E, NT>(w, sp, kMostAlternatives);
     wave_order();
-    const bool again[2] = {first >= 0 && first != lane, second >= 0 && second != 64 + lane};
+    const bool live[2] = {first[0] == lane, first[1] == 64 + lane};
+    const bool again[2] = {first[0] >= 0 && !live[0], first[1] >= 0 && !live[1]};
     if (again[0]) w.id[lane] = -1;
     if (again[1]) w.id[64 + lane] = -1;
     if (taken != kMostAlternatives && lane == 0) w.id[kMostAlternatives] = -1;
-    Prelude p{0.0, taken};
+    w.logit[lane] = logit[0];
+    w.logit[64 + lane] = logit[1];
+    Prelude p{0.0, 0.0, -INFINITY, taken};
     if constexpr (WORK == Listed::Distill) {
-#pragma unroll 1
-        for (int e = lane; e < kMostAlternatives; e += 64) {
-            const bool live = e < 64 ? first == e : second == e;
-            const float log_q = live ? a.words.logp[t * n + e] : -INFINITY;
-            const double q = exp((double)log_q);
-            w.log_q[e] = log_q;
+        const double inv_t = (double)a.l.inv_t + a.l.inv_t_low;
+        p.most = fmaxf(live[0] ? logit[0] : -INFINITY, live[1] ? logit[1] : -INFINITY);
+        p.most = fold_wave<64>(p.most, [](float x, float z) { return fmaxf(x, z); });
+        const double base = p.most == -INFINITY ? 0.0 : (double)p.most;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int e = lane + 64 * i;
+            if (!live[i]) number[i] = -INFINITY;
+            const double q = number[i] == -INFINITY ? 0.0 : exp_of((double)number[i]);
+            w.log_q[e] = number[i];
             w.q[e] = (float)q;
             p.sum += q;
+            if (live[i] && logit[i] != -INFINITY) p.named += exp_of(((double)logit[i] - base) * inv_t);   // (+inf, NaN: NaN)
+            if (n <= 64) {
+                w.log_q[64 + e] = -INFINITY;
+                w.q[64 + e] = 0.f;
+                break;
+            }
         }
         p.sum = sum_wave(p.sum);
+        p.named = sum_wave(p.named);
     } else {
         // derivatives by the words' log-probabilities, equal words' added in the order of the entries, to `q`
         const float inv_t = a.l.inv_t;
-        double mine[2] = {0.0, 0.0};
-        if (first >= 0) mine[0] = (double)a.dtop[t * n + lane];
-        if (second >= 0) mine[1] = (double)a.dtop[t * n + 64 + lane];
+        double mine[2] = {first[0] >= 0 ? (double)number[0] : 0.0, first[1] >= 0 ? (double)number[1] : 0.0};
         p.sum = sum_wave(mine[0] + mine[1]);
         if (__any(again[0] || again[1])) {
             for (int f = 1; f < n; ++f) {
-                const int same = f < 64 ? __shfl(first, f) : __shfl(second, f - 64);
-                const double d = f < 64 ? __shfl(mine[0], f) : __shfl(mine[1], f - 64);
+                const int same = f < 64 ? __shfl(first[0], f) : __shfl(first[1], f - 64);
+                const double d = (double)(f < 64 ? __shfl(number[0], f) : __shfl(number[1], f - 64));
                 if (same != f && same == lane) mine[0] += d;
                 if (same != f && same == 64 + lane) mine[1] += d;
             }
@@ -209,13 +267,7 @@ __device__ __forceinline__ Prelude list_words(const ListedArgs& a, WordList<NT>&
         w.q[lane] = (float)((mine[0] + (taken == lane ? dy : 0.0)) * inv_t);
         w.q[64 + lane] = (float)((mine[1] + (taken == 64 + lane ? dy : 0.0)) * inv_t);
     }
-    return p;
-}
-
-// e^x to the accuracy of fp32, of any x.
-__device__ __forceinline__ double near_exp(double x) {
-    const double z = fmax(x * 1.4426950408889634, -2000.0), n = rint(z);   // (NaN is dropped: whoever sums these sums the row's own as well)
-    return ldexp((double)__builtin_amdgcn_exp2f((float)(z - n)), (int)n);
+    if (lane == 0) w.given = p;
 }
 
 // q f(log p - log q), f(d) = e^d - d - 1, with d = log p - log q.
@@ -224,83 +276,81 @@ __device__ __forceinline__ double divergence_term(double q, double d, double p) 
     return fabs(d) < 0.25 ? q * (double)kl_of((float)d, 0.f) : p - q - q * d;
 }
 
-// Numbers of the distillation loss, from the maximum m and sum s of the words that are not named.
-template <int NT>
-__device__ __forceinline__ RowNumbers distill_words(const ListedArgs& a, WordList<NT>& w, const Prelude& given, int64_t t, float m, float s) {
-    const int lane = threadIdx.x, taken = given.taken;
-    const double weight = a.l.weights ? (double)a.l.weights[t] : 1.0, inv_t = (double)a.l.inv_t + a.l.inv_t_low, base = m == -INFINITY ? 0.f : m;
-    float most = m;
-    for (int e = lane; e < kMostAlternatives; e += 64)
-        if (w.id[e] >= 0) most = fmaxf(most, w.logit[e]);
-    most = fold_wave<64>(most, [](float p, float q) { return fmaxf(p, q); });
-    const double whole_base = most == -INFINITY ? 0.f : most;
-    // the sum over all words, relative to the largest: of the named ones, and of the rest (which without any word is 0)
-    double named = 0.0;
-    float sure = 0.f;   // NaN if a named word's logit is
-    for (int e = lane; e < kMostAlternatives; e += 64)
-        if (w.id[e] >= 0) {
-            named += near_exp(((double)w.logit[e] - whole_base) * inv_t);
-            sure += w.logit[e] - w.logit[e] == 0.f || w.logit[e] == -INFINITY ? 0.f : NAN;
+// A row of the distillation loss, from the maximum m and sum s of the words that are not named.
+struct Distilled {
+    double base, all;         // the largest logit, and the sum over all words of exp(z - that one's)
+    double down;              // exp of m's distance from it
+    double divide, whole, left, c, slope;
+    bool rest;                // whether there are words that are not named
+    __device__ __forceinline__ Distilled(const ListedArgs& a, const Prelude& given, double weight, float m, float s) {
+        const double inv_t = (double)a.l.inv_t + a.l.inv_t_low, most = given.most;
+        const bool named_lead = given.most > m;
+        rest = !(s == 0.f);
+        base = named_lead ? most : m == -INFINITY ? 0.0 : (double)m;
+        const double apart = rest && given.named != 0.0 ? exp_of((named_lead ? (double)m - most : most - (double)m) * inv_t) : 0.0;
+        down = !rest ? 0.0 : named_lead ? apart : 1.0;
+        all = given.named * (named_lead ? 1.0 : rest ? apart : 1.0) + (rest ? s * down : 0.0);
+        const double none = all > 0.0 && all < INFINITY ? 0.0 : NAN;   // NaN: a row without probabilities
+        double share = given.sum;
+        left = 0.0, divide = 1.0;
+        if (a.distill.renormalise) {
+            divide = share;
+            share = share == 0.0 ? 0.0 : share / share;
+        } else if (rest) {
+            left = share < 1.0 ? 1.0 - share : share - share;   // (0, or NaN)
         }
-    named = sum_wave(named + (double)sure);
-    const bool rest = !(s == 0.f);
-    const double down = rest ? near_exp((base - whole_base) * inv_t) : 0.0, all = named + (rest ? s * down : 0.0);
-    const double none = all > 0.0 && all < INFINITY ? 0.0 : NAN;   // NaN: a row without probabilities
-    double share = given.sum, left = 0.0, divide = 1.0;
-    if (a.distill.renormalise) {
-        divide = share;
-        share = share == 0.0 ? 0.0 : share / share;
-    } else if (rest) {
-        left = share < 1.0 ? 1.0 - share : share - share;   // (0, or NaN)
+        whole = share + left;
+        c = (double)a.distill.scale * weight * inv_t + none;
+        // of the rest e (c (Q + ce) / sum of all - c q_r / sum of the rest)
+        slope = rest ? c * ((whole + a.distill.ce) * down / all - left / s) : none;
     }
-    const double logs = log(lane == 0 ? all : lane == 1 ? (double)s : lane == 2 ? left : divide);
+};
+
+// The named words' numbers, c ((Q + ce) p - q - ce [taken]), and the row's loss, by the first wave.
+template <class Words>
+__device__ __forceinline__ void distill_words(const ListedArgs& a, Words& w, const Distilled& d, int64_t t, float m, float s) {
+    const int lane = threadIdx.x, taken = w.given.taken;
+    const double inv_t = (double)a.l.inv_t + a.l.inv_t_low, ce = a.distill.ce;
+    const double logs = log_of(lane == 0 ? d.all : lane == 1 ? (double)s : lane == 2 ? d.left : d.divide);
     const double log_all = __shfl(logs, 0), log_s = __shfl(logs, 1), log_left = __shfl(logs, 2), shift = a.distill.renormalise ? __shfl(logs, 3) : 0.0;
-    // the row's loss, and at the named words c ((Q + ce) p - q - ce [taken])
-    const double whole = share + left, ce = a.distill.ce, c = (double)a.distill.scale * weight * inv_t + none;
     double kl = 0.0;
 #pragma unroll 1
     for (int e = lane; e < kMostAlternatives; e += 64) {
         if (w.id[e] < 0) continue;
-        const double log_p = ((double)w.logit[e] - whole_base) * inv_t - log_all, p = exp(log_p);
-        const double q = w.q[e] == 0.f ? 0.0 : w.q[e] / divide;
+        const double log_p = ((double)w.logit[e] - d.base) * inv_t - log_all, p = w.logit[e] == -INFINITY ? 0.0 : exp_of(log_p);
+        const double q = w.q[e] == 0.f ? 0.0 : w.q[e] / d.divide;
         kl += divergence_term(q, log_p - (w.log_q[e] - shift), p);
-        w.value[e] = (float)(c * ((whole + ce) * p - q - (taken == e ? ce : 0.0)));
+        w.value[e] = (float)(d.c * ((d.whole + ce) * p - q - (taken == e ? ce : 0.0)));
     }
     kl = sum_wave(kl);
-    if (rest) kl += divergence_term(left, log_s + (base - whole_base) * inv_t - log_all - log_left, s * down / all);
-    kl = (whole == 0.0 ? 0.0 : kl + (whole - 1.0)) + none;     // (a teacher that says nothing costs nothing)
-    // of the rest e (c (Q + ce) / sum of all - c q_r / sum of the rest)
-    const double slope = rest ? c * ((whole + ce) * down / all - left / s) : none;
-    const double ly = taken >= 0 ? (double)w.logit[kMostAlternatives] : 0.0, nll = taken >= 0 ? log_all - (ly - whole_base) * inv_t : 0.0;
+    const double base = m == -INFINITY ? 0.0 : (double)m, none = d.all > 0.0 && d.all < INFINITY ? 0.0 : NAN;
+    if (d.rest) kl += divergence_term(d.left, log_s + (base - d.base) * inv_t - log_all - log_left, s * d.down / d.all);
+    kl = (d.whole == 0.0 ? 0.0 : kl + (d.whole - 1.0)) + none;     // (a teacher that says nothing costs nothing)
     if (lane == 0) {
-        w.value[kMostAlternatives] = (float)(slope * (rest ? exp((ly - base) * inv_t) : 0.0) - c * ce);
+        const double ly = taken >= 0 ? (double)w.logit[kMostAlternatives] : 0.0;
+        w.value[kMostAlternatives] = (float)(d.slope * (d.rest ? exp_of((ly - base) * inv_t) : 0.0) - d.c * ce);
         if (a.kl) a.kl[t] = (float)kl;
         a.terms[2 * t] = kl;
-        a.terms[2 * t + 1] = nll;
+        a.terms[2 * t + 1] = taken >= 0 ? log_all - (ly - d.base) * inv_t : 0.0;
     }
-    return RowNumbers{(float)slope, 0.f, 0.f};
 }
 
-// Numbers of a function of the alternatives, from the maximum m, sum s and sum of e_j x_j of all words.
-template <int NT, bool ENTROPY>
-__device__ __forceinline__ RowNumbers alternatives_words(const ListedArgs& a, WordList<NT>& w, const Prelude& given, int64_t t, float m, float s, float sx) {
+// The same of a function of the alternatives.
+template <bool ENTROPY, class Words>
+__device__ __forceinline__ void alternatives_words(const ListedArgs& a, Words& w, const Dense& dense, int64_t t, const Exponent& p) {
     const int lane = threadIdx.x;
-    const double inv_t = (double)a.l.inv_t + a.l.inv_t_low;
-    const double slope = ENTROPY ? (double)a.dentropy[t] * 0.693147180559945309 * inv_t / s : 0.0;
-    const Dense dense{m == -INFINITY ? 0.f : m, a.l.k, (float)(-given.sum * inv_t / s), (float)slope, ENTROPY ? sx / s : 0.f};
     for (int e = lane; e < kMostAlternatives; e += 64)
-        if (w.id[e] >= 0) w.value[e] = dense.of<ENTROPY>(w.logit[e]) + w.q[e];
+        if (w.id[e] >= 0) w.value[e] = dense.at<ENTROPY>((w.logit[e] - p.m) * p.k) + w.q[e];
     if (lane == 0 && w.id[kMostAlternatives] >= 0)
-        w.value[kMostAlternatives] = dense.of<ENTROPY>(w.logit[kMostAlternatives]) + (a.dlogp ? a.dlogp[t] * a.l.inv_t : 0.f);
-    return RowNumbers{dense.a, dense.b, dense.mean};
+        w.value[kMostAlternatives] = dense.at<ENTROPY>((w.logit[kMostAlternatives] - p.m) * p.k) + (a.dlogp ? a.dlogp[t] * a.l.inv_t : 0.f);
 }
 
 // A workgroup a row; the last H chunks a thread stay in registers, those before are read a second time, from their end.
 template <class E, int NT, int H, Listed WORK, bool ENTROPY>
 __global__ __launch_bounds__(NT, NT >= 512 ? 4 : 5) void listed_kernel(const ListedArgs a) {
-    __shared__ WordList<NT> w;
+    typedef WordList<NT, H> Words;
+    __shared__ Words w;
     __shared__ float shared[3][NT / 64];
-    __shared__ RowNumbers numbers;
     const int V = (int)a.l.vocab, tid = threadIdx.x;
     if (a.ticket && blockIdx.x == 0 && tid == 0) *a.ticket = 0u;
     const int64_t t = a.first + (NT >= 512 ? die_run(blockIdx.x) : (int64_t)blockIdx.x), y = a.l.targets ? a.l.targets[t] : -1;
@@ -320,66 +370,79 @@ __global__ __launch_bounds__(NT, NT >= 512 ? 4 : 5) void listed_kernel(const Lis
     u32x4 x[H];
     load_chunks<E, NT>(x, row, sp, rest + tid);
     const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
-    Prelude given{0.0, -1};
-    if (tid < 64) given = list_words<E, NT, WORK>(a, w, sp, row, t, y);
+    if (tid < 64) list_words<E, NT, WORK>(a, w, sp, row, t, y, rest);
     __syncthreads();
 
     Seen seen{-INFINITY, 0.f, 0.f};
     float edge_left = edge;
     RowSpan before = sp;
     before.chunks = rest;
-    {
-        LeftOut<E, NT> left(w, sp, tid);
-        if (WORK == Listed::Alternatives) left.at = 0x7fffffff;
-        else if (left.edge) edge_left = -INFINITY;
+    if constexpr (WORK == Listed::Distill) {
+        LeftOut<E, NT, Words> left(w, sp, tid, rest);
+        if (tid < sp.edge && (w.edge_marks[tid / 32] >> (tid % 32) & 1)) edge_left = -INFINITY;
         for (int c = tid; c < rest; c += 4 * NT) {
             u32x4 z[4];
             load_chunks<E, NT, Reading::Again>(z, row, before, c);
             static_for<0, 4>([&](auto I) {
                 constexpr int i = decltype(I)::value;
-                if (WORK == Listed::Distill && c + i * NT == left.at && c + i * NT < rest) left.take(z[i], c + i * NT);
+                if (c + i * NT == left.at) take_out<E>(z[i], left.find(c + i * NT));
             });
             see_chunks<E, ENTROPY>(seen, z, k);
         }
-        static_for<0, H>([&](auto I) {
-            constexpr int i = decltype(I)::value;
-            if (WORK == Listed::Distill && rest + tid + i * NT == left.at) left.take(x[i], rest + tid + i * NT);
+        static_for<0, Words::MARKS>([&](auto G) {
+            constexpr int g = decltype(G)::value;
+            const uint32_t marks = w.marks[tid * Words::MARKS + g];
+            if (__any(marks != 0))
+                static_for<0, (H - 4 * g < 4 ? H - 4 * g : 4)>([&](auto I) {
+                    constexpr int i = decltype(I)::value;
+                    const uint32_t mask = marks >> (8 * i) & 255;
+                    if (__any(mask != 0)) take_out<E>(x[4 * g + i], mask);
+                });
         });
+    } else {
+        for (int c = tid; c < rest; c += 4 * NT) {
+            u32x4 z[4];
+            load_chunks<E, NT, Reading::Again>(z, row, before, c);
+            see_chunks<E, ENTROPY>(seen, z, k);
+        }
     }
     const float most = max_of<E>(x, fmaxf(seen.m, edge_left));
     keep_packed(x);
     const float m = fold_row<NT>(most, shared[0], [](float p, float q) { return fmaxf(p, q); });
     see_max<ENTROPY>(seen, m, k);
-    see<ENTROPY>(seen, edge_left, k);
-    static_for<0, H>([&](auto I) {
-        static_for<0, E::VEC>([&](auto J) { see<ENTROPY>(seen, E::template get<decltype(J)::value>(x[decltype(I)::value]), k); });
-        // (a chunk after the other: the compiler would put a sum off to where it is used, and keep all of its terms till then)
-        asm volatile("" : "+v"(seen.s), "+v"(seen.w));
-    });
+    const Exponent p = exponent_of(m, k);
+    see_held<E, ENTROPY>(seen, x, edge_left, p);
     keep_packed(x);
     auto plus = [](float p, float q) { return p + q; };
     const float s = fold_row<NT>(seen.s, shared[1], plus);
     const float sx = ENTROPY ? fold_row<NT>(seen.w, shared[2], plus) : 0.f;
 
-    if (tid < 64) {
-        RowNumbers r;
-        if constexpr (WORK == Listed::Distill) r = distill_words<NT>(a, w, given, t, m, s);
-        else r = alternatives_words<NT, ENTROPY>(a, w, given, t, m, s, sx);
-        if (tid == 0) numbers = r;
+    const Prelude given = w.given;
+    auto finish = [&](const Dense& dense) {
+        keep_packed(x);
+        int mine = tid;
+        asm volatile("" : "+v"(mine));   // (the addresses are formed again: kept since the loads, they would not fit the registers)
+        store_dense<E, NT, ENTROPY>(x, out, sp, dense, p, rest + mine);
+        for (int first = (rest - 1) / (4 * NT) * (4 * NT); rest > 0 && first >= 0; first -= 4 * NT) {
+            u32x4 z[4];
+            load_chunks<E, NT>(z, row, before, first + tid);
+            store_dense<E, NT, ENTROPY>(z, out, before, dense, p, first + tid);
+        }
+        if (tid < sp.edge) E::put(out, sp.edge_element(tid), dense.at<ENTROPY>((edge - p.m) * k));
+    };
+    // (the list's numbers come behind the row's: the other waves write while the first one forms them)
+    if constexpr (WORK == Listed::Distill) {
+        const Distilled d(a, given, a.l.weights ? (double)a.l.weights[t] : 1.0, m, s);
+        if (out) finish(Dense{(float)d.slope, 0.f, 0.f});
+        if (tid < 64) distill_words(a, w, d, t, m, s);
+    } else {
+        const double inv_t = (double)a.l.inv_t + a.l.inv_t_low, slope = ENTROPY ? (double)a.dentropy[t] * 0.693147180559945309 * inv_t / s : 0.0;
+        const Dense dense{(float)(-given.sum * inv_t / s), (float)slope, ENTROPY ? sx / s : 0.f};
+        finish(dense);
+        if (tid < 64) alternatives_words<ENTROPY>(a, w, dense, t, p);
     }
-    __syncthreads();
     if (!out) return;
-    keep_packed(x);
-    int mine = tid;
-    asm volatile("" : "+v"(mine));   // (the addresses are formed again: kept since the loads, they would not fit the registers)
-    const Dense dense{m == -INFINITY ? 0.f : m, k, numbers.a, numbers.b, numbers.mean};
-    store_dense<E, NT, ENTROPY>(x, out, sp, dense, rest + mine);
-    for (int first = (rest - 1) / (4 * NT) * (4 * NT); rest > 0 && first >= 0; first -= 4 * NT) {
-        u32x4 z[4];
-        load_chunks<E, NT>(z, row, before, first + tid);
-        store_dense<E, NT, ENTROPY>(z, out, before, dense, first + tid);
-    }
-    if (tid < sp.edge) E::put(out, sp.edge_element(tid), dense.of<ENTROPY>(edge));
+    __syncthreads();
     // (a wave's own stores to one word keep their order)
     for (int e = w.head[tid]; e >= 0; e = w.next[e])
         if (w.id[e] >= 0) E::put(out, w.id[e], w.value[e]);

@@ -260,6 +260,45 @@ __device__ __forceinline__ void see_chunks(Seen& a, u32x4 (&x)[C], float k) {
     });
 }
 
+// x = (l - m) k as one multiply-add, l k - e with the whole number e = round(m k), where that loses nothing (is_far); it is `off` too large.
+struct Exponent {
+    float m, k, e, off;
+    bool far;
+    template <bool FAR>
+    __device__ __forceinline__ float of(float l) const {
+        return FAR ? (l - m) * k : __builtin_fmaf(l, k, -e);
+    }
+};
+__device__ __forceinline__ Exponent exponent_of(float m, float k) {
+    const bool far = is_far(m * k);
+    const float e = far ? 0.f : rintf(m * k);
+    return Exponent{m == -INFINITY ? 0.f : m, k, e, far ? 0.f : __builtin_fmaf(m, k, -e), far};
+}
+// Both have been formed here, for all that the compiler knows: it would put a sum off to where it is used, and keep all of its terms till then.
+__device__ __forceinline__ void pinned(float& s, float& w) { asm volatile("" : "+v"(s), "+v"(w)); }
+// Adds C chunks a thread and one element more, none of them above a.m.
+template <class E, bool ENTROPY, int C>
+__device__ __forceinline__ void see_held(Seen& a, const u32x4 (&x)[C], float more, const Exponent& p) {
+    float s = 0.f, w = 0.f;
+    auto all = [&](auto far) {
+        auto one = [&](float l) {
+            const float z = p.of<decltype(far)::value>(l), e = __builtin_amdgcn_exp2f(z);
+            s += e;
+            if (ENTROPY) w = __builtin_fmaf(e, fmaxf(z, kNoExponent), w);
+        };
+        one(more);
+        static_for<0, C>([&](auto I) {
+            static_for<0, E::VEC>([&](auto J) { one(E::template get<decltype(J)::value>(x[decltype(I)::value])); });
+            pinned(s, w);
+        });
+    };
+    if (p.far) all(std::true_type{});
+    else all(std::false_type{});
+    const float f = __builtin_amdgcn_exp2f(-p.off);
+    a.s += s * f;
+    if (ENTROPY) a.w += (w - p.off * s) * f;
+}
+
 // Workgroups go round the 8 dies; this gives each die a run of long rows of its own (8192 x 65536, bf16: 4 % faster, 16384 x
 // 32768: 7 %; rows of 16 KB and less are up to 5 % slower that way and stay in the order of the workgroups, as do rows whose number is no
 // multiple of 8).

@@ -43,16 +43,20 @@ __device__ __forceinline__ void for_elements(const char* row, const RowSpan& sp,
 }
 
 // Keys that a workgroup has put together, and the count of them (which may be more than there is room for).
-constexpr int kListed = 1024;
+template <int ROOM>
 struct KeyList {
     int count;
-    uint64_t key[kListed];
+    uint64_t key[ROOM];
+    __device__ __forceinline__ void put(uint64_t k) {
+        const int at = atomicAdd(&count, 1);
+        if (at < ROOM) key[at] = k;
+    }
 };
 
 // The k largest keys of the row, one digit of 8 bits at a time: a histogram of the keys that agree with the digits found so far, then the digit in
 // which the k-th lies.  Reads the row once a digit, and once more; ends where a digit leaves no choice.  Fewer than k if the row holds fewer.
-template <class E, int NT>
-__device__ void select_by_digits(const char* row, const RowSpan& sp, int k, KeyList& list, int (&bins)[256], int (&found)[2]) {
+template <class E, int NT, int ROOM>
+__device__ void select_by_digits(const char* row, const RowSpan& sp, int k, KeyList<ROOM>& list, int (&bins)[256], int (&found)[2]) {
     const int tid = threadIdx.x;
     uint64_t prefix = 0;   // digits found, the rest 0: in the end the k-th key
     int need = k;
@@ -82,7 +86,7 @@ __device__ void select_by_digits(const char* row, const RowSpan& sp, int k, KeyL
     __syncthreads();
     for_elements<E, NT>(row, sp, tid, [&](float v, int j) {
         const uint64_t key = key_of(order_of(v), j);
-        if (order_of(v) > kBanned && key >= prefix) list.key[atomicAdd(&list.count, 1)] = key;
+        if (order_of(v) > kBanned && key >= prefix) list.put(key);
     });
     __syncthreads();
 }
@@ -102,40 +106,105 @@ __device__ __forceinline__ float wave_max(float x) {
     x = dpp_max<0x143, 0xc>(x);
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
-// The r-th largest of the lanes' values.
-__device__ __forceinline__ float wave_rth(float x, int r) {
-    float m = wave_max(x);
-    for (; r > 1 && m > -INFINITY; --r) {
-        if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)__ballot(x == m)) - 1) x = -INFINITY;
-        m = wave_max(x);
-    }
-    return m;
-}
 
-// Puts the values of x that are no less than `least` on the list.  (A lane's largest value of a chunk tells first whether any is.)
-template <class E>
-__device__ __forceinline__ void list_chunk(KeyList& list, const u32x4& x, float least, int id) {
-    u32x4 one[1] = {x};
-    if (max_of<E>(one, -INFINITY) < least) return;
-    static_for<0, E::VEC>([&](auto J) {
-        const float v = E::template get<decltype(J)::value>(x);
-        if (v >= least) {
-            const int at = atomicAdd(&list.count, 1);
-            if (at < kListed) list.key[at] = key_of(order_of(v), id + decltype(J)::value);
+// Chunks that hold a value that may be an alternative, as they were read, and the ids of their first words.
+template <int ROOM>
+struct HotChunks {
+    u32x4 chunk[ROOM];
+    int id[ROOM], count;
+    __device__ __forceinline__ void put(bool hot, const u32x4& x, int first) {
+        const unsigned long long lanes = __ballot(hot);
+        if (lanes == 0) return;
+        const int leader = __ffsll(lanes) - 1;
+        int at = 0;
+        if ((int)(threadIdx.x & 63) == leader) at = atomicAdd(&count, __popcll(lanes));
+        at = __builtin_amdgcn_readlane(at, leader) + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0u));
+        if (hot && at < ROOM) {
+            chunk[at] = x;
+            id[at] = first;
         }
-    });
+    }
+};
+
+// How far values lie below the row's largest one, in steps of 1/32 of an octave from 2^-14 to 2^18 (what lies nearer or further: the first, the
+// last).  In such steps the k-th value's distance is found to 3 % at any scale of the logits.
+constexpr int kSteps = 1024;
+__device__ __forceinline__ int step_of(float distance) {
+    return min(max((int)(__float_as_uint(distance) >> 18) - ((127 - 14) << 5), 0), kSteps - 1);   // (NaN: the last)
+}
+// A little more than any distance of that step.
+__device__ __forceinline__ float beyond_step(int step) {
+    return step == kSteps - 1 ? INFINITY : __uint_as_float((uint32_t)(step + 1 + ((127 - 14) << 5)) << 18) * (1.f + 0x1p-20f);
 }
 
-// A workgroup a row.  Its first H chunks a thread are held in registers until their largest values are known, one a thread: of these the
-// `rank`-th of every wave, and of those the least, is no more than the k-th largest value of the row.  Words that reach it go on a list, which
-// holds the alternatives and little else (about 1.3 k words of a row held whole, more in proportion of one that is not), and a word's place among them is the
-// number of larger keys.  The rest of the row goes by once.  A row that has more such words than the list holds -- of equal values, or
-// rising ones -- is searched digit by digit.
+// A bound that at least k values of the row reach: the least of about the k largest of what the threads have seen at most, one value a thread, by a
+// histogram of their distances from the largest.  `most` becomes the workgroup's.  Ends with a barrier.
+template <int NT>
+__device__ __forceinline__ float bound_of(float& most, int k, float* shared, int (&steps)[kSteps], float& least) {
+    constexpr int WAVES = NT / 64;
+    const int tid = threadIdx.x;
+    const float mine = most, m = wave_max(mine);
+    if ((tid & 63) == 0) shared[tid >> 6] = m;
+    for (int i = tid; i < kSteps / 4; i += NT) reinterpret_cast<u32x4*>(steps)[i] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) most = fmaxf(most, shared[i]);
+    if (k == 0) return INFINITY;
+    atomicAdd(&steps[step_of(most - mine)], 1);
+    __syncthreads();
+    if (tid < 64) {
+        // 16 steps a lane, then the lane in which the k-th value lies, then the step
+        u32x4 n[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[i] = reinterpret_cast<const u32x4*>(steps)[4 * tid + i];
+        int own = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) own += (int)n[i / 4][i % 4];
+        int up_to = own;
+        for (int d = 1; d < 64; d *= 2) {
+            const int below = __shfl_up(up_to, d);
+            if (tid >= d) up_to += below;
+        }
+        if (up_to >= k && up_to - own < k) {   // (one lane: NT values, of which k is no more)
+            int sum = up_to - own, step = -1;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (step < 0 && sum + (int)n[i / 4][i % 4] >= k) step = i;
+                sum += (int)n[i / 4][i % 4];
+            }
+            least = fmaxf(most - beyond_step(16 * tid + step), -3.402823466e38f);   // (banned words are no alternatives)
+        }
+    }
+    __syncthreads();
+    return least;
+}
+
+// Sum over the workgroup, in a fixed order; every thread gets it.
+template <int WAVES>
+__device__ __forceinline__ float sum_group(float x, float* shared) {
+    x = wave_sum_to_lane63(x);
+    if ((threadIdx.x & 63) == 63) shared[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) x += shared[i];
+    return x;
+}
+
+// A workgroup a row.  Its first H chunks a thread are held in registers until their largest values are known, one a thread: the k-th largest
+// of these (or a little less) is no more than that of the row.  Chunks with a value that reaches it go on a list, their words that do on a second one, which holds the
+// alternatives and little else (about 1.1 k words of a row held whole, more in proportion of one that is not), and a word's place among
+// them is the number of larger keys.  The rest of the row goes by once.  A row that has more such words than the lists hold -- of equal
+// values, or rising ones -- is searched digit by digit.
 template <class E, int NT, int H, bool ENTROPY>
-__global__ __launch_bounds__(NT, 8) void top_kernel(const TopArgs a) {
-    __shared__ float shared[4][NT / 64];
-    __shared__ KeyList list;
-    __shared__ int bins[256], found[2];
+__global__ __launch_bounds__(NT, H == 16 ? 4 : 8) void top_kernel(const TopArgs a) {
+    constexpr int WAVES = NT / 64, CHUNKS = NT >= 512 ? 512 : 256, KEYS = 2 * CHUNKS;
+    __shared__ float shared[3][WAVES];
+    __shared__ __align__(16) int steps[kSteps];
+    __shared__ float bound;
+    __shared__ KeyList<KEYS> list;
+    __shared__ HotChunks<CHUNKS> hot;
+    __shared__ uint64_t sorted[kMostAlternatives];
     const int V = (int)a.l.vocab, tid = threadIdx.x;
     const int64_t t = a.first + (NT >= 512 ? die_run(blockIdx.x) : (int64_t)blockIdx.x), y = a.l.targets ? a.l.targets[t] : 0;
     int64_t* ids = a.ids + t * a.k;
@@ -159,63 +228,57 @@ __global__ __launch_bounds__(NT, 8) void top_kernel(const TopArgs a) {
     load_chunks<E, NT>(x, row, sp, tid);
     const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
     const float ly = E::one(row, y);
-    if (tid == 0) list.count = 0;
-    const float mine = max_of<E>(x, edge);
-    keep_packed(x);
-    const float rth = a.k ? wave_rth(mine, (a.k + NT / 64 - 1) / (NT / 64)) : INFINITY, most = wave_max(mine);
-    if ((tid & 63) == 0) {
-        shared[0][tid >> 6] = most;
-        shared[1][tid >> 6] = rth;
-    }
-    __syncthreads();
-    Seen seen{-INFINITY, 0.f, 0.f};
-    float least = shared[1][0];
-#pragma unroll
-    for (int i = 0; i < NT / 64; ++i) {
-        seen.m = fmaxf(seen.m, shared[0][i]);
-        least = fminf(least, shared[1][i]);
-    }
-    least = fmaxf(least, -3.402823466e38f);   // (banned words are no alternatives)
+    if (tid == 0) hot.count = list.count = 0;
+    float most_of[H], most = edge;
     static_for<0, H>([&](auto I) {
         constexpr int i = decltype(I)::value;
-        list_chunk<E>(list, x[i], least, sp.head + (tid + i * NT) * E::VEC);
+        const u32x4 one[1] = {x[i]};
+        most_of[i] = max_of<E>(one, -INFINITY);
+        most = fmaxf(most, most_of[i]);
     });
-    if (edge >= least) {
-        const int at = atomicAdd(&list.count, 1);
-        if (at < kListed) list.key[at] = key_of(order_of(edge), sp.edge_element(tid));
-    }
     keep_packed(x);
-    see<ENTROPY>(seen, edge, k);
+    const float least = bound_of<NT>(most, a.k, shared[0], steps, bound);
     static_for<0, H>([&](auto I) {
-        static_for<0, E::VEC>([&](auto J) { see<ENTROPY>(seen, E::template get<decltype(J)::value>(x[decltype(I)::value]), k); });
+        constexpr int i = decltype(I)::value;
+        hot.put(most_of[i] >= least, x[i], sp.head + (tid + i * NT) * E::VEC);
     });
+    Seen seen{most, 0.f, 0.f};
+    see_held<E, ENTROPY>(seen, x, edge, exponent_of(most, k));
     for (int c = tid + H * NT; c < sp.chunks; c += 4 * NT) {
         u32x4 z[4];
         load_chunks<E, NT>(z, row, sp, c);
-        const float m = max_of<E>(z, -INFINITY);
-        if (m >= least)
+        float m[4], of_all = -INFINITY;
+        static_for<0, 4>([&](auto I) {
+            constexpr int i = decltype(I)::value;
+            const u32x4 one[1] = {z[i]};
+            m[i] = max_of<E>(one, -INFINITY);
+            of_all = fmaxf(of_all, m[i]);
+        });
+        if (__any(of_all >= least))
             static_for<0, 4>([&](auto I) {
                 constexpr int i = decltype(I)::value;
-                list_chunk<E>(list, z[i], least, sp.head + (c + i * NT) * E::VEC);
+                hot.put(m[i] >= least, z[i], sp.head + (c + i * NT) * E::VEC);
             });
-        if (m > seen.m) see_max<ENTROPY>(seen, m, k);
+        if (of_all > seen.m) see_max<ENTROPY>(seen, of_all, k);
         static_for<0, 4>([&](auto I) {
             static_for<0, E::VEC>([&](auto J) { see<ENTROPY>(seen, E::template get<decltype(J)::value>(z[decltype(I)::value]), k); });
         });
     }
-    float m = seen.m;
+    float m = most;
     if (sp.chunks > H * NT) {
-        m = wave_max(m);
-        __syncthreads();
-        if ((tid & 63) == 0) shared[0][tid >> 6] = m;
+        m = wave_max(seen.m);
+        if ((tid & 63) == 0) shared[2][tid >> 6] = m;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < NT / 64; ++i) m = fmaxf(m, shared[0][i]);
+        for (int i = 0; i < WAVES; ++i) m = fmaxf(m, shared[2][i]);
         see_max<ENTROPY>(seen, m, k);
     }
-    auto plus = [](float p, float q) { return p + q; };
-    const float s = fold_row<NT>(seen.s, shared[2], plus), w = ENTROPY ? fold_row<NT>(seen.w, shared[3], plus) : 0.f;
-    const Two log_s = two_log(s);
+    float s = sum_group<WAVES>(seen.s, shared[0]), w = ENTROPY ? sum_group<WAVES>(seen.w, shared[1]) : 0.f;
+    // (the largest term is 1 and its x 0, which two exponentials that undo each other need not give: no log-probability is above 0, no entropy below)
+    s = s > 0.f && s < 1.f ? 1.f : s;
+    w = fminf(w, 0.f);
+    Two log_s{0.f, 0.f};
+    if (tid < kMostAlternatives) log_s = two_log(s);   // (the threads that write)
     if (tid == 0) {
         if (a.logp) a.logp[t] = add(scaled_difference(a.l, ly, m), log_s, -1.f).high;
         if (a.lse) a.lse[t] = add(scaled_difference(a.l, m, 0.f), log_s, 1.f).high;
@@ -223,20 +286,39 @@ __global__ __launch_bounds__(NT, 8) void top_kernel(const TopArgs a) {
     }
     if (a.k == 0) return;
     const bool there = s > 0.f && s < INFINITY;   // (a row of NaN, +inf or nothing but -inf has no alternatives)
-    if (there && list.count > kListed) {
+    int n = 0;
+    if (there) {
+        const int chunks = hot.count;   // (a barrier lies behind the last one that was put)
+        for (int i = tid; i < min(chunks, CHUNKS) * E::VEC; i += NT) {
+            const float v = E::one(&hot.chunk[i / E::VEC], i % E::VEC);
+            if (v >= least) list.put(key_of(order_of(v), hot.id[i / E::VEC] + i % E::VEC));
+        }
+        if (edge >= least) list.put(key_of(order_of(edge), sp.edge_element(tid)));
         __syncthreads();
-        select_by_digits<E, NT>(row, sp, a.k, list, bins, found);
+        n = list.count;
+        if (chunks > CHUNKS || n > KEYS) {
+            __syncthreads();
+            select_by_digits<E, NT>(row, sp, a.k, list, *reinterpret_cast<int(*)[256]>(steps), *reinterpret_cast<int(*)[2]>(steps + 256));
+            n = list.count;
+        }
+        // four threads a key, a quarter of the others each
+        for (int first = (tid & ~63) / 4; first < n; first += NT / 4) {
+            const int e = first + (tid & 63) / 4;
+            const uint64_t key = e < n ? list.key[e] : ~0ull;
+            int place = 0;
+            for (int i = tid % 4; i < n; i += 4) place += list.key[i] > key;
+            place += __builtin_amdgcn_update_dpp(0, place, 0xB1, 0xf, 0xf, false);
+            place += __builtin_amdgcn_update_dpp(0, place, 0x4E, 0xf, 0xf, false);
+            if (e < n && place < a.k && tid % 4 == 0) sorted[place] = key;
+        }
+        n = min(n, a.k);
     }
-    const int listed = there ? list.count : 0, n = min(listed, a.k);
-    for (int e = tid; e < listed; e += NT) {
-        const uint64_t key = list.key[e];
-        int rank = 0;
-        for (int i = 0; i < listed; ++i) rank += list.key[i] > key;
-        if (rank >= a.k) continue;
-        ids[rank] = (int64_t)(uint32_t)~(uint32_t)key;
-        top[rank] = add(scaled_difference(a.l, value_of((uint32_t)(key >> 32)), m), log_s, -1.f).high;
-    }
-    if (tid >= n && tid < a.k) {
+    __syncthreads();
+    if (tid < n) {
+        const uint64_t key = sorted[tid];
+        ids[tid] = (int64_t)(uint32_t)~(uint32_t)key;
+        top[tid] = add(scaled_difference(a.l, value_of((uint32_t)(key >> 32)), m), log_s, -1.f).high;
+    } else if (tid < a.k) {
         ids[tid] = -1;
         top[tid] = there ? -INFINITY : NAN;
     }
@@ -248,7 +330,7 @@ void launch_top_of(const TopArgs& a, unsigned rows, hipStream_t stream) {
     if (chunks <= 512) top_kernel<E, 256, 2, ENTROPY><<<rows, 256, 0, stream>>>(a);
     else if (chunks <= 2048) top_kernel<E, 256, 8, ENTROPY><<<rows, 256, 0, stream>>>(a);
     else if (chunks <= 4096) top_kernel<E, 1024, 4, ENTROPY><<<rows, 1024, 0, stream>>>(a);
-    else top_kernel<E, 1024, 8, ENTROPY><<<rows, 1024, 0, stream>>>(a);
+    else top_kernel<E, 512, 16, ENTROPY><<<rows, 512, 0, stream>>>(a);
 }
 
 }  // namespace
