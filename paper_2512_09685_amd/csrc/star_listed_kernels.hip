@@ -134,11 +134,12 @@ struct Dense {
 };
 // Its chunks; `p` as they were summed.
 template <class E, int NT, bool ENTROPY, int C>
-__device__ __forceinline__ void store_dense(const u32x4 (&x)[C], char* out, const RowSpan& sp, const Dense& d, const Exponent& p, int first) {
+__device__ __forceinline__ void store_dense(u32x4 (&x)[C], char* out, const RowSpan& sp, const Dense& d, const Exponent& p, int first) {
     u32x4_any* to = reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES);
     const float f = __builtin_amdgcn_exp2f(-p.off);
     const Dense here{d.a * f, d.b * f, d.mean + p.off};
     auto all = [&](auto far) {
+        keep_packed(x);
         static_for<0, C>([&](auto I) {
             constexpr int i = decltype(I)::value;
             const int at = first + i * NT;

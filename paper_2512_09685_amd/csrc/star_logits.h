@@ -278,9 +278,10 @@ __device__ __forceinline__ Exponent exponent_of(float m, float k) {
 __device__ __forceinline__ void pinned(float& s, float& w) { asm volatile("" : "+v"(s), "+v"(w)); }
 // Adds C chunks a thread and one element more, none of them above a.m.
 template <class E, bool ENTROPY, int C>
-__device__ __forceinline__ void see_held(Seen& a, const u32x4 (&x)[C], float more, const Exponent& p) {
+__device__ __forceinline__ void see_held(Seen& a, u32x4 (&x)[C], float more, const Exponent& p) {
     float s = 0.f, w = 0.f;
     auto all = [&](auto far) {
+        keep_packed(x);   // (or elements would be widened for both ways at once)
         auto one = [&](float l) {
             const float z = p.of<decltype(far)::value>(l), e = __builtin_amdgcn_exp2f(z);
             s += e;

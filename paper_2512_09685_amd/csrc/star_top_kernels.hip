@@ -197,7 +197,7 @@ __device__ __forceinline__ float sum_group(float x, float* shared) {
 // them is the number of larger keys.  The rest of the row goes by once.  A row that has more such words than the lists hold -- of equal
 // values, or rising ones -- is searched digit by digit.
 template <class E, int NT, int H, bool ENTROPY>
-__global__ __launch_bounds__(NT, H == 16 ? 4 : 8) void top_kernel(const TopArgs a) {
+__global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs a) {
     constexpr int WAVES = NT / 64, CHUNKS = NT >= 512 ? 512 : 256, KEYS = 2 * CHUNKS;
     __shared__ float shared[3][WAVES];
     __shared__ __align__(16) int steps[kSteps];
@@ -329,7 +329,7 @@ void launch_top_of(const TopArgs& a, unsigned rows, hipStream_t stream) {
     const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;
     if (chunks <= 512) top_kernel<E, 256, 2, ENTROPY><<<rows, 256, 0, stream>>>(a);
     else if (chunks <= 2048) top_kernel<E, 256, 8, ENTROPY><<<rows, 256, 0, stream>>>(a);
-    else if (chunks <= 4096) top_kernel<E, 1024, 4, ENTROPY><<<rows, 1024, 0, stream>>>(a);
+    else if (chunks <= 4096) top_kernel<E, 512, 8, ENTROPY><<<rows, 512, 0, stream>>>(a);
     else top_kernel<E, 512, 16, ENTROPY><<<rows, 512, 0, stream>>>(a);
 }
 
