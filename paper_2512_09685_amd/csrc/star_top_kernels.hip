@@ -107,22 +107,21 @@ __device__ __forceinline__ float wave_max(float x) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
-// Chunks that hold a value that may be an alternative, as they were read, and the ids of their first words.
-template <int ROOM>
+// A wave's chunks that hold a value that may be an alternative, as they were read, and the ids of their first words; `count` is the wave's, and may
+// be more than there is room for.
+constexpr int kHot = 128;
 struct HotChunks {
-    u32x4 chunk[ROOM];
-    int id[ROOM], count;
-    __device__ __forceinline__ void put(bool hot, const u32x4& x, int first) {
+    u32x4 chunk[kHot];
+    int id[kHot];
+    __device__ __forceinline__ void put(int& count, bool hot, const u32x4& x, int first) {
         const unsigned long long lanes = __ballot(hot);
         if (lanes == 0) return;
-        const int leader = __ffsll(lanes) - 1;
-        int at = 0;
-        if ((int)(threadIdx.x & 63) == leader) at = atomicAdd(&count, __popcll(lanes));
-        at = __builtin_amdgcn_readlane(at, leader) + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0u));
-        if (hot && at < ROOM) {
+        const int at = count + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0u));
+        if (hot && at < kHot) {
             chunk[at] = x;
             id[at] = first;
         }
+        count += __popcll(lanes);
     }
 };
 
@@ -198,12 +197,12 @@ __device__ __forceinline__ float sum_group(float x, float* shared) {
 // values, or rising ones -- is searched digit by digit.
 template <class E, int NT, int H, bool ENTROPY>
 __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs a) {
-    constexpr int WAVES = NT / 64, CHUNKS = NT >= 512 ? 512 : 256, KEYS = 2 * CHUNKS;
+    constexpr int WAVES = NT / 64, KEYS = NT >= 512 ? 1024 : 512, AHEAD = H == 16 && E::VEC == 8 ? 8 : 4;
     __shared__ float shared[3][WAVES];
     __shared__ __align__(16) int steps[kSteps];
     __shared__ float bound;
     __shared__ KeyList<KEYS> list;
-    __shared__ HotChunks<CHUNKS> hot;
+    __shared__ HotChunks hots[WAVES];
     __shared__ uint64_t sorted[kMostAlternatives];
     const int V = (int)a.l.vocab, tid = threadIdx.x;
     const int64_t t = a.first + (NT >= 512 ? die_run(blockIdx.x) : (int64_t)blockIdx.x), y = a.l.targets ? a.l.targets[t] : 0;
@@ -228,7 +227,9 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
     load_chunks<E, NT>(x, row, sp, tid);
     const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
     const float ly = E::one(row, y);
-    if (tid == 0) hot.count = list.count = 0;
+    if (tid == 0) list.count = 0;
+    HotChunks& hot = hots[tid >> 6];
+    int chunks = 0;   // of the wave's
     float most_of[H], most = edge;
     static_for<0, H>([&](auto I) {
         constexpr int i = decltype(I)::value;
@@ -240,27 +241,27 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
     const float least = bound_of<NT>(most, a.k, shared[0], steps, bound);
     static_for<0, H>([&](auto I) {
         constexpr int i = decltype(I)::value;
-        hot.put(most_of[i] >= least, x[i], sp.head + (tid + i * NT) * E::VEC);
+        hot.put(chunks, most_of[i] >= least, x[i], sp.head + (tid + i * NT) * E::VEC);
     });
     Seen seen{most, 0.f, 0.f};
     see_held<E, ENTROPY>(seen, x, edge, exponent_of(most, k));
-    for (int c = tid + H * NT; c < sp.chunks; c += 4 * NT) {
-        u32x4 z[4];
+    for (int c = tid + H * NT; c - tid < sp.chunks; c += AHEAD * NT) {   // (all of a wave, for its list)
+        u32x4 z[AHEAD];
         load_chunks<E, NT>(z, row, sp, c);
-        float m[4], of_all = -INFINITY;
-        static_for<0, 4>([&](auto I) {
+        float m[AHEAD], of_all = -INFINITY;
+        static_for<0, AHEAD>([&](auto I) {
             constexpr int i = decltype(I)::value;
             const u32x4 one[1] = {z[i]};
             m[i] = max_of<E>(one, -INFINITY);
             of_all = fmaxf(of_all, m[i]);
         });
         if (__any(of_all >= least))
-            static_for<0, 4>([&](auto I) {
+            static_for<0, AHEAD>([&](auto I) {
                 constexpr int i = decltype(I)::value;
-                hot.put(m[i] >= least, z[i], sp.head + (c + i * NT) * E::VEC);
+                hot.put(chunks, m[i] >= least, z[i], sp.head + (c + i * NT) * E::VEC);
             });
         if (of_all > seen.m) see_max<ENTROPY>(seen, of_all, k);
-        static_for<0, 4>([&](auto I) {
+        static_for<0, AHEAD>([&](auto I) {
             static_for<0, E::VEC>([&](auto J) { see<ENTROPY>(seen, E::template get<decltype(J)::value>(z[decltype(I)::value]), k); });
         });
     }
@@ -288,15 +289,24 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
     const bool there = s > 0.f && s < INFINITY;   // (a row of NaN, +inf or nothing but -inf has no alternatives)
     int n = 0;
     if (there) {
-        const int chunks = hot.count;   // (a barrier lies behind the last one that was put)
-        for (int i = tid; i < min(chunks, CHUNKS) * E::VEC; i += NT) {
-            const float v = E::one(&hot.chunk[i / E::VEC], i % E::VEC);
-            if (v >= least) list.put(key_of(order_of(v), hot.id[i / E::VEC] + i % E::VEC));
+        // every wave's own list; one that has run over leaves too many keys
+        if (chunks > kHot) {
+            if ((tid & 63) == 0) atomicAdd(&list.count, KEYS + 1);
+            chunks = 0;
+        }
+        for (int first = 0; first < chunks * E::VEC; first += 64) {
+            const int i = first + (tid & 63), in = min(i / E::VEC, kHot - 1);
+            const float v = i < chunks * E::VEC ? E::one(&hot.chunk[in], i % E::VEC) : -INFINITY;
+            const unsigned long long lanes = __ballot(v >= least);
+            int at = 0;
+            if ((tid & 63) == 0) at = atomicAdd(&list.count, __popcll(lanes));
+            at = __builtin_amdgcn_readlane(at, 0) + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0u));
+            if (v >= least && at < KEYS) list.key[at] = key_of(order_of(v), hot.id[in] + i % E::VEC);
         }
         if (edge >= least) list.put(key_of(order_of(edge), sp.edge_element(tid)));
         __syncthreads();
         n = list.count;
-        if (chunks > CHUNKS || n > KEYS) {
+        if (n > KEYS) {
             __syncthreads();
             select_by_digits<E, NT>(row, sp, a.k, list, *reinterpret_cast<int(*)[256]>(steps), *reinterpret_cast<int(*)[2]>(steps + 256));
             n = list.count;
@@ -306,6 +316,7 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
             const int e = first + (tid & 63) / 4;
             const uint64_t key = e < n ? list.key[e] : ~0ull;
             int place = 0;
+#pragma unroll 8
             for (int i = tid % 4; i < n; i += 4) place += list.key[i] > key;
             place += __builtin_amdgcn_update_dpp(0, place, 0xB1, 0xf, 0xf, false);
             place += __builtin_amdgcn_update_dpp(0, place, 0x4E, 0xf, 0xf, false);
