@@ -17,6 +17,7 @@ struct TopArgs {
     int k;                               // 0 to kMostAlternatives
     float *logp, *entropy, *lse, *top;   // each may be null
     int64_t* ids;
+    bool again;                          // the rows may be read again by the gradient's launch
     int64_t first;
 };
 
@@ -224,7 +225,8 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
     const RowSpan sp = row_span<E, NT>(row, V);
     const float k = a.l.k;
     u32x4 x[H];
-    load_chunks<E, NT>(x, row, sp, tid);
+    if (a.again) load_chunks<E, NT, Reading::Again>(x, row, sp, tid);
+    else load_chunks<E, NT>(x, row, sp, tid);
     const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
     const float ly = E::one(row, y);
     if (tid == 0) list.count = 0;
@@ -247,7 +249,8 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
     see_held<E, ENTROPY>(seen, x, edge, exponent_of(most, k));
     for (int c = tid + H * NT; c - tid < sp.chunks; c += AHEAD * NT) {   // (all of a wave, for its list)
         u32x4 z[AHEAD];
-        load_chunks<E, NT>(z, row, sp, c);
+        if (a.again) load_chunks<E, NT, Reading::Again>(z, row, sp, c);
+        else load_chunks<E, NT>(z, row, sp, c);
         float m[AHEAD], of_all = -INFINITY;
         static_for<0, AHEAD>([&](auto I) {
             constexpr int i = decltype(I)::value;
@@ -346,8 +349,8 @@ void launch_top_of(const TopArgs& a, unsigned rows, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_top(const Logits& l, int k, float* logp, float* entropy, float* lse, int64_t* ids, float* top, hipStream_t stream) {
-    TopArgs a{l, k, logp, entropy, lse, top, ids, 0};
+hipError_t launch_top(const Logits& l, int k, float* logp, float* entropy, float* lse, int64_t* ids, float* top, bool again, hipStream_t stream) {
+    TopArgs a{l, k, logp, entropy, lse, top, ids, again, 0};
     constexpr int64_t kRows = (int64_t)1 << 21;
     for (a.first = 0; a.first < l.tokens; a.first += kRows) {
         const unsigned rows = (unsigned)std::min(kRows, l.tokens - a.first);

@@ -74,8 +74,8 @@ hipError_t launch_pair_loss(const PairLoss& loss, hipStream_t stream);
 // ---------------------------------------------------------------- named words of a row
 constexpr int kMostAlternatives = 128;
 
-// logp, entropy, lse (each may be null) of all rows and their k most likely words.
-hipError_t launch_top(const Logits& l, int k, float* logp, float* entropy, float* lse, int64_t* ids, float* top, hipStream_t stream);
+// logp, entropy, lse (each may be null) of all rows and their k most likely words.  `again`: a gradient may read the logits once more soon.
+hipError_t launch_top(const Logits& l, int k, float* logp, float* entropy, float* lse, int64_t* ids, float* top, bool again, hipStream_t stream);
 
 // k words a row: their ids [tokens][k] and, of a teacher, log-probabilities.
 struct ListedWords {
