@@ -231,7 +231,7 @@ __device__ __forceinline__ void list_words(const ListedArgs& a, Words& w, const 
     if constexpr (WORK == Listed::Distill) {
         const double inv_t = (double)a.l.inv_t + a.l.inv_t_low;
         p.most = fmaxf(live[0] ? logit[0] : -INFINITY, live[1] ? logit[1] : -INFINITY);
-        p.most = fold_wave<64>(p.most, [](float x, float z) { return fmaxf(x, z); });
+        p.most = wave_max(p.most);
         const double base = p.most == -INFINITY ? 0.0 : (double)p.most;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -409,14 +409,13 @@ __global__ __launch_bounds__(NT, NT >= 512 ? 4 : 5) void listed_kernel(const Lis
     }
     const float most = max_of<E>(x, fmaxf(seen.m, edge_left));
     keep_packed(x);
-    const float m = fold_row<NT>(most, shared[0], [](float p, float q) { return fmaxf(p, q); });
+    float m = max_group<NT / 64>(most, shared[0]);
+    asm volatile("" : "+v"(m));   // (known to be one number for all threads, it would have the whole rest compiled once for rows that are far and once not)
     see_max<ENTROPY>(seen, m, k);
     const Exponent p = exponent_of(m, k);
     see_held<E, ENTROPY>(seen, x, edge_left, p);
     keep_packed(x);
-    auto plus = [](float p, float q) { return p + q; };
-    const float s = fold_row<NT>(seen.s, shared[1], plus);
-    const float sx = ENTROPY ? fold_row<NT>(seen.w, shared[2], plus) : 0.f;
+    const float s = sum_group<NT / 64>(seen.s, shared[1]), sx = ENTROPY ? sum_group<NT / 64>(seen.w, shared[2]) : 0.f;
 
     const Prelude given = w.given;
     auto finish = [&](const Dense& dense) {

@@ -232,6 +232,43 @@ __device__ __forceinline__ float fold_row(float x, float* shared, Op&& op) {
     return fold_wave<NT / 64>(shared[threadIdx.x % (NT / 64)], op);
 }
 
+// Over a wave, without LDS: the maximum, in every lane.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float dpp_max(float x) {   // (lanes without a source keep their own)
+    const int b = __float_as_int(x);
+    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(b, b, CTRL, ROW_MASK, 0xf, false)));
+}
+__device__ __forceinline__ float wave_max(float x) {
+    x = dpp_max<0xB1, 0xf>(x);    // within pairs, quads, 8, 16 lanes, then the rows of 16 (see wave_sum_to_lane63)
+    x = dpp_max<0x4E, 0xf>(x);
+    x = dpp_max<0x141, 0xf>(x);
+    x = dpp_max<0x140, 0xf>(x);
+    x = dpp_max<0x142, 0xa>(x);
+    x = dpp_max<0x143, 0xc>(x);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
+// Maximum and sum over the workgroup, in a fixed order; every thread gets them.
+template <int WAVES>
+__device__ __forceinline__ float max_group(float x, float* shared) {
+    x = wave_max(x);
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) x = fmaxf(x, shared[i]);
+    return x;
+}
+template <int WAVES>
+__device__ __forceinline__ float sum_group(float x, float* shared) {
+    x = wave_sum_to_lane63(x);
+    if ((threadIdx.x & 63) == 63) shared[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) x += shared[i];
+    return x;
+}
+
 // 2^x is 0 from here on down; products of it with x are formed with no less, so that they are 0 too.
 constexpr float kNoExponent = -1e4f;
 

@@ -92,22 +92,6 @@ __device__ void select_by_digits(const char* row, const RowSpan& sp, int k, KeyL
     __syncthreads();
 }
 
-// Over a wave, without LDS: the maximum, in every lane.
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ float dpp_max(float x) {   // (lanes without a source keep their own)
-    const int b = __float_as_int(x);
-    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(b, b, CTRL, ROW_MASK, 0xf, false)));
-}
-__device__ __forceinline__ float wave_max(float x) {
-    x = dpp_max<0xB1, 0xf>(x);    // within pairs, quads, 8, 16 lanes, then the rows of 16 (see wave_sum_to_lane63)
-    x = dpp_max<0x4E, 0xf>(x);
-    x = dpp_max<0x141, 0xf>(x);
-    x = dpp_max<0x140, 0xf>(x);
-    x = dpp_max<0x142, 0xa>(x);
-    x = dpp_max<0x143, 0xc>(x);
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
-}
-
 // A wave's chunks that hold a value that may be an alternative, as they were read, and the ids of their first words; `count` is the wave's, and may
 // be more than there is room for.
 constexpr int kHot = 128;
@@ -177,18 +161,6 @@ __device__ __forceinline__ float bound_of(float& most, int k, float* shared, int
     }
     __syncthreads();
     return least;
-}
-
-// Sum over the workgroup, in a fixed order; every thread gets it.
-template <int WAVES>
-__device__ __forceinline__ float sum_group(float x, float* shared) {
-    x = wave_sum_to_lane63(x);
-    if ((threadIdx.x & 63) == 63) shared[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = 0.f;
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) x += shared[i];
-    return x;
 }
 
 // A workgroup a row.  Its first H chunks a thread are held in registers until their largest values are known, one a thread: the k-th largest
@@ -270,11 +242,7 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
     }
     float m = most;
     if (sp.chunks > H * NT) {
-        m = wave_max(seen.m);
-        if ((tid & 63) == 0) shared[2][tid >> 6] = m;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) m = fmaxf(m, shared[2][i]);
+        m = max_group<WAVES>(seen.m, shared[2]);
         see_max<ENTROPY>(seen, m, k);
     }
     float s = sum_group<WAVES>(seen.s, shared[0]), w = ENTROPY ? sum_group<WAVES>(seen.w, shared[1]) : 0.f;
