@@ -348,7 +348,7 @@ __device__ __forceinline__ void alternatives_words(const ListedArgs& a, Words& w
 
 // A workgroup a row; the last H chunks a thread stay in registers, those before are read a second time, from their end.
 template <class E, int NT, int H, Listed WORK, bool ENTROPY>
-__global__ __launch_bounds__(NT, NT >= 512 ? 4 : 5) void listed_kernel(const ListedArgs a) {
+__global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kernel(const ListedArgs a) {
     typedef WordList<NT, H> Words;
     __shared__ Words w;
     __shared__ float shared[3][NT / 64];
@@ -491,7 +491,9 @@ void launch_listed_of(const ListedArgs& a, hipStream_t stream) {
     const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;
     const unsigned rows = (unsigned)a.rows;
     if (chunks <= 512) return listed_kernel<E, 256, 2, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
+    if (chunks <= 1024) return listed_kernel<E, 256, 4, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
     if (chunks <= 2048) return listed_kernel<E, 256, 8, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
+    if (chunks <= 4096) return listed_kernel<E, 512, 8, WORK, ENTROPY><<<rows, 512, 0, stream>>>(a);
     listed_kernel<E, 512, 16, WORK, ENTROPY><<<rows, 512, 0, stream>>>(a);
 }
 
