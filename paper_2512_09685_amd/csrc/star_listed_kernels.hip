@@ -38,11 +38,12 @@ struct ListedArgs {
 
 constexpr int kEntries = kMostAlternatives + 1;   // the taken token is the last
 
-// What the first wave knows of its row before the row's sums do: sum of the teacher's shares, or of the derivatives; the entry that stands for the
-// taken token (-1: none is taken); of the teacher's words the largest logit, and the sum of exp(z - that one's).
+// What the first wave knows of its row before the row's sums do: sum of the teacher's shares, relative to exp(likeliest), its largest, or of the
+// derivatives; the entry that stands for the taken token (-1: none is taken); of the teacher's words the largest logit, and the sum of
+// exp(z - that one's).
 struct Prelude {
     double sum, named;
-    float most;
+    float most, likeliest;
     int taken;
 };
 
@@ -57,6 +58,7 @@ struct WordList {
     float logit[kEntries], value[kEntries];       // value: what is written there
     float q[kMostAlternatives], log_q[kMostAlternatives];
     Prelude given;
+    float slope;                                  // of the words that are not named
 };
 
 // The wave's own LDS accesses before and behind this keep their order, also for the compiler; the hardware takes them in order.
@@ -227,17 +229,20 @@ __device__ __forceinline__ void list_words(const ListedArgs& a, Words& w, const 
     if (taken != kMostAlternatives && lane == 0) w.id[kMostAlternatives] = -1;
     w.logit[lane] = logit[0];
     w.logit[64 + lane] = logit[1];
-    Prelude p{0.0, 0.0, -INFINITY, taken};
+    Prelude p{0.0, 0.0, -INFINITY, 0.f, taken};
     if constexpr (WORK == Listed::Distill) {
         const double inv_t = (double)a.l.inv_t + a.l.inv_t_low;
         p.most = fmaxf(live[0] ? logit[0] : -INFINITY, live[1] ? logit[1] : -INFINITY);
         p.most = wave_max(p.most);
         const double base = p.most == -INFINITY ? 0.0 : (double)p.most;
+        for (int i = 0; i < 2; ++i)
+            if (!live[i]) number[i] = -INFINITY;
+        const float likeliest = wave_max(fmaxf(number[0], number[1]));
+        p.likeliest = likeliest == -INFINITY ? 0.f : likeliest;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int e = lane + 64 * i;
-            if (!live[i]) number[i] = -INFINITY;
-            const double q = number[i] == -INFINITY ? 0.0 : exp_of((double)number[i]);
+            const double q = number[i] == -INFINITY ? 0.0 : exp_of((double)number[i] - p.likeliest);
             w.log_q[e] = number[i];
             w.q[e] = (float)q;
             p.sum += q;
@@ -281,9 +286,9 @@ __device__ __forceinline__ double divergence_term(double q, double d, double p) 
 struct Distilled {
     double base, all;         // the largest logit, and the sum over all words of exp(z - that one's)
     double down;              // exp of m's distance from it
-    double divide, whole, left, c, slope;
+    double part, whole, left, c, slope;   // part: of a share, what it is taken as
     bool rest;                // whether there are words that are not named
-    __device__ __forceinline__ Distilled(const ListedArgs& a, const Prelude& given, double weight, float m, float s) {
+    __device__ __forceinline__ void form(const ListedArgs& a, const Prelude& given, double weight, float m, float s) {
         const double inv_t = (double)a.l.inv_t + a.l.inv_t_low, most = given.most;
         const bool named_lead = given.most > m;
         rest = !(s == 0.f);
@@ -292,18 +297,13 @@ struct Distilled {
         down = !rest ? 0.0 : named_lead ? apart : 1.0;
         all = given.named * (named_lead ? 1.0 : rest ? apart : 1.0) + (rest ? s * down : 0.0);
         const double none = all > 0.0 && all < INFINITY ? 0.0 : NAN;   // NaN: a row without probabilities
-        double share = given.sum;
-        left = 0.0, divide = 1.0;
-        if (a.distill.renormalise) {
-            divide = share;
-            share = share == 0.0 ? 0.0 : share / share;
-        } else if (rest) {
-            left = share < 1.0 ? 1.0 - share : share - share;   // (0, or NaN)
-        }
+        left = 0.0, part = a.distill.renormalise ? 1.0 / given.sum : exp_of(given.likeliest);
+        const double share = given.sum == 0.0 ? 0.0 : given.sum * part;
+        if (!a.distill.renormalise && rest) left = share < 1.0 ? 1.0 - share : share - share;   // (0, or NaN)
         whole = share + left;
         c = (double)a.distill.scale * weight * inv_t + none;
         // of the rest e (c (Q + ce) / sum of all - c q_r / sum of the rest)
-        slope = rest ? c * ((whole + a.distill.ce) * down / all - left / s) : none;
+        slope = rest ? c * (((whole + a.distill.ce) * down * s - left * all) / (all * s)) : none;
     }
 };
 
@@ -312,15 +312,15 @@ template <class Words>
 __device__ __forceinline__ void distill_words(const ListedArgs& a, Words& w, const Distilled& d, int64_t t, float m, float s) {
     const int lane = threadIdx.x, taken = w.given.taken;
     const double inv_t = (double)a.l.inv_t + a.l.inv_t_low, ce = a.distill.ce;
-    const double logs = log_of(lane == 0 ? d.all : lane == 1 ? (double)s : lane == 2 ? d.left : d.divide);
-    const double log_all = __shfl(logs, 0), log_s = __shfl(logs, 1), log_left = __shfl(logs, 2), shift = a.distill.renormalise ? __shfl(logs, 3) : 0.0;
+    const double logs = log_of(lane == 0 ? d.all : lane == 1 ? (double)s : lane == 2 ? d.left : d.part);
+    const double log_all = __shfl(logs, 0), log_s = __shfl(logs, 1), log_left = __shfl(logs, 2), shift = a.distill.renormalise ? __shfl(logs, 3) - w.given.likeliest : 0.0;
     double kl = 0.0;
 #pragma unroll 1
     for (int e = lane; e < kMostAlternatives; e += 64) {
         if (w.id[e] < 0) continue;
         const double log_p = ((double)w.logit[e] - d.base) * inv_t - log_all, p = w.logit[e] == -INFINITY ? 0.0 : exp_of(log_p);
-        const double q = w.q[e] == 0.f ? 0.0 : w.q[e] / d.divide;
-        kl += divergence_term(q, log_p - (w.log_q[e] - shift), p);
+        const double q = w.q[e] == 0.f ? 0.0 : w.q[e] * d.part;
+        kl += divergence_term(q, log_p - (w.log_q[e] + shift), p);
         w.value[e] = (float)(d.c * ((d.whole + ce) * p - q - (taken == e ? ce : 0.0)));
     }
     kl = sum_wave(kl);
@@ -417,7 +417,6 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kerne
     keep_packed(x);
     const float s = sum_group<NT / 64>(seen.s, shared[1]), sx = ENTROPY ? sum_group<NT / 64>(seen.w, shared[2]) : 0.f;
 
-    const Prelude given = w.given;
     auto finish = [&](const Dense& dense) {
         keep_packed(x);
         int mine = tid;
@@ -432,12 +431,17 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kerne
     };
     // (the list's numbers come behind the row's: the other waves write while the first one forms them)
     if constexpr (WORK == Listed::Distill) {
-        const Distilled d(a, given, a.l.weights ? (double)a.l.weights[t] : 1.0, m, s);
-        if (out) finish(Dense{(float)d.slope, 0.f, 0.f});
+        Distilled d;
+        if (tid < 64) {
+            d.form(a, w.given, a.l.weights ? (double)a.l.weights[t] : 1.0, m, s);
+            if (tid == 0) w.slope = (float)d.slope;
+        }
+        __syncthreads();
+        if (out) finish(Dense{w.slope, 0.f, 0.f});
         if (tid < 64) distill_words(a, w, d, t, m, s);
     } else {
         const double inv_t = (double)a.l.inv_t + a.l.inv_t_low, slope = ENTROPY ? (double)a.dentropy[t] * 0.693147180559945309 * inv_t / s : 0.0;
-        const Dense dense{(float)(-given.sum * inv_t / s), (float)slope, ENTROPY ? sx / s : 0.f};
+        const Dense dense{(float)(-w.given.sum * inv_t / s), (float)slope, ENTROPY ? sx / s : 0.f};
         finish(dense);
         if (tid < 64) alternatives_words<ENTROPY>(a, w, dense, t, p);
     }

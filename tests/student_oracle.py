@@ -92,7 +92,7 @@ class Distilled:
         V = len(x64)
         logp, z, m = log_softmax(x64, temperature)
         p, q, named = np.exp(logp), np.zeros(V), np.zeros(V, bool)
-        for i, t in zip(ids, tlogp.astype(np.float64)):
+        for i, t in zip(ids, np.asarray(tlogp, np.float64)):
             if 0 <= i < V and not named[i]:
                 named[i], q[i] = True, np.exp(t)
         rest = p[~named].sum()

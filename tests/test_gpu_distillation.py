@@ -162,6 +162,22 @@ def test_banned_words(V, dtype):
     assert np.isnan(kl[3:]).all() and np.isnan(got[3:]).all()
 
 
+@pytest.mark.parametrize("shift", [-300.0, -60.0, 200.0])
+def test_renormalised_numbers_of_any_scale(shift):
+    """Renormalised, a teacher's numbers may be logits: a constant in them makes no difference but for their own rounding (|shift| u)."""
+    T, V, k = 3, 900, 30
+    x, x64, y, rng = make(T, V, "f32", seed=15)
+    ids, tlogp = teacher(x64, k, rng, 1.0, ragged=False)
+    moved = (tlogp.astype(np.float64) + shift).astype(np.float32)
+    kl, d = torch.zeros(T, device="cuda"), torch.zeros_like(x)
+    star.star_distill_loss(x, i64(ids), f32(moved), torch.zeros(4, device="cuda"), dlogits=d, kl_out=kl, renormalise=True, scale=1.0)
+    for t in range(T):
+        r = so.Distilled(x64[t], 1.0, None, ids[t], (moved[t].astype(np.float64) - shift).astype(np.float64), 0.0, True)
+        assert abs(float(kl[t]) - r.kl) <= r.kl_error + so.U * abs(r.kl)
+        bound = r.d_error + 4 * so.U * np.abs(r.d)
+        assert (np.abs(d[t].double().cpu().numpy() - r.d) <= bound + so.U * np.abs(r.d) + 1e-38).all()
+
+
 def test_a_teacher_that_says_nothing():
     V = 700
     x, x64, y, rng = make(3, V, "f32", seed=12)
