@@ -105,7 +105,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_kernel(const NormArg
                 v[j] = E::template get<j>(x[i]) + E::template get<j>(r[i]);
             });
             x[i] = E::pack(v);   // the norm is that of the sum as it is stored
-            if (tid + i * NT < sp.chunks) to[tid + i * NT] = x[i];
+            if (tid + i * NT < sp.chunks) __builtin_nontemporal_store(x[i], to + tid + i * NT);
         });
         if (tid < sp.tail) {
             more += E::one(other, last);
@@ -148,70 +148,83 @@ struct NormGradArgs {
     float* partial;   // [workgroups][width]: sums of the gain's gradient; null: not wanted
 };
 
-// Workgroups take rows in turn and keep the sums of dy h' of their columns in registers.
+// Workgroups take rows in turn and keep the gains of their columns, and the sums of dy h', in registers.
 template <class E, int NT, int C, bool GAIN>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_grad_kernel(const NormGradArgs a) {
     constexpr int ROWS = NT < 256 ? 256 / NT : 1;
+    constexpr bool HELD = NT < 1024 || C <= 2;   // (gains and dresidual: of longer rows they do not fit, and are read where they are used)
     __shared__ double shared[2][NT / 64];
     __shared__ float joined[GAIN && ROWS > 1 ? (ROWS - 1) * NT * (C * E::VEC + 1) : 1];
     const int tid = threadIdx.x % NT, in = ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0, width = (int)a.n.width;
     const Span sp = span_of<E>(width);
     const int last = width - sp.tail + tid;
-    float sum[C][E::VEC] = {}, sum_more = 0.f;
+    float sum[C][E::VEC] = {}, sum_more = 0.f, held[HELD ? C : 1][E::VEC] = {};
+    auto gains_of = [&](auto I, float (&g)[E::VEC]) {
+        constexpr int i = decltype(I)::value;
+        load_gain(g, a.n.gain, a.n.gain_dtype, (tid + i * NT) * E::VEC);
+    };
+    if constexpr (HELD)
+        static_for<0, C>([&](auto I) {
+            if (tid + decltype(I)::value * NT < sp.chunks) gains_of(I, held[decltype(I)::value]);
+        });
+    const float g_more = tid < sp.tail ? one_gain(a.n.gain, a.n.gain_dtype, last) : 0.f;
     int turn = 0;
     for (int64_t t = (int64_t)blockIdx.x * ROWS + in; t < a.n.tokens; t += (int64_t)gridDim.x * ROWS, turn ^= 1) {
         const char *dy_row = at_row(a.dy, t, E::BYTES), *h_row = at_row(a.h, t, E::BYTES);
-        u32x4 d[C], h[C];
+        const char* more_row = a.dresidual.x ? at_row(a.dresidual, t, E::BYTES) : nullptr;
+        u32x4 d[C], h[C], r[HELD ? C : 1];
         load_row<E, NT>(d, dy_row, sp, tid);
         load_row<E, NT>(h, h_row, sp, tid);
+        if constexpr (HELD) {
+            if (more_row) load_row<E, NT>(r, more_row, sp, tid);
+            else static_for<0, C>([&](auto I) { r[decltype(I)::value] = u32x4{0, 0, 0, 0}; });
+        }
         const float rstd = a.rstd[t];
-        float d_more = 0.f, h_more = 0.f, g_more = 0.f;
+        float d_more = 0.f, h_more = 0.f, r_more = 0.f;
         if (tid < sp.tail) {
             d_more = E::one(dy_row, last);
             h_more = E::one(h_row, last) * rstd;
-            g_more = one_gain(a.n.gain, a.n.gain_dtype, last);
+            if (more_row) r_more = E::one(more_row, last);
         }
         double s = (double)(d_more * g_more) * h_more;
         if (GAIN) sum_more += d_more * h_more;
-        static_for<0, C>([&](auto I) {
+        static_for<0, C>([&](auto I) {   // (what a row does not have holds 0)
             constexpr int i = decltype(I)::value;
-            const int c = tid + i * NT;
-            if (c < sp.chunks) {
-                float g[E::VEC];
-                load_gain(g, a.n.gain, a.n.gain_dtype, c * E::VEC);
-                static_for<0, E::VEC>([&](auto J) {
-                    constexpr int j = decltype(J)::value;
-                    const float dj = E::template get<j>(d[i]), hj = E::template get<j>(h[i]) * rstd;
-                    if (GAIN) sum[i][j] += dj * hj;
-                    s = __builtin_fma((double)(dj * g[j]), (double)hj, s);
-                });
-            }
+            if (!HELD && tid + i * NT >= sp.chunks) return;   // (a branch a chunk keeps the compiler from having all chunks' gains under way)
+            float g[E::VEC];
+            if constexpr (!HELD) gains_of(I, g);
+            static_for<0, E::VEC>([&](auto J) {
+                constexpr int j = decltype(J)::value;
+                const float dj = E::template get<j>(d[i]), hj = E::template get<j>(h[i]) * rstd, gj = HELD ? held[HELD ? i : 0][j] : g[j];
+                if (GAIN) sum[i][j] += dj * hj;
+                s = __builtin_fma((double)(dj * gj), (double)hj, s);
+            });
         });
         keep_packed(d);
         keep_packed(h);
         const float mean = (float)(sum_row<NT>(s, shared[turn]) / width);   // (two turns' numbers lie apart: one barrier a row is enough)
-        const char* more_row = a.dresidual.x ? at_row(a.dresidual, t, E::BYTES) : nullptr;
-        char* out = a.dx + t * a.ld_dx * E::BYTES;
+        u32x4_any* out = reinterpret_cast<u32x4_any*>(a.dx + t * a.ld_dx * E::BYTES);
         static_for<0, C>([&](auto I) {
             constexpr int i = decltype(I)::value;
             const int c = tid + i * NT;
             if (c < sp.chunks) {
-                float g[E::VEC], v[E::VEC];
-                load_gain(g, a.n.gain, a.n.gain_dtype, c * E::VEC);
-                u32x4 r{0, 0, 0, 0};
-                if (more_row) r = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(more_row) + c);
+                float v[E::VEC], g[E::VEC];
+                u32x4 more{0, 0, 0, 0};
+                if constexpr (HELD) {
+                    more = r[i];
+                } else {
+                    gains_of(I, g);
+                    if (more_row) more = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(more_row) + c);
+                }
                 static_for<0, E::VEC>([&](auto J) {
                     constexpr int j = decltype(J)::value;
-                    const float hj = E::template get<j>(h[i]) * rstd;
-                    v[j] = rstd * (E::template get<j>(d[i]) * g[j] - hj * mean) + E::template get<j>(r);
+                    const float hj = E::template get<j>(h[i]) * rstd, gj = HELD ? held[HELD ? i : 0][j] : g[j];
+                    v[j] = rstd * (E::template get<j>(d[i]) * gj - hj * mean) + E::template get<j>(more);
                 });
-                __builtin_nontemporal_store(E::pack(v), reinterpret_cast<u32x4_any*>(out) + c);
+                __builtin_nontemporal_store(E::pack(v), out + c);
             }
         });
-        if (tid < sp.tail) {
-            const float r = more_row ? E::one(more_row, last) : 0.f;
-            E::put(out, last, rstd * (d_more * g_more - h_more * mean) + r);
-        }
+        if (tid < sp.tail) E::put(out, last, rstd * (d_more * g_more - h_more * mean) + r_more);
     }
     if constexpr (GAIN) {
         if constexpr (ROWS > 1) {
@@ -247,29 +260,35 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_grad_kernel(const No
     }
 }
 
-// The workgroups' sums joined: 64 columns a workgroup, 16 threads a column.
-constexpr int kJoinThreads = 1024;
+// The workgroups' sums joined: 32 columns a workgroup, 32 threads a column.
+constexpr int kJoinThreads = 1024, kJoinColumns = 32;
 __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(const float* partial, int groups, int width, void* dgain, int dtype, bool accumulate) {
-    __shared__ double shared[kJoinThreads / 64][64];
-    const int c = (int)blockIdx.x * 64 + threadIdx.x % 64, part = threadIdx.x / 64;
+    constexpr int PARTS = kJoinThreads / kJoinColumns;
+    __shared__ double shared[PARTS][kJoinColumns + 1];
+    const int in = threadIdx.x % kJoinColumns, c = (int)blockIdx.x * kJoinColumns + in, part = threadIdx.x / kJoinColumns;
     double s = 0.0;
     if (c < width)
-        for (int g = part; g < groups; g += kJoinThreads / 64) s += (double)partial[(int64_t)g * width + c];
-    shared[part][threadIdx.x % 64] = s;
+#pragma unroll 8
+        for (int g = part; g < groups; g += PARTS) s += (double)partial[(int64_t)g * width + c];
+    shared[part][in] = s;
     __syncthreads();
-    if (part != 0 || c >= width) return;
-    for (int i = 1; i < kJoinThreads / 64; ++i) s += shared[i][threadIdx.x];
+    // (a column's 32 sums lie with the lanes of half a wave)
+    s = shared[in][part];
+    for (int d = 16; d; d >>= 1) s += __shfl_xor(s, d);
+    const int column = (int)blockIdx.x * kJoinColumns + part;
+    if (in != 0 || column >= width) return;
     if (dtype == STAR_F32) {
-        float* to = reinterpret_cast<float*>(dgain) + c;
+        float* to = reinterpret_cast<float*>(dgain) + column;
         *to = (float)(accumulate ? (double)*to + s : s);
     } else {
-        uint16_t* to = reinterpret_cast<uint16_t*>(dgain) + c;
+        uint16_t* to = reinterpret_cast<uint16_t*>(dgain) + column;
         const double held = accumulate ? (double)__uint_as_float((uint32_t)*to << 16) : 0.0;
         *to = (uint16_t)bf16_bits_rne((float)(held + s));
     }
 }
 
-// Threads a row and chunks a thread, by the chunks of a row.
+// Threads a row and chunks a thread, by the chunks of a row (8 a thread: fp32 alone, the widest rows).
+static_assert(kMostNormWidth / ElemBf16::VEC <= 4096 && kMostNormWidth / ElemF32::VEC <= 8192);
 template <class F>
 void for_width(int64_t chunks, F&& f) {
     if (chunks <= 64) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
@@ -295,7 +314,7 @@ hipError_t launch_norm(const Norm& n, const Rows& x, const Rows& residual, float
         for_width(chunks, [&](auto nt, auto c) {
             constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
             if (n.dtype == STAR_F32) norm_kernel<ElemF32, NT, C><<<grid, NT < 256 ? 256 : NT, 0, stream>>>(a);
-            else norm_kernel<ElemBf16, NT, C><<<grid, NT < 256 ? 256 : NT, 0, stream>>>(a);
+            else if constexpr (C < 8) norm_kernel<ElemBf16, NT, C><<<grid, NT < 256 ? 256 : NT, 0, stream>>>(a);
         });
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -304,8 +323,11 @@ hipError_t launch_norm(const Norm& n, const Rows& x, const Rows& residual, float
 }
 
 int norm_grad_groups(int dtype, int64_t tokens, int64_t width) {
-    const int64_t rows = rows_a_group(chunks_of(dtype, width));
-    return (int)std::max<int64_t>(1, std::min<int64_t>(512, (tokens + rows - 1) / rows));
+    // Two a unit, which hold the row, its gains and their sums in registers (us, 512 / 256 / 1024 groups: 8192 x 8192 and 16384 x 4096, bf16: 192 / 213 /
+    // 199 and 180 / 220 / 195), one where that leaves them fewer than four turns, whose sums cost as much as their rows (1000 x 5003, fp32:
+    // 34.3 / 31.5 / 39.1).
+    const int64_t rows = rows_a_group(chunks_of(dtype, width)), turns = (tokens + rows - 1) / rows;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({turns, 512, std::max<int64_t>(256, turns / 4)}));
 }
 
 hipError_t launch_norm_grad(const Norm& n, const Rows& dy, const Rows& h, const float* rstd, const Rows& dresidual, void* dx, int64_t ld_dx, void* dgain,
@@ -321,13 +343,13 @@ hipError_t launch_norm_grad(const Norm& n, const Rows& dy, const Rows& h, const 
                 else norm_grad_kernel<E, NT, C, false><<<groups, NT < 256 ? 256 : NT, 0, stream>>>(a);
             };
             if (n.dtype == STAR_F32) of(ElemF32{});
-            else of(ElemBf16{});
+            else if constexpr (C < 8) of(ElemBf16{});
         });
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (!dgain) return hipSuccess;
-    norm_join_kernel<<<dim3((unsigned)((n.width + 63) / 64)), kJoinThreads, 0, stream>>>(a.partial, n.tokens > 0 ? groups : 0, (int)n.width, dgain,
+    norm_join_kernel<<<dim3((unsigned)((n.width + kJoinColumns - 1) / kJoinColumns)), kJoinThreads, 0, stream>>>(a.partial, n.tokens > 0 ? groups : 0, (int)n.width, dgain,
                                                                                          dgain_dtype, accumulate);
     return hipGetLastError();
 }
