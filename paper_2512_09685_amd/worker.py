@@ -137,19 +137,28 @@ def _words(ids, numbers, tokens: int, what: str, device: int):
         return 0, None, None
     if ids is None or numbers is None:
         raise ValueError(f"{what} go together")
-    for x, dtype in ((ids, _i64), (numbers, _f32)):
-        if x.dtype is not dtype or x.dim() != 2 or x.size(0) != tokens or x.size(1) != ids.size(1) or not x.is_contiguous():
-            raise ValueError(f"{what} must be contiguous int64 and float32 tensors [{tokens}, k]")
-        if x.get_device() != device:
-            raise ValueError(f"{what} must be on the logits' device")
-    return ids.size(1), ids.data_ptr(), numbers.data_ptr()
+    shape = ids.shape
+    if (ids.dtype is not _i64 or numbers.dtype is not _f32 or len(shape) != 2 or shape[0] != tokens or numbers.shape != shape
+            or not ids.is_contiguous() or not numbers.is_contiguous()):
+        raise ValueError(f"{what} must be contiguous int64 and float32 tensors [{tokens}, k]")
+    if ids.get_device() != device or numbers.get_device() != device:
+        raise ValueError(f"{what} must be on the logits' device")
+    return shape[1], ids.data_ptr(), numbers.data_ptr()
+
+
+_device = None
 
 
 def _on_this_gpu(device: int, stream):
-    """As _on_gpu; a call without a stream goes to the current device's, which must be the tensors'."""
+    """As _on_gpu; a call without a stream goes to the current device's, which must be the tensors'.  (Asked for past torch's
+    public function, as ``_stream_handle`` does; a torch without that gives the public one.)"""
+    global _device
     _on_gpu(device)
-    if stream is None and device != _torch.cuda.current_device():
-        raise ValueError(f"the tensors are on device {device}, which is not the current one")
+    if stream is None:
+        if _device is None:
+            _device = getattr(_torch._C, "_cuda_getDevice", None) or _torch.cuda.current_device
+        if _device() != device:
+            raise ValueError(f"the tensors are on device {device}, which is not the current one")
 
 
 def _on_gpu(device: int):
@@ -308,13 +317,15 @@ def star_distill_loss(logits, teacher_ids, teacher_logp, stats_out, *, targets=N
     _check(lib.star_distill_loss(*head, k, ids, teacher, wts, ctypes.byref(p), *out, kl, stats, w, size, _stream_handle(stream)))
 
 
-def _same_rows(x, like, what: str, rows: int, columns: int):
-    """(address, distance of the rows) of a tensor like another, or (None, 0)."""
+def _same_rows(x, what: str, dtype, device: int, shape):
+    """(address, distance of the rows) of a tensor like the first one, or (None, 0)."""
     if x is None:
         return None, 0
-    if x.dtype is not like.dtype or x.get_device() != like.get_device():
+    if x.dtype is not dtype or x.get_device() != device:
         raise TypeError(f"{what} must have the first tensor's type and device")
-    p, _, _, ld = _matrix(x, what, rows, columns)
+    if x.shape == shape and x.is_contiguous():
+        return x.data_ptr(), shape[1]
+    p, _, _, ld = _matrix(x, what, *shape)
     return p, ld
 
 
@@ -335,7 +346,8 @@ def star_rms_norm(x, gain, out, *, residual=None, sum_out=None, rstd_out=None, p
     code = _dtype(x, "x")
     p, tokens, width, ld = _matrix(x, "x")
     device = x.get_device()
-    add, total, y = (_same_rows(v, x, name, tokens, width) for v, name in ((residual, "residual"), (sum_out, "sum_out"), (out, "out")))
+    like = (x.dtype, device, x.shape)
+    add, total, y = _same_rows(residual, "residual", *like), _same_rows(sum_out, "sum_out", *like), _same_rows(out, "out", *like)
     if (residual is None) != (sum_out is None):
         raise StarError(_ERR_NULL, "residual and sum_out go together")
     g, g_code = _gain(gain, width, "gain", device)
@@ -354,7 +366,8 @@ def star_rms_norm_grad(dy, h, gain, rstd, dx, *, dresidual=None, dgain=None, acc
     code = _dtype(dy, "dy")
     p, tokens, width, ld = _matrix(dy, "dy")
     device = dy.get_device()
-    taken, more, to = (_same_rows(v, dy, name, tokens, width) for v, name in ((h, "h"), (dresidual, "dresidual"), (dx, "dx")))
+    like = (dy.dtype, device, dy.shape)
+    taken, more, to = _same_rows(h, "h", *like), _same_rows(dresidual, "dresidual", *like), _same_rows(dx, "dx", *like)
     g, g_code = _gain(gain, width, "gain", device)
     dg, dg_code = _gain(dgain, width, "dgain", device)
     r = _vector(rstd, _f32, tokens, "rstd", device)
