@@ -494,7 +494,8 @@ template <class E, Listed WORK, bool ENTROPY>
 void launch_listed_of(const ListedArgs& a, hipStream_t stream) {
     const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;
     const unsigned rows = (unsigned)a.rows;
-    if (chunks <= 512) return listed_kernel<E, 256, 2, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
+    if (chunks <= 128) return listed_kernel<E, 64, 2, WORK, ENTROPY><<<rows, 64, 0, stream>>>(a);
+    if (chunks <= 512) return listed_kernel<E, 128, 4, WORK, ENTROPY><<<rows, 128, 0, stream>>>(a);
     if (chunks <= 1024) return listed_kernel<E, 256, 4, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
     if (chunks <= 2048) return listed_kernel<E, 256, 8, WORK, ENTROPY><<<rows, 256, 0, stream>>>(a);
     if (chunks <= 4096) return listed_kernel<E, 512, 8, WORK, ENTROPY><<<rows, 512, 0, stream>>>(a);

@@ -121,10 +121,10 @@ __device__ __forceinline__ float beyond_step(int step) {
     return step == kSteps - 1 ? INFINITY : __uint_as_float((uint32_t)(step + 1 + ((127 - 14) << 5)) << 18) * (1.f + 0x1p-20f);
 }
 
-// A bound that at least k values of the row reach: the least of about the k largest of what the threads have seen at most, one value a thread, by a
-// histogram of their distances from the largest.  `most` becomes the workgroup's.  Ends with a barrier.
-template <int NT>
-__device__ __forceinline__ float bound_of(float& most, int k, float* shared, int (&steps)[kSteps], float& least) {
+// A bound that at least k values of the row reach: the least of about the k largest of what the threads have seen at most, one value a thread (or
+// of what `count` counts), by a histogram of their distances from the largest.  `most` becomes the workgroup's.  Ends with a barrier.
+template <int NT, class F>
+__device__ __forceinline__ float bound_of(float& most, int k, float* shared, int (&steps)[kSteps], float& least, F&& count) {
     constexpr int WAVES = NT / 64;
     const int tid = threadIdx.x;
     const float mine = most, m = wave_max(mine);
@@ -134,7 +134,7 @@ __device__ __forceinline__ float bound_of(float& most, int k, float* shared, int
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) most = fmaxf(most, shared[i]);
     if (k == 0) return INFINITY;
-    atomicAdd(&steps[step_of(most - mine)], 1);
+    count(mine, [&](float v) { atomicAdd(&steps[step_of(most - v)], 1); });
     __syncthreads();
     if (tid < 64) {
         // 16 steps a lane, then the lane in which the k-th value lies, then the step
@@ -149,7 +149,8 @@ __device__ __forceinline__ float bound_of(float& most, int k, float* shared, int
             const int below = __shfl_up(up_to, d);
             if (tid >= d) up_to += below;
         }
-        if (up_to >= k && up_to - own < k) {   // (one lane: NT values, of which k is no more)
+        if (tid == 63 && up_to < k) least = -3.402823466e38f;   // (fewer words than alternatives)
+        if (up_to >= k && up_to - own < k) {                    // (one lane)
             int sum = up_to - own, step = -1;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -169,8 +170,8 @@ __device__ __forceinline__ float bound_of(float& most, int k, float* shared, int
 // them is the number of larger keys.  The rest of the row goes by once.  A row that has more such words than the lists hold -- of equal
 // values, or rising ones -- is searched digit by digit.
 template <class E, int NT, int H, bool ENTROPY>
-__global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs a) {
-    constexpr int WAVES = NT / 64, KEYS = NT >= 512 ? 1024 : 512, AHEAD = H == 16 && E::VEC == 8 ? 8 : 4;
+__global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(const TopArgs a) {
+    constexpr int WAVES = NT / 64, KEYS = NT >= 512 ? 1024 : NT == 256 ? 512 : 256, AHEAD = H == 16 && E::VEC == 8 ? 8 : 4;
     __shared__ float shared[3][WAVES];
     __shared__ __align__(16) int steps[kSteps];
     __shared__ float bound;
@@ -187,9 +188,9 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
             if (a.entropy) a.entropy[t] = 0.f;
             if (a.lse) a.lse[t] = 0.f;
         }
-        if (tid < a.k) {
-            ids[tid] = -1;
-            top[tid] = 0.f;
+        for (int i = tid; i < a.k; i += NT) {
+            ids[i] = -1;
+            top[i] = 0.f;
         }
         return;
     }
@@ -212,7 +213,21 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
         most = fmaxf(most, most_of[i]);
     });
     keep_packed(x);
-    const float least = bound_of<NT>(most, a.k, shared[0], steps, bound);
+    // (few threads have a value for so many alternatives: all words are counted then)
+    const bool all = H <= 4 && min(sp.chunks, NT) < 2 * a.k;
+    const float least = bound_of<NT>(most, a.k, shared[0], steps, bound, [&](float mine, auto&& add_one) {
+        if (all) {
+            static_for<0, H>([&](auto I) {
+                static_for<0, E::VEC>([&](auto J) {
+                    const float v = E::template get<decltype(J)::value>(x[decltype(I)::value]);
+                    if (v > -INFINITY) add_one(v);
+                });
+            });
+            if (edge > -INFINITY) add_one(edge);
+        } else {
+            add_one(mine);
+        }
+    });
     static_for<0, H>([&](auto I) {
         constexpr int i = decltype(I)::value;
         hot.put(chunks, most_of[i] >= least, x[i], sp.head + (tid + i * NT) * E::VEC);
@@ -296,20 +311,19 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : 6) void top_kernel(const TopArgs 
         n = min(n, a.k);
     }
     __syncthreads();
-    if (tid < n) {
-        const uint64_t key = sorted[tid];
-        ids[tid] = (int64_t)(uint32_t)~(uint32_t)key;
-        top[tid] = add(scaled_difference(a.l, value_of((uint32_t)(key >> 32)), m), log_s, -1.f).high;
-    } else if (tid < a.k) {
-        ids[tid] = -1;
-        top[tid] = there ? -INFINITY : NAN;
+    for (int i = tid; i < a.k; i += NT) {
+        const uint64_t key = i < n ? sorted[i] : 0;
+        ids[i] = i < n ? (int64_t)(uint32_t)~(uint32_t)key : -1;
+        top[i] = i < n ? add(scaled_difference(a.l, value_of((uint32_t)(key >> 32)), m), log_s, -1.f).high : there ? -INFINITY : NAN;
     }
 }
 
 template <class E, bool ENTROPY>
 void launch_top_of(const TopArgs& a, unsigned rows, hipStream_t stream) {
     const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;
-    if (chunks <= 512) top_kernel<E, 256, 2, ENTROPY><<<rows, 256, 0, stream>>>(a);
+    if (chunks <= 128) top_kernel<E, 64, 2, ENTROPY><<<rows, 64, 0, stream>>>(a);
+    else if (chunks <= 512) top_kernel<E, 128, 4, ENTROPY><<<rows, 128, 0, stream>>>(a);
+    else if (chunks <= 1024) top_kernel<E, 256, 4, ENTROPY><<<rows, 256, 0, stream>>>(a);
     else if (chunks <= 2048) top_kernel<E, 256, 8, ENTROPY><<<rows, 256, 0, stream>>>(a);
     else if (chunks <= 4096) top_kernel<E, 512, 8, ENTROPY><<<rows, 512, 0, stream>>>(a);
     else top_kernel<E, 512, 16, ENTROPY><<<rows, 512, 0, stream>>>(a);
