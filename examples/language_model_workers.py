@@ -106,6 +106,64 @@ class Worker:
         return loss
 
 
+class Student:
+    """A worker that learns a norm's gain and a head from a teacher: one gradient row holds both."""
+
+    SIZE = VOCAB * WIDTH + WIDTH
+
+    def __init__(self, number, device):
+        self.worker, self.device = Worker(number, device), device
+        self.row = torch.zeros(self.SIZE, device=device)
+
+    @classmethod
+    def parameters(cls, device):
+        g = torch.Generator(device=device).manual_seed(1)
+        p = torch.randn(cls.SIZE, generator=g, device=device) * 0.02
+        p[VOCAB * WIDTH:] = 1.0
+        return p
+
+    def alternatives(self, logits, k=32):
+        """What a teacher reports: its likeliest words and their log-probabilities."""
+        T = logits.shape[0]
+        ids, logp = torch.empty(T, k, dtype=torch.int64, device=self.device), torch.empty(T, k, device=self.device)
+        entropy = torch.empty(T, device=self.device)
+        star.star_top_logprobs(logits, None, None, entropy_out=entropy, top_ids=ids, top_logp=logp)
+        return ids, logp, entropy
+
+    def gradient(self, params, teacher, residual):
+        """Fills the gradient row; returns the loss's sums.  ``params``: a bfloat16 copy; ``residual``: what runs past the layer before
+        the norm, [TOKENS, WIDTH]."""
+        head, gain = params[:VOCAB * WIDTH].view(VOCAB, WIDTH), params[VOCAB * WIDTH:]
+        _, x = self.worker.hidden(TOKENS)
+        self.total, self.y, self.rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(TOKENS, device=self.device)
+        self.packed = torch.empty(star.star_act_bytes(TOKENS, WIDTH), dtype=torch.uint8, device=self.device)
+        star.star_rms_norm(x, gain, self.y, residual=residual, sum_out=self.total, rstd_out=self.rstd, packed=self.packed)
+        self.ids, self.logp, _ = self.alternatives(x @ teacher.t())
+        self.logits = self.y @ head.t()
+        self.dlogits, stats = torch.empty_like(self.logits), torch.empty(4, device=self.device)
+        star.star_distill_loss(self.logits, self.ids, self.logp, stats, dlogits=self.dlogits)
+        star.star_act_weight_grad(self.dlogits, self.packed, self.row[:VOCAB * WIDTH].view(VOCAB, WIDTH))
+        self.dy, self.dx = self.dlogits @ head, torch.empty_like(x)
+        star.star_rms_norm_grad(self.dy, self.total, gain, self.rstd, self.dx, dgain=self.row[VOCAB * WIDTH:])
+        return stats
+
+
+def distil(teacher, rounds=30, device="cuda"):
+    """Students learn from a teacher's head [VOCAB, WIDTH]; returns the rounds' losses."""
+    students = [Student(n, device) for n in range(WORKERS)]
+    params, momentum = Student.parameters(device), torch.zeros(Student.SIZE, device=device)
+    copy, rows = params.to(torch.bfloat16), star.GradRows([s.row for s in students])
+    residual = torch.zeros(TOKENS, WIDTH, dtype=torch.bfloat16, device=device)
+    stream = star.UpdateStream([0, 2, 4], [0, 1, 2, 3])
+    losses = []
+    for r in range(rounds):
+        losses.append(float(torch.stack([s.gradient(copy, teacher, residual) for s in students])[:, 0].mean()))
+        star.star_group_update_publish(params, momentum, rows, stream, copy, lr=0.5, momentum_coef=0.5)
+        if r % 10 == 0 or r == rounds - 1:
+            print(f"students   round {r:3d}: divergence {losses[-1]:.4f}", flush=True)
+    return losses
+
+
 def main(rounds=30, device="cuda"):
     server, workers = Server(device), [Worker(w, device) for w in range(WORKERS)]
     reference = server.head().clone()
@@ -126,6 +184,7 @@ def main(rounds=30, device="cuda"):
         server.update([[0, 1, 2, 3]], [0] * WORKERS, lr=0.05)
         if r % 10 == 0 or r == rounds - 1:
             print(f"preference round {r:3d}: loss {losses[-1]:.4f}", flush=True)
+    distil(server.head(), rounds, device)
     return rewards, losses
 
 
