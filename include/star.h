@@ -584,8 +584,8 @@ star_status star_preference_loss(const void *logits, star_dtype dtype, int64_t t
  *   top_ids     : device int64[tokens][k], the most likely words, the likeliest first, of equal logits the lowest id first
  *   top_logp    : device float[tokens][k], their log-probabilities
  * Words of probability 0 (logits of -inf) are no alternatives: where a row has fewer than k others the rest of its ids are -1 and their
- * log-probabilities -inf.  A row without probabilities (NaN, +inf, nothing but -inf) has ids of -1 and NaN everywhere else, a row that does not count
- * ids of -1 and 0.
+ * log-probabilities -inf.  A row without probabilities (NaN, +inf, nothing but -inf) has ids of -1 and NaN everywhere else (lse_out as of
+ * star_token_logprobs), a row that does not count ids of -1 and 0 everywhere else.
  */
 star_status star_top_logprobs(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
                               const int64_t *targets, float temperature, int32_t k, float *logp_out,

@@ -122,6 +122,30 @@ def test_a_sure_student(V, dtype):
     check_loss(x, x64, y, ids, tlogp, None, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [60, 300, 3000, 40001, 140003])
+def test_logits_of_any_size(V, dtype):
+    """Values far apart, values far from 0 that lie close together, and named words far above and far below the others."""
+    rng = np.random.default_rng(V)
+    x = np.stack([rng.standard_normal(V) * 1e5, 3e4 + rng.standard_normal(V), -1e6 + rng.standard_normal(V), rng.standard_normal(V), rng.standard_normal(V)])
+    x[3, :4] += 300.0
+    x[4, :4] -= 300.0
+    x = torch.from_numpy(x.astype(np.float32)).to(TYPES[dtype])
+    x64 = x.double().numpy()
+    ids = np.tile(np.arange(6) * 7 % V, (5, 1))
+    ids[3:] = np.arange(6)
+    tlogp = np.log(np.tile([0.3, 0.2, 0.1, 0.1, 0.1, 0.1], (5, 1))).astype(np.float32)
+    kl, d = torch.zeros(5, device="cuda"), torch.zeros(5, V, dtype=TYPES[dtype], device="cuda")
+    star.star_distill_loss(x.cuda(), i64(ids), f32(tlogp), torch.zeros(4, device="cuda"), dlogits=d, kl_out=kl, scale=1.0, temperature=0.9)
+    temperature = float(np.float32(0.9))
+    for t in range(5):
+        r = so.Distilled(x64[t], temperature, None, ids[t], tlogp[t], 0.0, False)
+        assert abs(float(kl[t]) - r.kl) <= r.kl_error + so.U * abs(r.kl), (t, float(kl[t]), r.kl, r.kl_error)
+        c = 1.0 / temperature
+        want, bound = c * r.d, c * (r.d_error + 4 * so.U * np.abs(r.d))
+        assert (np.abs(d[t].double().cpu().numpy() - want) <= bound + so.HALF_STEP[dtype] * (np.abs(want) + bound) + 1e-38).all(), t
+
+
 def test_a_student_that_agrees():
     """The teacher's numbers are the student's own: the divergence is that of their rounding to fp32 (squared, below 1e-12), never negative, and the gradient
     vanishes but for roundings."""
