@@ -4,6 +4,10 @@
 //     log p_j = (l_j - m) / temperature - log s,   H = -sum p_j log p_j = log s - log 2 w / s.
 // Alternatives are ordered by their logits, which no rounding has touched yet, ties by the lower id: a word's key is its value's order in 32 bits,
 // then the complement of its id, so that no two are alike.
+//
+// One reading of the logits is all that it cannot do without.  Beside the memory it is the vector instructions that count: nine an element of a bf16
+// row (widen, multiply-add, exponential of two turns, two sums, the entropy's product and its guard, half a maximum), and what the lists cost a row.
+// 4096 x 131072, bf16, k = 64: 197 us, 4.9 TB/s, vector pipes busy 73 %; 1023 x 50021, fp32, k = 5: 37 us, 5.5 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "star_logits.h"
@@ -93,7 +97,7 @@ __device__ void select_by_digits(const char* row, const RowSpan& sp, int k, KeyL
 }
 
 // A wave's chunks that hold a value that may be an alternative, as they were read, and the ids of their first words; `count` is the wave's, and may
-// be more than there is room for.
+// be more than there is room for.  (A list a wave needs no atomics: 4096 x 131072, k = 64: 221 us, one list of the workgroup 235.)
 constexpr int kHot = 128;
 struct HotChunks {
     u32x4 chunk[kHot];
@@ -318,6 +322,11 @@ __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(co
     }
 }
 
+// Threads a row, by its chunks: as few as hold it in registers up to 8192 chunks, two rows a unit at least (us, this way / the other; bf16):
+// one and two waves up to 128 and 512 chunks against four: 16384 x 1000, k = 20: 27 / 55, 16384 x 4000: 44 / 57; 4 chunks a thread up to 1024
+// against 8: 8192 x 8000: 38 / 48; 512 threads up to 4096 against 1024: 4096 x 32000: 54 / 95; beyond, 16 chunks a thread against 8 of 1024:
+// 4096 x 131072, k = 64: 242 / 279, and against 8 of 512, which hold half as much and list twice as many: 235 / 336 (k = 8, 2048 x 65536 with the
+// gradient: 163 / 156).
 template <class E, bool ENTROPY>
 void launch_top_of(const TopArgs& a, unsigned rows, hipStream_t stream) {
     const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;
