@@ -13,7 +13,8 @@
 // teacher agree, errors enter squared.
 //
 // Bound by memory, a row read once and written once where it is held (8192 x 65536, bf16, 64 words: 360 us, 5.2 TB/s; without the list 346); short rows by the
-// list, some 1000 instructions of one wave a row (16384 x 1000, 20 words: 44 us).
+// list, some 900 instructions of one wave a row (16384 x 1000, 20 words: 41 us; 44 with ids and numbers asked for after the row and equal words looked
+// for by every entry's own chain).
 //
 // Alternatives.  With D the sum of all derivatives by log-probabilities, H' that by the entropy and E = sum e_j x_j / s:
 //     dz_j = sum_i d_i [j = i] - D p_j - H' p_j log 2 (x_j - E).
@@ -42,10 +43,10 @@ struct ListedArgs {
 constexpr int kEntries = kMostAlternatives + 1;   // the taken token is the last
 
 // What the first wave knows of its row before the row's sums do: sum of the teacher's shares, relative to exp(likeliest), its largest, or of the
-// derivatives; the entry that stands for the taken token (-1: none is taken); of the teacher's words the largest logit, and the sum of
-// exp(z - that one's).
+// derivatives; what such a share is to be multiplied with; the entry that stands for the taken token (-1: none is taken); of the teacher's words
+// the largest logit, and the sum of exp(z - that one's).
 struct Prelude {
-    double sum, named;
+    double sum, named, part;
     float most, likeliest;
     int taken;
 };
@@ -161,13 +162,13 @@ __device__ __forceinline__ void store_dense(u32x4 (&x)[C], char* out, const RowS
     else all(std::false_type{});
 }
 
-// Over a wave, in every lane.
-__device__ __forceinline__ double sum_wave(double x) {
-    x = wave_sum_to_lane63(x);
+// One lane's number, and the sum over a wave, in every lane.
+__device__ __forceinline__ double lane_of(double x, int lane) {
     const unsigned long long b = (unsigned long long)__double_as_longlong(x);
-    const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63), high = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63);
+    const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane), high = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
     return __longlong_as_double((long long)((unsigned long long)high << 32 | low));
 }
+__device__ __forceinline__ double sum_wave(double x) { return lane_of(wave_sum_to_lane63(x), 63); }
 
 // e^x in 64 bits: n log 2 taken out, then the series up to the twelfth power, which at most log 2 / 2 leaves 2e-16 of.
 __device__ __forceinline__ double exp_of(double x) {
@@ -186,58 +187,87 @@ __device__ __forceinline__ double log_of(double v) {
     return v > 0.0 && v < INFINITY ? near + (v * exp_of(-near) - 1.0) : near;
 }
 
-// Puts the list together: entries `lane`, 64 + lane and the taken token.
-template <class E, int NT, Listed WORK, class Words>
-__device__ __forceinline__ void list_words(const ListedArgs& a, Words& w, const RowSpan& sp, const char* row, int64_t t, int64_t y, int rest) {
-    const int lane = threadIdx.x, n = a.words.k;
-    float logit[2] = {-INFINITY, -INFINITY}, number[2] = {0.f, 0.f};
+// What the first wave asks for before the row itself is asked for: it comes in the order it was asked for.  Entries `lane` and 64 + lane.
+struct Asked {
+    int64_t id[2];
+    float number[2];
+};
+template <Listed WORK>
+__device__ __forceinline__ Asked ask_words(const ListedArgs& a, int64_t t) {
+    Asked w{{-1, -1}, {0.f, 0.f}};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int e = lane + 64 * i;
-        const int64_t id = e < n ? a.words.ids[t * n + e] : -1;
-        const bool there = id >= 0 && id < sp.V;
-        w.id[e] = there ? (int)id : -1;
-        if (there) logit[i] = E::one(row, id);
-        if (there) number[i] = WORK == Listed::Distill ? a.words.logp[t * n + e] : a.dtop[t * n + e];
+        const int e = (int)threadIdx.x + 64 * i, n = a.words.k;
+        if (e < n) {
+            w.id[i] = a.words.ids[t * n + e];
+            w.number[i] = WORK == Listed::Distill ? a.words.logp[t * n + e] : a.dtop[t * n + e];
+        }
     }
-    if (lane == 0) {
-        w.id[kMostAlternatives] = y >= 0 && y < sp.V ? (int)y : -1;
-        w.logit[kMostAlternatives] = y >= 0 && y < sp.V ? E::one(row, y) : 0.f;
+    return w;
+}
+
+// Puts the list together: entries `lane`, 64 + lane and the taken token.
+template <class E, int NT, Listed WORK, class Words>
+__device__ __forceinline__ void list_words(const ListedArgs& a, Words& w, const Asked& asked, const RowSpan& sp, const char* row, int64_t t, int64_t y, int rest) {
+    const int lane = threadIdx.x, n = a.words.k;
+    const bool takes = y >= 0 && y < sp.V;
+    float logit[2] = {-INFINITY, -INFINITY}, number[2] = {asked.number[0], asked.number[1]}, y_logit = 0.f;
+    int id[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool there = asked.id[i] >= 0 && asked.id[i] < sp.V;
+        id[i] = there ? (int)asked.id[i] : -1;
+        if (there) logit[i] = E::one(row, id[i]);
+        w.id[lane + 64 * i] = id[i];
     }
+    if (takes) y_logit = E::one(row, y);
+    // (what does not need the logits comes first, while they are on their way)
+    const double dy = WORK == Listed::Alternatives && takes && a.dlogp ? (double)a.dlogp[t] : 0.0;
     for (int i = lane; i < NT; i += 64) w.head[i] = -1;
     if (WORK == Listed::Distill) {
         for (int i = lane; i < NT * Words::MARKS / 4; i += 64) reinterpret_cast<u32x4*>(w.marks)[i] = u32x4{0, 0, 0, 0};
         if (lane < 4) w.edge_marks[lane] = 0;
     }
+    // the entry that stands for the taken token: the first that names it, or its own
+    const unsigned long long named[2] = {__ballot(takes && id[0] == (int)y), __ballot(takes && id[1] == (int)y)};
+    const int taken = !takes ? -1 : named[0] ? __ffsll(named[0]) - 1 : named[1] ? 63 + __ffsll(named[1]) : kMostAlternatives;
+    if (lane == 0) w.id[kMostAlternatives] = taken == kMostAlternatives ? (int)y : -1;
     wave_order();
-    for (int e = lane; e < kEntries; e += 64)
-        if (w.id[e] >= 0) {
-            const Owner o = owner_of<E, NT>(sp, w.id[e]);
-            w.next[e] = atomicExch(&w.head[o.thread], e);
-            if (WORK == Listed::Distill && e != kMostAlternatives) {
-                const int turn = (o.chunk - rest) / NT;
-                if (o.chunk >= rest)
-                    atomicOr(&w.marks[o.thread * Words::MARKS + turn / 4], 1u << (8 * (turn % 4) + (w.id[e] - sp.head) % E::VEC));
-                else if (o.chunk < 0)
-                    atomicOr(&w.edge_marks[o.thread / 32], 1u << (o.thread % 32));
-            }
+    bool again = false;   // a word that an entry of the chain below names too
+    auto link = [&](int e, int word) {
+        const Owner o = owner_of<E, NT>(sp, word);
+        int below = atomicExch(&w.head[o.thread], e);
+        w.next[e] = below;
+        if (WORK == Listed::Distill && e != kMostAlternatives) {
+            const int turn = (o.chunk - rest) / NT;
+            if (o.chunk >= rest)
+                atomicOr(&w.marks[o.thread * Words::MARKS + turn / 4], 1u << (8 * (turn % 4) + (word - sp.head) % E::VEC));
+            else if (o.chunk < 0)
+                atomicOr(&w.edge_marks[o.thread / 32], 1u << (o.thread % 32));
         }
+    };
+    if (id[0] >= 0) link(lane, id[0]);
+    if (id[1] >= 0) link(64 + lane, id[1]);
+    if (lane == 0 && taken == kMostAlternatives) link(kMostAlternatives, (int)y);
     wave_order();
-    const int first[2] = {first_of<E, NT>(w, sp, lane), first_of<E, NT>(w, sp, 64 + lane)}, taken = first_of<E, NT>(w, sp, kMostAlternatives);
-    wave_order();
-    const bool live[2] = {first[0] == lane, first[1] == 64 + lane};
-    const bool again[2] = {first[0] >= 0 && !live[0], first[1] >= 0 && !live[1]};
-    if (again[0]) w.id[lane] = -1;
-    if (again[1]) w.id[64 + lane] = -1;
-    if (taken != kMostAlternatives && lane == 0) w.id[kMostAlternatives] = -1;
-    w.logit[lane] = logit[0];
-    w.logit[64 + lane] = logit[1];
-    Prelude p{0.0, 0.0, -INFINITY, 0.f, taken};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        for (int e = id[i] >= 0 ? w.next[lane + 64 * i] : -1; e >= 0; e = w.next[e]) again |= w.id[e] == id[i];
+    bool live[2] = {id[0] >= 0, id[1] >= 0};
+    const bool repeats = __any(again);
+    int first[2] = {lane, 64 + lane};
+    if (repeats) {
+        if (live[0]) first[0] = first_of<E, NT>(w, sp, lane);
+        if (live[1]) first[1] = first_of<E, NT>(w, sp, 64 + lane);
+        wave_order();
+        for (int i = 0; i < 2; ++i)
+            if (live[i] && first[i] != lane + 64 * i) {
+                live[i] = false;
+                w.id[lane + 64 * i] = -1;
+            }
+    }
+    Prelude p{0.0, 0.0, 1.0, -INFINITY, 0.f, taken};
     if constexpr (WORK == Listed::Distill) {
-        const double inv_t = (double)a.l.inv_t + a.l.inv_t_low;
-        p.most = fmaxf(live[0] ? logit[0] : -INFINITY, live[1] ? logit[1] : -INFINITY);
-        p.most = wave_max(p.most);
-        const double base = p.most == -INFINITY ? 0.0 : (double)p.most;
         for (int i = 0; i < 2; ++i)
             if (!live[i]) number[i] = -INFINITY;
         const float likeliest = wave_max(fmaxf(number[0], number[1]));
@@ -249,7 +279,6 @@ __device__ __forceinline__ void list_words(const ListedArgs& a, Words& w, const 
             w.log_q[e] = number[i];
             w.q[e] = (float)q;
             p.sum += q;
-            if (live[i] && logit[i] != -INFINITY) p.named += exp_of(((double)logit[i] - base) * inv_t);   // (+inf, NaN: NaN)
             if (n <= 64) {
                 w.log_q[64 + e] = -INFINITY;
                 w.q[64 + e] = 0.f;
@@ -257,26 +286,35 @@ __device__ __forceinline__ void list_words(const ListedArgs& a, Words& w, const 
             }
         }
         p.sum = sum_wave(p.sum);
+        p.part = a.distill.renormalise ? 1.0 / p.sum : exp_of(p.likeliest);
+        const double inv_t = (double)a.l.inv_t + a.l.inv_t_low;
+        p.most = wave_max(fmaxf(live[0] ? logit[0] : -INFINITY, live[1] ? logit[1] : -INFINITY));
+        const double base = p.most == -INFINITY ? 0.0 : (double)p.most;
+        for (int i = 0; i < (n <= 64 ? 1 : 2); ++i)
+            if (live[i] && logit[i] != -INFINITY) p.named += exp_of(((double)logit[i] - base) * inv_t);   // (+inf, NaN: NaN)
         p.named = sum_wave(p.named);
     } else {
         // derivatives by the words' log-probabilities, equal words' added in the order of the entries, to `q`
         const float inv_t = a.l.inv_t;
-        double mine[2] = {first[0] >= 0 ? (double)number[0] : 0.0, first[1] >= 0 ? (double)number[1] : 0.0};
-        p.sum = sum_wave(mine[0] + mine[1]);
-        if (__any(again[0] || again[1])) {
+        double mine[2] = {id[0] >= 0 ? (double)number[0] : 0.0, id[1] >= 0 ? (double)number[1] : 0.0};
+        p.sum = sum_wave(mine[0] + mine[1]) + dy;
+        if (repeats) {
             for (int f = 1; f < n; ++f) {
-                const int same = f < 64 ? __shfl(first[0], f) : __shfl(first[1], f - 64);
+                const int same = f < 64 ? __shfl(id[0] >= 0 ? first[0] : -1, f) : __shfl(id[1] >= 0 ? first[1] : -1, f - 64);
                 const double d = (double)(f < 64 ? __shfl(number[0], f) : __shfl(number[1], f - 64));
                 if (same != f && same == lane) mine[0] += d;
                 if (same != f && same == 64 + lane) mine[1] += d;
             }
         }
-        const double dy = taken >= 0 && a.dlogp ? (double)a.dlogp[t] : 0.0;
-        p.sum += dy;
         w.q[lane] = (float)((mine[0] + (taken == lane ? dy : 0.0)) * inv_t);
         w.q[64 + lane] = (float)((mine[1] + (taken == 64 + lane ? dy : 0.0)) * inv_t);
     }
-    if (lane == 0) w.given = p;
+    w.logit[lane] = logit[0];
+    w.logit[64 + lane] = logit[1];
+    if (lane == 0) {
+        w.logit[kMostAlternatives] = y_logit;
+        w.given = p;
+    }
 }
 
 // q f(log p - log q), f(d) = e^d - d - 1, with d = log p - log q.
@@ -300,7 +338,7 @@ struct Distilled {
         down = !rest ? 0.0 : named_lead ? apart : 1.0;
         all = given.named * (named_lead ? 1.0 : rest ? apart : 1.0) + (rest ? s * down : 0.0);
         const double none = all > 0.0 && all < INFINITY ? 0.0 : NAN;   // NaN: a row without probabilities
-        left = 0.0, part = a.distill.renormalise ? 1.0 / given.sum : exp_of(given.likeliest);
+        left = 0.0, part = given.part;
         const double share = given.sum == 0.0 ? 0.0 : given.sum * part;
         if (!a.distill.renormalise && rest) left = share < 1.0 ? 1.0 - share : share - share;   // (0, or NaN)
         whole = share + left;
@@ -316,7 +354,8 @@ __device__ __forceinline__ void distill_words(const ListedArgs& a, Words& w, con
     const int lane = threadIdx.x, taken = w.given.taken;
     const double inv_t = (double)a.l.inv_t + a.l.inv_t_low, ce = a.distill.ce;
     const double logs = log_of(lane == 0 ? d.all : lane == 1 ? (double)s : lane == 2 ? d.left : d.part);
-    const double log_all = __shfl(logs, 0), log_s = __shfl(logs, 1), log_left = __shfl(logs, 2), shift = a.distill.renormalise ? __shfl(logs, 3) - w.given.likeliest : 0.0;
+    const double log_all = lane_of(logs, 0), log_s = lane_of(logs, 1), log_left = lane_of(logs, 2);
+    const double shift = a.distill.renormalise ? lane_of(logs, 3) - w.given.likeliest : 0.0;
     double kl = 0.0;
 #pragma unroll 1
     for (int e = lane; e < kMostAlternatives; e += 64) {
@@ -361,7 +400,10 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kerne
     const char* row = reinterpret_cast<const char*>(a.l.x) + t * a.l.ld * E::BYTES;
     char* out = a.dlogits ? a.dlogits + t * a.ld_out * E::BYTES : nullptr;
     const float k = a.l.k;
-    if ((a.l.targets && (y < 0 || y >= V)) || (a.l.weights && a.l.weights[t] == 0.f)) {
+    const float weight = a.l.weights ? a.l.weights[t] : 1.f;
+    Asked asked{};
+    if (tid < 64) asked = ask_words<WORK>(a, t);
+    if ((a.l.targets && (y < 0 || y >= V)) || weight == 0.f) {
         if (WORK == Listed::Distill && tid == 0) {
             if (a.kl) a.kl[t] = 0.f;
             a.terms[2 * t] = a.terms[2 * t + 1] = 0.0;
@@ -374,7 +416,7 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kerne
     u32x4 x[H];
     load_chunks<E, NT>(x, row, sp, rest + tid);
     const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;
-    if (tid < 64) list_words<E, NT, WORK>(a, w, sp, row, t, y, rest);
+    if (tid < 64) list_words<E, NT, WORK>(a, w, asked, sp, row, t, y, rest);
     __syncthreads();
 
     Seen seen{-INFINITY, 0.f, 0.f};
@@ -436,7 +478,7 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kerne
     if constexpr (WORK == Listed::Distill) {
         Distilled d;
         if (tid < 64) {
-            d.form(a, w.given, a.l.weights ? (double)a.l.weights[t] : 1.0, m, s);
+            d.form(a, w.given, weight, m, s);
             if (tid == 0) w.slope = (float)d.slope;
         }
         __syncthreads();
@@ -494,8 +536,8 @@ __global__ __launch_bounds__(kSumThreads) void distill_stats_kernel(const Logits
 }
 
 // Threads a row, by its chunks (us, this way / the other; bf16, distillation): one and two waves up to 128 and 512 chunks against four: 16384 x 1000, 20
-// words: 44 / 94, 16384 x 4000: 86 / 113; 4 chunks a thread up to 1024 against 8: 8192 x 8000, 64 words: 83 / 94; 8 up to 4096 against 16: 2048 x
-// 32000: 66 / 78; beyond, two rows a unit of 512 threads against one of 1024: 2000 x 131075: 228 / 271, 777 x 50021, fp32: 79 / 100.  More than 16 chunks a
+// words: 43 / 92, 16384 x 4000: 77 / 107; 4 chunks a thread up to 1024 against 8: 8192 x 8000, 64 words: 76 / 87; 8 up to 4096 against 16: 2048 x
+// 32000: 68 / 76; beyond, two rows a unit of 512 threads against one of 1024: 2000 x 131075: 228 / 271, 777 x 50021, fp32: 79 / 100.  More than 16 chunks a
 // thread held of long rows: 2048 x 40000, fp32, 16 / 18 / 20: 127 / 130 / 133, 2000 x 131075: 215 / 217 / 212.
 template <class E, Listed WORK, bool ENTROPY>
 void launch_listed_of(const ListedArgs& a, hipStream_t stream) {
