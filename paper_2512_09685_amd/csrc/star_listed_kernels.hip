@@ -13,7 +13,7 @@
 // teacher agree, errors enter squared.
 //
 // Bound by memory, a row read once and written once where it is held (8192 x 65536, bf16, 64 words: 360 us, 5.2 TB/s; without the list 346); short rows by the
-// list, some 900 instructions of one wave a row (16384 x 1000, 20 words: 41 us; 44 with ids and numbers asked for after the row and equal words looked
+// list, which one wave puts together (16384 x 1000, 20 words: 41 us; 44 with ids and numbers asked for after the row and equal words looked
 // for by every entry's own chain).
 //
 // Alternatives.  With D the sum of all derivatives by log-probabilities, H' that by the entropy and E = sum e_j x_j / s:
@@ -537,8 +537,8 @@ __global__ __launch_bounds__(kSumThreads) void distill_stats_kernel(const Logits
 
 // Threads a row, by its chunks (us, this way / the other; bf16, distillation): one and two waves up to 128 and 512 chunks against four: 16384 x 1000, 20
 // words: 43 / 92, 16384 x 4000: 77 / 107; 4 chunks a thread up to 1024 against 8: 8192 x 8000, 64 words: 76 / 87; 8 up to 4096 against 16: 2048 x
-// 32000: 68 / 76; beyond, two rows a unit of 512 threads against one of 1024: 2000 x 131075: 228 / 271, 777 x 50021, fp32: 79 / 100.  More than 16 chunks a
-// thread held of long rows: 2048 x 40000, fp32, 16 / 18 / 20: 127 / 130 / 133, 2000 x 131075: 215 / 217 / 212.
+// 32000: 68 / 76; beyond, two rows a unit of 512 threads against one of 1024: 2000 x 131075: 220 / 241, 777 x 50021, fp32: 66 / 79.  More than 16 chunks a
+// thread held of long rows: 2048 x 40000, fp32, 16 / 18 / 20: 128 / 130 / 132, 2000 x 131075: 220 / 223 / 218.
 template <class E, Listed WORK, bool ENTROPY>
 void launch_listed_of(const ListedArgs& a, hipStream_t stream) {
     const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;
