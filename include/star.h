@@ -687,8 +687,8 @@ size_t star_act_weight_grad_workspace(star_dtype dy_dtype, int64_t tokens, int64
  *   y        : may be x or the residual
  *   rstd_out : device float[tokens] or NULL
  *   packed   : NULL, or star_act_bytes(tokens, width) bytes: y as star_act_pack keeps it, for star_act_weight_grad
- * "May be" means same address and same distance of rows; overlapping otherwise is not allowed.  The mean is taken in 64 bits.  A row that holds inf or
- * NaN gives NaN.
+ * "May be" means same address and same distance of rows; overlapping otherwise is not allowed.  The mean is taken in 64 bits.  A row that holds NaN
+ * is NaN throughout; one that holds inf has an rstd of 0 and is 0 but for NaN in inf's place.
  */
 star_status star_rms_norm(const void *x, star_dtype dtype, int64_t tokens, int64_t width, int64_t ld,
                           const void *residual, int64_t ld_residual, const void *gain, star_dtype gain_dtype, float eps,

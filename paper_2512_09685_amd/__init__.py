@@ -1,5 +1,6 @@
 """MI355X-native group-synchronous parameter update of STAR (arXiv 2512.09685), and the worker's side of it: losses on
-logits with their gradients, weight gradients from activations kept in 8 bits.
+logits with their gradients, a teacher's alternatives and distillation from them, root-mean-square norms, weight gradients
+from activations kept in 8 bits.
 
 The product is ``libstar.so`` (C ABI, declared in ``include/star.h``); this
 package is its thin Python binding.  PyTorch only supplies device memory and

@@ -1,7 +1,7 @@
 """Binding of the worker-side entry points of libstar.so: losses on logits with their gradients, a teacher's alternatives and
-the loss on them, the root-mean-square norm, activations kept in 8 bits and the weight gradient formed from them.  Argument marshalling only, as in ``binding``; outputs are tensors that the
-caller hands in.  A workspace, where a call needs one, is taken from torch's allocator on the call's stream, or
-passed in (a uint8 tensor of at least the bytes the C header's ``*_workspace`` function returns)."""
+the loss on them, the root-mean-square norm, activations kept in 8 bits and the weight gradient formed from them.  Argument
+marshalling only, as in ``binding``; outputs are tensors that the caller hands in.  A workspace, where a call needs one, is taken
+from torch's allocator on the call's stream, or passed in (a uint8 tensor of at least the bytes the C header's ``*_workspace`` function returns)."""
 from __future__ import annotations
 
 import ctypes
