@@ -129,21 +129,28 @@ struct LeftOut {
     }
 };
 
-// Dense part of the gradient: e (a - b (x - mean)), with x = (l - m) k and e = 2^x.
+// Dense part of the gradient: e (a - b x), with x = (l - m) k and e = 2^x.
 struct Dense {
-    float a, b, mean;
-    template <bool ENTROPY>
-    __device__ __forceinline__ float at(float x) const {
-        const float e = __builtin_amdgcn_exp2f(x);
-        return ENTROPY ? e * (a - b * (fmaxf(x, kNoExponent) - mean)) : e * a;
+    double a, b;
+    struct At {
+        float a, b;
+        template <bool ENTROPY>
+        __device__ __forceinline__ float at(float x) const {
+            const float e = __builtin_amdgcn_exp2f(x);
+            return ENTROPY ? e * __builtin_fmaf(-b, fmaxf(x, kNoExponent), a) : e * a;
+        }
+    };
+    // The same of an x that is `off` too large.
+    __device__ __forceinline__ At with(float off) const {
+        const float f = __builtin_amdgcn_exp2f(-off);
+        return At{(float)(a + b * off) * f, (float)b * f};
     }
 };
 // Its chunks; `p` as they were summed.
 template <class E, int NT, bool ENTROPY, int C>
 __device__ __forceinline__ void store_dense(u32x4 (&x)[C], char* out, const RowSpan& sp, const Dense& d, const Exponent& p, int first) {
     u32x4_any* to = reinterpret_cast<u32x4_any*>(out + sp.head * E::BYTES);
-    const float f = __builtin_amdgcn_exp2f(-p.off);
-    const Dense here{d.a * f, d.b * f, d.mean + p.off};
+    const Dense::At here = d.with(p.off);
     auto all = [&](auto far) {
         keep_packed(x);
         static_for<0, C>([&](auto I) {
@@ -152,7 +159,7 @@ __device__ __forceinline__ void store_dense(u32x4 (&x)[C], char* out, const RowS
             if (at < sp.chunks) {
                 float v[E::VEC];
                 static_for<0, E::VEC>([&](auto J) {
-                    v[decltype(J)::value] = here.at<ENTROPY>(p.of<decltype(far)::value>(E::template get<decltype(J)::value>(x[i])));
+                    v[decltype(J)::value] = here.template at<ENTROPY>(p.of<decltype(far)::value>(E::template get<decltype(J)::value>(x[i])));
                 });
                 __builtin_nontemporal_store(E::pack(v), to + at);
             }
@@ -382,10 +389,11 @@ __device__ __forceinline__ void distill_words(const ListedArgs& a, Words& w, con
 template <bool ENTROPY, class Words>
 __device__ __forceinline__ void alternatives_words(const ListedArgs& a, Words& w, const Dense& dense, int64_t t, const Exponent& p) {
     const int lane = threadIdx.x;
+    const Dense::At of = dense.with(0.f);
     for (int e = lane; e < kMostAlternatives; e += 64)
-        if (w.id[e] >= 0) w.value[e] = dense.at<ENTROPY>((w.logit[e] - p.m) * p.k) + w.q[e];
+        if (w.id[e] >= 0) w.value[e] = of.at<ENTROPY>((w.logit[e] - p.m) * p.k) + w.q[e];
     if (lane == 0 && w.id[kMostAlternatives] >= 0)
-        w.value[kMostAlternatives] = dense.at<ENTROPY>((w.logit[kMostAlternatives] - p.m) * p.k) + (a.dlogp ? a.dlogp[t] * a.l.inv_t : 0.f);
+        w.value[kMostAlternatives] = of.at<ENTROPY>((w.logit[kMostAlternatives] - p.m) * p.k) + (a.dlogp ? a.dlogp[t] * a.l.inv_t : 0.f);
 }
 
 // A workgroup a row; the last H chunks a thread stay in registers, those before are read a second time, from their end.
@@ -452,7 +460,7 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kerne
             see_chunks<E, ENTROPY>(seen, z, k);
         }
     }
-    const float most = max_of<E>(x, fmaxf(seen.m, edge_left));
+    const float most = max_of_many<E>(x, fmaxf(seen.m, edge_left));
     keep_packed(x);
     float m = max_group<NT / 64>(most, shared[0]);
     asm volatile("" : "+v"(m));   // (known to be one number for all threads, it would have the whole rest compiled once for rows that are far and once not)
@@ -472,7 +480,7 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kerne
             load_chunks<E, NT>(z, row, before, first + tid);
             store_dense<E, NT, ENTROPY>(z, out, before, dense, p, first + tid);
         }
-        if (tid < sp.edge) E::put(out, sp.edge_element(tid), dense.at<ENTROPY>((edge - p.m) * k));
+        if (tid < sp.edge) E::put(out, sp.edge_element(tid), dense.with(0.f).template at<ENTROPY>((edge - p.m) * k));
     };
     // (the list's numbers come behind the row's: the other waves write while the first one forms them)
     if constexpr (WORK == Listed::Distill) {
@@ -482,11 +490,11 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kerne
             if (tid == 0) w.slope = (float)d.slope;
         }
         __syncthreads();
-        if (out) finish(Dense{w.slope, 0.f, 0.f});
+        if (out) finish(Dense{w.slope, 0.0});
         if (tid < 64) distill_words(a, w, d, t, m, s);
     } else {
         const double inv_t = (double)a.l.inv_t + a.l.inv_t_low, slope = ENTROPY ? (double)a.dentropy[t] * 0.693147180559945309 * inv_t / s : 0.0;
-        const Dense dense{(float)(-w.given.sum * inv_t / s), (float)slope, ENTROPY ? sx / s : 0.f};
+        const Dense dense{-w.given.sum * inv_t / s + (ENTROPY ? slope * (sx / s) : 0.0), slope};
         finish(dense);
         if (tid < 64) alternatives_words<ENTROPY>(a, w, dense, t, p);
     }

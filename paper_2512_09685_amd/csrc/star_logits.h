@@ -313,6 +313,27 @@ __device__ __forceinline__ Exponent exponent_of(float m, float k) {
 }
 // Both have been formed here, for all that the compiler knows: it would put a sum off to where it is used, and keep all of its terms till then.
 __device__ __forceinline__ void pinned(float& s, float& w) { asm volatile("" : "+v"(s), "+v"(w)); }
+// max_of many values: those that are not negative are ordered as their bits are, two bf16 to an instruction and none widened; a wave with a thread that
+// has nothing but negative values looks at all of them again.  (A NaN comes out, or the largest of the others.)
+template <class E, int C>
+__device__ __forceinline__ float max_of_many(const u32x4 (&x)[C], float more) {
+    if constexpr (E::VEC == 4) {
+        return max_of<E>(x, more);
+    } else {
+        typedef short __attribute__((ext_vector_type(2))) s16x2;
+        s16x2 m{-32768, -32768};
+        static_for<0, C>([&](auto I) {
+            static_for<0, 4>([&](auto J) {
+                const uint32_t pair = x[decltype(I)::value][decltype(J)::value];   // (of a vector's element itself, a bit cast takes the first)
+                m = __builtin_elementwise_max(m, __builtin_bit_cast(s16x2, pair));
+            });
+        });
+        const int most = max((int)m[0], (int)m[1]);
+        float f = __uint_as_float((uint32_t)most << 16);
+        if (__any(most < 0)) f = max_of<E>(x, -INFINITY);
+        return fmaxf(f, more);
+    }
+}
 // Adds C chunks a thread and one element more, none of them above a.m.
 template <class E, bool ENTROPY, int C>
 __device__ __forceinline__ void see_held(Seen& a, u32x4 (&x)[C], float more, const Exponent& p) {
