@@ -420,7 +420,8 @@ __global__ __launch_bounds__(NT, H == 16 ? 4 : H == 8 ? 6 : 7) void listed_kerne
         return;
     }
     const RowSpan sp = row_span<E, NT>(row, V);
-    const int rest = (max(sp.chunks - H * NT, 0) + NT - 1) / NT * NT;   // (whole turns of the threads: chunk c is thread c % NT's)
+    // (16 chunks a thread: the rows that are longer, too)
+    const int rest = H == 16 ? (max(sp.chunks - H * NT, 0) + NT - 1) / NT * NT : 0;   // (whole turns of the threads: chunk c is thread c % NT's)
     u32x4 x[H];
     load_chunks<E, NT>(x, row, sp, rest + tid);
     const float edge = tid < sp.edge ? E::one(row, sp.edge_element(tid)) : -INFINITY;

@@ -176,6 +176,7 @@ __device__ __forceinline__ float bound_of(float& most, int k, float* shared, int
 template <class E, int NT, int H, bool ENTROPY>
 __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(const TopArgs a) {
     constexpr int WAVES = NT / 64, KEYS = NT >= 512 ? 1024 : NT == 256 ? 512 : 256, AHEAD = H == 16 && E::VEC == 8 ? 8 : 4;
+    constexpr bool LONG = H == 16;   // rows that are not held whole; the others' registers are not to pay for them (8192 x 8000: 33.0 / 35.6 us)
     __shared__ float shared[3][WAVES];
     __shared__ __align__(16) int steps[kSteps];
     __shared__ float bound;
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(co
     });
     Seen seen{most, 0.f, 0.f};
     see_held<E, ENTROPY>(seen, x, edge, exponent_of(most, k));
-    for (int c = tid + H * NT; c - tid < sp.chunks; c += AHEAD * NT) {   // (all of a wave, for its list)
+    if constexpr (LONG) for (int c = tid + H * NT; c - tid < sp.chunks; c += AHEAD * NT) {   // (all of a wave, for its list)
         u32x4 z[AHEAD];
         if (a.again) load_chunks<E, NT, Reading::Again>(z, row, sp, c);
         else load_chunks<E, NT>(z, row, sp, c);
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(co
         });
     }
     float m = most;
-    if (sp.chunks > H * NT) {
+    if (LONG && sp.chunks > H * NT) {
         m = max_group<WAVES>(seen.m, shared[2]);
         see_max<ENTROPY>(seen, m, k);
     }
