@@ -176,7 +176,7 @@ __device__ __forceinline__ float bound_of(float& most, int k, float* shared, int
 template <class E, int NT, int H, bool ENTROPY>
 __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(const TopArgs a) {
     constexpr int WAVES = NT / 64, KEYS = NT >= 512 ? 1024 : NT == 256 ? 512 : 256, AHEAD = H == 16 && E::VEC == 8 ? 8 : 4;
-    constexpr bool LONG = H == 16;   // rows that are not held whole; the others' registers are not to pay for them (8192 x 8000: 33.0 / 35.6 us)
+    constexpr bool LONG = H == 16;   // rows that are not held whole; the others' registers are not to pay for them (8192 x 8000, k = 20: 32 / 36 us)
     __shared__ float shared[3][WAVES];
     __shared__ __align__(16) int steps[kSteps];
     __shared__ float bound;
@@ -324,8 +324,8 @@ __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(co
 }
 
 // Threads a row, by its chunks: as few as hold it in registers up to 8192 chunks, two rows a unit at least (us, this way / the other; bf16):
-// one and two waves up to 128 and 512 chunks against four: 16384 x 1000, k = 20: 27 / 55, 16384 x 4000: 44 / 57; 4 chunks a thread up to 1024
-// against 8: 8192 x 8000: 38 / 48; 512 threads up to 4096 against 1024: 4096 x 32000: 54 / 95; beyond, 16 chunks a thread against 8 of 1024:
+// one and two waves up to 128 and 512 chunks against four: 16384 x 1000, k = 20: 27 / 60, 16384 x 4000: 42 / 55; 4 chunks a thread up to 1024
+// against 8: 8192 x 8000: 35 / 48; 512 threads up to 4096 against 1024: 4096 x 32000: 57 / 68; beyond, 16 chunks a thread against 8 of 1024:
 // 4096 x 131072, k = 64: 242 / 279, and against 8 of 512, which hold half as much and list twice as many: 235 / 336 (k = 8, 2048 x 65536 with the
 // gradient: 163 / 156).
 template <class E, bool ENTROPY>

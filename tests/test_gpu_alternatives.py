@@ -288,3 +288,22 @@ def test_rows_far_into_a_long_buffer():
     for t in range(T):
         want, bound = so.top_grad(host[t].double().numpy(), 1.0, y[t], 1.0, 1.0, [], [], "bf16")
         assert (np.abs(x[t].double().cpu().numpy() - want) <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 3000, 8192, 40001, 140003])
+def test_rows_that_are_nowhere_above_zero(V, dtype):
+    """All of a row below 0, one thread's words alone, and the largest of them 0 or -0."""
+    x, _, y, rng = make(4, V, dtype, seed=12)
+    x[0] -= 100.0
+    x[1, V // 2:] -= 100.0
+    x[2:] = -x[2:].abs()
+    x[2, V // 3], x[3, V // 3] = 0.0, -0.0
+    x64 = x.double().cpu().numpy()
+    check_rows(x64, y, 20, 1.0, alternatives(x, i64(y), 20, 1.0))
+    one, ids, dtop = f32(rng.standard_normal(4)), rng.integers(0, V, (4, 20)), rng.standard_normal((4, 20)).astype(np.float32)
+    d = torch.zeros_like(x)
+    star.star_top_logprobs_grad(x, i64(y), d, dlogp=one, dentropy=one, top_ids=i64(ids), dtop=f32(dtop))
+    for t in range(4):
+        want, bound = so.top_grad(x64[t], 1.0, y[t], float(one[t]), float(one[t]), ids[t], dtop[t].astype(np.float64), dtype)
+        assert (np.abs(d[t].double().cpu().numpy() - want) <= bound).all(), t

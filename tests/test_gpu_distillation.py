@@ -351,3 +351,17 @@ def test_a_teacher_and_a_student_together():
     stats = torch.zeros(4, device="cuda")
     star.star_distill_loss(theirs, ids, top, stats, targets=i64(y), temperature=1.5)
     assert 0.0 <= float(stats[1]) < 1e-6 and float(stats[3]) > 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 3000, 8192, 40001, 140003])
+def test_rows_that_are_nowhere_above_zero(V, dtype):
+    """All of a row below 0, one thread's words alone, and the largest of them 0 or -0."""
+    x, _, y, rng = make(4, V, dtype, seed=12)
+    x[0] -= 100.0
+    x[1, V // 2:] -= 100.0
+    x[2:] = -x[2:].abs()
+    x[2, V // 3], x[3, V // 3] = 0.0, -0.0
+    x64 = x.double().cpu().numpy()
+    ids, tlogp = teacher(x64, 20, rng, 1.0)
+    check_loss(x, x64, y, ids, tlogp, None, dtype, ce=0.2)
