@@ -13,7 +13,7 @@
 // teacher agree, errors enter squared.
 //
 // Bound by memory, a row read once and written once where it is held (8192 x 65536, bf16, 64 words: 360 us, 5.2 TB/s; without the list 346); short rows by the
-// list, which one wave puts together (16384 x 1000, 20 words: 41 us; 44 with ids and numbers asked for after the row and equal words looked
+// list, which one wave puts together (16384 x 1000, 20 words: 40 us; 43 with ids and numbers asked for after the row and equal words looked
 // for by every entry's own chain).
 //
 // Alternatives.  With D the sum of all derivatives by log-probabilities, H' that by the entropy and E = sum e_j x_j / s:
