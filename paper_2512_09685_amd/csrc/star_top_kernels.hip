@@ -127,7 +127,8 @@ __device__ __forceinline__ float beyond_step(int step) {
 }
 
 // A bound that at least k values of the row reach: the least of about the k largest of what the threads have seen at most, one value a thread (or
-// of what `count` counts), by a histogram of their distances from the largest.  `most` becomes the workgroup's.  Ends with a barrier.
+// of what `count` counts), by a histogram of their distances from the largest.  `most` becomes the workgroup's.  Without alternatives nothing
+// but that is formed, and no barrier stands behind the reading of `shared`: it is this function's alone.
 template <int NT, class F>
 __device__ __forceinline__ float bound_of(float& most, int k, float* shared, int (&steps)[kSteps], float& least, F&& count) {
     constexpr int WAVES = NT / 64;
@@ -178,7 +179,7 @@ template <class E, int NT, int H, bool ENTROPY>
 __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(const TopArgs a) {
     constexpr int WAVES = NT / 64, KEYS = NT >= 512 ? 1024 : NT == 256 ? 512 : 256, AHEAD = H == 16 && E::VEC == 8 ? 8 : 4;
     constexpr bool LONG = H == 16;   // rows that are not held whole; the others' registers are not to pay for them (8192 x 8000, k = 20: 32 / 36 us)
-    __shared__ float shared[3][WAVES];
+    __shared__ float shared[4][WAVES];   // sum of the exponentials, that of the entropy, the whole row's maximum, the bound's: each written once
     __shared__ __align__(16) int steps[kSteps];
     __shared__ float bound;
     __shared__ KeyList<KEYS> list;
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(co
     keep_packed(x);
     // (few threads have a value for so many alternatives: all words are counted then)
     const bool all = H <= 4 && min(sp.chunks, NT) < 2 * a.k;
-    const float least = bound_of<NT>(most, a.k, shared[0], steps, bound, [&](float mine, auto&& add_one) {
+    const float least = bound_of<NT>(most, a.k, shared[3], steps, bound, [&](float mine, auto&& add_one) {
         if (all) {
             static_for<0, H>([&](auto I) {
                 static_for<0, E::VEC>([&](auto J) {

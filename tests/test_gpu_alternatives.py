@@ -307,3 +307,21 @@ def test_rows_that_are_nowhere_above_zero(V, dtype):
     for t in range(4):
         want, bound = so.top_grad(x64[t], 1.0, y[t], float(one[t]), float(one[t]), ids[t], dtop[t].astype(np.float64), dtype)
         assert (np.abs(d[t].double().cpu().numpy() - want) <= bound).all(), t
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [900, 2000, 4000, 8000, 16000, 32000, 60000])
+def test_numbers_of_a_row_are_the_same_without_alternatives(V, dtype):
+    """Log-probability, entropy and normaliser do not depend on whether a list is asked for: thousands of rows on a card that is full of them, bit for
+    bit.  Logits far below 0, where a sum in the place of a maximum would be above all of them."""
+    T = 4096
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = (torch.randn(T, V, generator=g, device="cuda") * 3 - 50).to(TYPES[dtype])
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    y[::7] = -1
+    listed = alternatives(x, y, 1, 0.7)
+    for _ in range(3):
+        alone = alternatives(x, y, 0, 0.7)
+        assert all(torch.equal(a, b) for a, b in zip(listed[:3], alone[:3]))
+    rows = [0, 1, 2, T // 2, T - 1]
+    check_rows(x[rows].double().cpu().numpy(), y[rows].cpu().numpy(), 0, float(np.float32(0.7)), [v[rows] for v in alone])
