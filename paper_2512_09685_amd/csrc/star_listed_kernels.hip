@@ -327,7 +327,8 @@ __device__ __forceinline__ void list_words(const ListedArgs& a, Words& w, const 
 // q f(log p - log q), f(d) = e^d - d - 1, with d = log p - log q.
 __device__ __forceinline__ double divergence_term(double q, double d, double p) {
     if (q == 0.0) return p;
-    return fabs(d) < 0.25 ? q * (double)kl_of((float)d, 0.f) : p - q - q * d;
+    const float near = (float)d;   // (as kl_of sees it: what rounds to 0.25 is not of its series either)
+    return fabsf(near) < 0.25f ? q * (double)kl_of(near, 0.f) : p - q - q * d;
 }
 
 // A row of the distillation loss, from the maximum m and sum s of the words that are not named.

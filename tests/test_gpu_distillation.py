@@ -365,3 +365,21 @@ def test_rows_that_are_nowhere_above_zero(V, dtype):
     x64 = x.double().cpu().numpy()
     ids, tlogp = teacher(x64, 20, rng, 1.0)
     check_loss(x, x64, y, ids, tlogp, None, dtype, ce=0.2)
+
+
+@pytest.mark.parametrize("share,side", [("named", 0.25), ("named", -0.25), ("rest", 0.25), ("rest", -0.25)])
+def test_divergence_where_its_form_turns(share, side):
+    """Student and teacher a quarter apart in log p, step by step of a logit through the border, values that fp32 rounds to it among them."""
+    n, log_q = 1001, {0.25: -0.9375, -0.25: -0.4375}[side] if share == "named" else {0.25: np.log(0.6), -0.25: np.log(0.4)}[side]
+    log_q = np.float32(log_q)
+    left = -np.expm1(np.float64(log_q))
+    p0 = np.exp(np.float64(log_q) + side) if share == "named" else 1.0 - left * np.exp(side)
+    middle = np.array([np.log(1.0 / p0 - 1.0)], np.float32).view(np.int32)[0]
+    z = np.zeros((n, 2), np.float32)
+    z[:, 1] = (middle + np.arange(n, dtype=np.int32) - n // 2).view(np.float32)
+    logp = np.stack([so.log_softmax(row, 1.0)[0] for row in z.astype(np.float64)])
+    d = logp[:, 0] - np.float64(log_q) if share == "named" else logp[:, 1] - np.log(left)
+    assert (d < side).any() and (d > side).any()
+    assert ((np.abs(d) < 0.25) & (np.abs(d.astype(np.float32)) == 0.25)).any()
+    ids, tlogp = np.zeros((n, 1), np.int64), np.full((n, 1), log_q)
+    check_loss(f32(z), z.astype(np.float64), None, ids, tlogp, None, "f32")
