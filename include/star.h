@@ -585,7 +585,7 @@ star_status star_preference_loss(const void *logits, star_dtype dtype, int64_t t
  *   top_logp    : device float[tokens][k], their log-probabilities
  * Words of probability 0 (logits of -inf) are no alternatives: where a row has fewer than k others the rest of its ids are -1 and their
  * log-probabilities -inf.  A row without probabilities (NaN, +inf, nothing but -inf) has ids of -1 and NaN everywhere else (lse_out as of
- * star_token_logprobs), a row that does not count ids of -1 and 0 everywhere else.
+ * star_token_logprobs), a row that does not count ids of -1 and 0 everywhere else.  Outputs over one another or over the targets are refused.
  */
 star_status star_top_logprobs(const void *logits, star_dtype dtype, int64_t tokens, int64_t vocab, int64_t ld,
                               const int64_t *targets, float temperature, int32_t k, float *logp_out,
@@ -616,7 +616,8 @@ star_status star_top_logprobs_grad(const void *logits, star_dtype dtype, int64_t
  *   targets      : device int64[tokens], or NULL: all rows count (then ce_coef must be 0)
  *   weights      : device float[tokens] or NULL (all 1); a token of weight 0 does not count
  *   dlogits      : as above, or NULL: the loss alone
- *   kl_out       : device float[tokens] or NULL: l_t without its last term; 0 for a token that does not count
+ *   kl_out       : device float[tokens] or NULL: l_t without its last term; 0 for a token that does not count.
+ *                  Over weights, targets, the teacher's words or stats_out it is refused
  *   stats_out    : device float[4]: loss, and sum_t scale weights[t] times the divergence (kl_out), times -log p[targets[t]] (0 without targets), times 1
  * Where the student gives the words not named a probability of 0 (there are none, or all are banned), they are left out: q_r is taken as 0.  A word of
  * the teacher's that the student bans costs infinity, and has a gradient all the same.  A teacher that names nothing costs 0.  The named words' numbers are

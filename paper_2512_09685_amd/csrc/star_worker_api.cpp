@@ -29,6 +29,16 @@ bool over(const float* out, const float* in, int64_t tokens) {
     return out && in && (a < b ? b - a : a - b) < bytes;
 }
 
+// The same of vectors of any lengths.
+struct Stretch {
+    const void* p;   // may be null
+    size_t bytes;
+};
+bool meet(const Stretch& a, const Stretch& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && (x < y ? y - x < a.bytes : x - y < b.bytes) && a.bytes && b.bytes;
+}
+
 // `rows` rows of `length` values, `ld` apart: no size negative, no offset beyond 63 bits.
 bool rows_fit(int64_t rows, int64_t length, int64_t ld) {
     return rows >= 0 && length >= 0 && ld >= length && ld <= kMostElements && (rows == 0 || ld == 0 || rows <= kMostElements / ld);
@@ -239,9 +249,15 @@ star_status star_top_logprobs(const void* logits, star_dtype dtype, int64_t toke
     STAR_CHECK(check_logits(logits, dtype, tokens, vocab, ld, targets, temperature, nullptr, 0, true));
     STAR_CHECK(check_words(k, 0, top_ids, top_logp, tokens));
     if (logp_out && !targets && tokens > 0) return set_error(STAR_ERR_NULL, "logp_out without targets");
-    if (over(logp_out, entropy_out, tokens) || over(logp_out, lse_out, tokens) || over(entropy_out, lse_out, tokens))
-        return set_error(STAR_ERR_SHAPE, "two outputs overlap");
     if (tokens == 0) return STAR_OK;
+    // (the rows' workgroups run in any order: one would write what another has yet to read, or has written)
+    const size_t n = (size_t)tokens, words = n * (size_t)k;
+    const Stretch taken{targets, 8 * n}, outs[5] = {{logp_out, 4 * n}, {entropy_out, 4 * n}, {lse_out, 4 * n}, {top_ids, 8 * words}, {top_logp, 4 * words}};
+    for (int i = 0; i < 5; ++i) {
+        if (meet(outs[i], taken)) return set_error(STAR_ERR_SHAPE, "an output overlaps the targets");
+        for (int j = 0; j < i; ++j)
+            if (meet(outs[i], outs[j])) return set_error(STAR_ERR_SHAPE, "two outputs overlap");
+    }
     STAR_CHECK(check_workspace(workspace, workspace_bytes, star_top_logprobs_workspace(dtype, tokens, vocab, k)));
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, nullptr, temperature);
     // Taken tokens' log-probabilities are what a loss is made of: logits that the memory-side cache holds stay in it for its gradient (2048 x
@@ -282,7 +298,11 @@ star_status star_distill_loss(const void* logits, star_dtype dtype, int64_t toke
     STAR_CHECK(check_words(k, 1, teacher_ids, teacher_logp, tokens));
     if (!stats_out) return set_error(STAR_ERR_NULL, "stats_out is NULL");
     if (tokens > 0 && params->ce_coef != 0.f && !targets) return set_error(STAR_ERR_NULL, "ce_coef is not 0 and targets is NULL");
-    if (over(kl_out, weights, tokens)) return set_error(STAR_ERR_SHAPE, "kl_out overlaps an input");
+    const size_t n = (size_t)tokens, words = n * (size_t)k;
+    const Stretch kl{kl_out, 4 * n};
+    for (const Stretch& in : {Stretch{weights, 4 * n}, Stretch{targets, 8 * n}, Stretch{teacher_ids, 8 * words}, Stretch{teacher_logp, 4 * words}})
+        if (meet(kl, in)) return set_error(STAR_ERR_SHAPE, "kl_out overlaps an input");
+    if (meet(kl, Stretch{stats_out, 16})) return set_error(STAR_ERR_SHAPE, "two outputs overlap");
     STAR_CHECK(check_workspace(workspace, workspace_bytes, star_distill_loss_workspace(dtype, tokens, vocab, k)));
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, weights, params->temperature);
     const star::DistillArgs d{params->scale, params->ce_coef, params->renormalise != 0};

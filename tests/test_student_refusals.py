@@ -207,3 +207,37 @@ def test_binding_refuses_host_memory():
                  lambda: star.star_rms_norm_grad(x, x, torch.ones(V), f, x.clone(), stream=0)):
         with pytest.raises(ValueError, match="GPU memory"):
             call()
+
+
+def _apart(names):
+    return {name: 0x1000 * P + i * 0x10000 for i, name in enumerate(names)}
+
+
+@pytest.mark.parametrize("k", [1, 4])
+def test_outputs_over_one_another_or_the_targets_refused(lib, k):
+    """Every pair, at both ends of the stretch in which they meet: 3 tokens, k words each."""
+    size = dict(targets=24, logp=12, entropy=12, lse=12, ids=24 * k, top=12 * k)
+    for a in size:
+        for b in size:
+            if a == b:
+                continue
+            at = _apart(size)
+            grid = 8 if b in ("targets", "ids") else 4
+            for off in (0, -grid, (size[a] - 1) // grid * grid):
+                at[b] = at[a] + off
+                args = {n: at[n] for n in size if n != "targets"}
+                assert _top(lib, _head(dict(targets=at["targets"])), k=k, **args) == SHAPE, (a, b, off)
+                assert "overlap" in star.last_error()
+
+
+@pytest.mark.parametrize("k", [1, 4])
+def test_divergences_over_an_input_or_the_sums_refused(lib, k):
+    size = dict(targets=24, ids=24 * k, teacher=12 * k, weights=12, stats=16)
+    for name in size:
+        at = _apart(size)
+        args = {n: at[n] for n in size if n != "targets"}
+        for off in (0, -8, size[name] - 4):
+            assert _distill(lib, _head(dict(targets=at["targets"])), k=k, kl=at[name] + off, **args) == SHAPE and "overlap" in star.last_error(), (name, off)
+        # side by side: the next check's answer
+        for off in (-12, size[name]):
+            assert _distill(lib, _head(dict(targets=at["targets"])), k=k, kl=at[name] + off, ws=None, size=0, **args) == NULL
