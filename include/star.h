@@ -592,7 +592,7 @@ star_status star_top_logprobs(const void *logits, star_dtype dtype, int64_t toke
                               float *entropy_out, float *lse_out, int64_t *top_ids, float *top_logp, void *workspace,
                               size_t workspace_bytes, void *hip_stream);
 
-/* The gradient of any function of them.  With D[t] = dlogp[t] + sum_i dtop[t][i] and H the entropy,
+/* The gradient of any function of the log-probabilities and entropies among them (not of lse_out: a derivative by it has no place here).  With D[t] = dlogp[t] + sum_i dtop[t][i] and H the entropy,
  *     dlogits[t][j] = (dlogp[t] [j == targets[t]] + sum_i dtop[t][i] [j == top_ids[t][i]] - p[t][j] (D[t] + dentropy[t] (log p[t][j] + H[t]))) / temperature.
  *   dlogp, dentropy : device float[tokens], or NULL: 0; dlogp needs targets
  *   top_ids, dtop   : device int64[tokens][k], float[tokens][k], k from 0 to 128 (NULL for k == 0).  Any words in any order, the same one
@@ -607,7 +607,7 @@ star_status star_top_logprobs_grad(const void *logits, star_dtype dtype, int64_t
  * Distillation loss on a teacher's alternatives, and its gradient.  Row t of the teacher names k words i with log-probabilities
  * teacher_logp[t][i], as star_top_logprobs returns them (at the same temperature).  With q_i = exp(teacher_logp) its shares, p the student's, and the
  * words not named taken together (q_r = max(0, 1 - sum q_i), p_r the sum of their p), token t costs
- *     l_t = sum_i q_i log(q_i / p_i) + q_r log(q_r / p_r) - ce_coef log p[targets[t]]
+ *     l_t = sum_i q_i log(q_i / p_i) + q_r log(q_r / p_r) - ce_coef log p[targets[t]]     (p at `temperature` in the last term too)
  * and loss = scale sum_t weights[t] l_t.  With renormalise nonzero the named words are the whole of the teacher: q_i is divided by their sum, and
  * q_r is 0.
  *   teacher_ids  : device int64[tokens][k], k from 1 to 128, in any order.  An id outside [0, vocab) names nothing; of a word that is named twice the
@@ -621,7 +621,7 @@ star_status star_top_logprobs_grad(const void *logits, star_dtype dtype, int64_t
  *   stats_out    : device float[4]: loss, and sum_t scale weights[t] times the divergence (kl_out), times -log p[targets[t]] (0 without targets), times 1
  * Where the student gives the words not named a probability of 0 (there are none, or all are banned), they are left out: q_r is taken as 0.  A word of
  * the teacher's that the student bans costs infinity, and has a gradient all the same.  A teacher that names nothing costs 0.  The named words' numbers are
- * formed in 64 bits, p_r from the words that are not named.
+ * formed in 64 bits, from the row's sums and the shares q_i as fp32 holds them; p_r comes from the words that are not named.
  */
 typedef struct {
     float scale;

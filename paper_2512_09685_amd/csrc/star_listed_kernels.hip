@@ -12,9 +12,9 @@
 // its words.  As sum p_i + p_r = 1, KL = sum q f(log p - log q) + Q - 1 with f(d) = e^d - d - 1, whose terms are never negative: where student and
 // teacher agree, errors enter squared.
 //
-// Bound by memory, a row read once and written once where it is held (8192 x 65536, bf16, 64 words: 360 us, 5.2 TB/s; without the list 346); short rows by the
-// list, which one wave puts together (16384 x 1000, 20 words: 40 us; 43 with ids and numbers asked for after the row and equal words looked
-// for by every entry's own chain).
+// Bound by memory, a row read once and written once where it is held (8192 x 65536, bf16, 64 words, a quarter of the rows written as zeros and not read: 360
+// us, 5.2 TB/s; without the list 346); short rows by the list, which one wave puts together (16384 x 1000, 20 words, all rows counting: 41 us, and 7 % more
+// with ids and numbers asked for after the row and equal words looked for by every entry's own chain).
 //
 // Alternatives.  With D the sum of all derivatives by log-probabilities, H' that by the entropy and E = sum e_j x_j / s:
 //     dz_j = sum_i d_i [j = i] - D p_j - H' p_j log 2 (x_j - E).
@@ -60,7 +60,7 @@ struct WordList {
     __align__(16) uint32_t marks[NT * MARKS];
     uint32_t edge_marks[4];                       // (fewer than 128 elements lie outside the chunks)
     float logit[kEntries], value[kEntries];       // value: what is written there
-    float q[kMostAlternatives], log_q[kMostAlternatives];
+    float q[kMostAlternatives], log_q[kMostAlternatives];   // (in fp32, as the sums behind p are: neither leaves p - q more digits than the other)
     Prelude given;
     float slope;                                  // of the words that are not named
 };
@@ -546,9 +546,9 @@ __global__ __launch_bounds__(kSumThreads) void distill_stats_kernel(const Logits
 }
 
 // Threads a row, by its chunks (us, this way / the other; bf16, distillation): one and two waves up to 128 and 512 chunks against four: 16384 x 1000, 20
-// words: 43 / 92, 16384 x 4000: 77 / 107; 4 chunks a thread up to 1024 against 8: 8192 x 8000, 64 words: 76 / 87; 8 up to 4096 against 16: 2048 x
-// 32000: 68 / 76; beyond, two rows a unit of 512 threads against one of 1024: 2000 x 131075: 220 / 241, 777 x 50021, fp32: 66 / 79.  More than 16 chunks a
-// thread held of long rows: 2048 x 40000, fp32, 16 / 18 / 20: 128 / 130 / 132, 2000 x 131075: 220 / 223 / 218.
+// words: 41 / 89, 16384 x 4000: 74 / 100; 4 chunks a thread up to 1024 against 8: 8192 x 8000, 64 words: 72 / 78; 8 up to 4096 against 16: 2048 x
+// 32000: 66 / 74; beyond, two rows a unit of 512 threads against one of 1024: 2000 x 131075: 212 / 230, 777 x 50021, fp32: 66 / 74.  More than 16 chunks a
+// thread held of long rows: 2048 x 40000, fp32, 16 / 18 / 20: 126 / 128 / 130, 2000 x 131075: 213 / 216 / 212.
 template <class E, Listed WORK, bool ENTROPY>
 void launch_listed_of(const ListedArgs& a, hipStream_t stream) {
     const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;

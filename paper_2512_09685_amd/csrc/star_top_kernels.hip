@@ -7,8 +7,9 @@
 //
 // One reading of the logits is all that it cannot do without.  Beside the memory it is the vector instructions that count: nine an element of a bf16
 // row (widen, multiply-add, exponential of two turns, two sums, the entropy's product and its guard, half a maximum), and what the lists cost a row.
-// 4096 x 131072, bf16, k = 64, a tenth of the rows without a target: 196 us, 4.9 TB/s, vector pipes busy 86 % (all rows
-// counting 206, without alternatives 178, without the entropy too 169; the scan for log-probabilities alone 160); 1023 x 50021, fp32, k = 5: 37 us, 5.5 TB/s.
+// 4096 x 131072, bf16, k = 64, a tenth of the rows without a target: 197 us, 4.9 TB/s, vector pipes busy 86 % (without the entropy 187, without
+// alternatives 168, without both 152; the scan for log-probabilities alone 148).  All rows counting: 210, 201, 180, 167 and 159.  1023 x 50021, fp32, k =
+// 5, all counting: 37 us, 5.5 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "star_logits.h"
@@ -98,7 +99,7 @@ __device__ void select_by_digits(const char* row, const RowSpan& sp, int k, KeyL
 }
 
 // A wave's chunks that hold a value that may be an alternative, as they were read, and the ids of their first words; `count` is the wave's, and may
-// be more than there is room for.  (A list a wave needs no atomics: 4096 x 131072, k = 64: 221 us, one list of the workgroup 235.)
+// be more than there is room for.  (A list a wave needs no atomics; one list of the workgroup took 6 % more for 4096 x 131072, k = 64.)
 constexpr int kHot = 128;
 struct HotChunks {
     u32x4 chunk[kHot];
@@ -178,7 +179,7 @@ __device__ __forceinline__ float bound_of(float& most, int k, float* shared, int
 template <class E, int NT, int H, bool ENTROPY>
 __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(const TopArgs a) {
     constexpr int WAVES = NT / 64, KEYS = NT >= 512 ? 1024 : NT == 256 ? 512 : 256, AHEAD = H == 16 && E::VEC == 8 ? 8 : 4;
-    constexpr bool LONG = H == 16;   // rows that are not held whole; the others' registers are not to pay for them (8192 x 8000, k = 20: 32 / 36 us)
+    constexpr bool LONG = H == 16;   // rows that are not held whole; the others' registers are not to pay for them (8192 x 8000, k = 20: 35 / 38 us)
     __shared__ float shared[4][WAVES];   // sum of the exponentials, that of the entropy, the whole row's maximum, the bound's: each written once
     __shared__ __align__(16) int steps[kSteps];
     __shared__ float bound;
@@ -326,10 +327,11 @@ __global__ __launch_bounds__(NT, H == 16 || NT == 64 ? 4 : 6) void top_kernel(co
 }
 
 // Threads a row, by its chunks: as few as hold it in registers up to 8192 chunks, two rows a unit at least (us, this way / the other; bf16):
-// one and two waves up to 128 and 512 chunks against four: 16384 x 1000, k = 20: 27 / 60, 16384 x 4000: 42 / 55; 4 chunks a thread up to 1024
-// against 8: 8192 x 8000: 35 / 48; 512 threads up to 4096 against 1024: 4096 x 32000: 57 / 68; beyond, 16 chunks a thread against 8 of 1024:
-// 4096 x 131072, k = 64: 242 / 279, and against 8 of 512, which hold half as much and list twice as many: 235 / 336 (k = 8, 2048 x 65536 with the
-// gradient: 163 / 156).
+// one and two waves up to 128 and 512 chunks against four: 16384 x 1000, k = 20: 27 / 58, 16384 x 4000: 41 / 54; 4 chunks a thread up to 1024
+// against 8: 8192 x 8000: 34 / 46; 512 threads up to 4096 against 1024: 4096 x 32000: 58 / 70; beyond, 16 chunks a thread against 8 of 1024:
+// 4096 x 131072, k = 64: 217 / 277.  Against 8 of 512, which leave room for a third row on a unit, but hold half as much and list twice as many words:
+// k = 64: 4096 x 131072: 217 / 224, 2048 x 65536: 63 / 64; k = 8: 194 / 173, 2048 x 65536 with the gradient 152 / 148; 1023 x 50021, fp32, k = 5: 37.3 /
+// 35.4.  (So the few alternatives of a server would do better with 8: the rule does not look at k.)
 template <class E, bool ENTROPY>
 void launch_top_of(const TopArgs& a, unsigned rows, hipStream_t stream) {
     const int64_t chunks = (a.l.vocab + E::VEC - 1) / E::VEC;

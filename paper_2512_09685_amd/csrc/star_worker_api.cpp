@@ -261,7 +261,8 @@ star_status star_top_logprobs(const void* logits, star_dtype dtype, int64_t toke
     STAR_CHECK(check_workspace(workspace, workspace_bytes, star_top_logprobs_workspace(dtype, tokens, vocab, k)));
     const star::Logits l = make_logits(logits, dtype, tokens, vocab, ld, targets, nullptr, temperature);
     // Taken tokens' log-probabilities are what a loss is made of: logits that the memory-side cache holds stay in it for its gradient (2048 x
-    // 65536, bf16, both calls: 139 against 156 us, 1000 x 50000, fp32: 100 / 116; a call alone loses a tenth, 1023 x 50021, fp32: 41.5 / 37.1).
+    // 65536, bf16, both calls: 149 against 156 us, a fifth masked 135 / 152, 1000 x 50000, fp32: 101 / 116).  A call that no gradient follows loses a
+    // tenth by it (1023 x 50021, fp32: 41.5 / 37.4), and one without targets that one does follow does not gain: no argument says which it is.
     const bool again = logp_out && tokens * vocab <= kCacheBytes / (int64_t)bytes_of(dtype);
     STAR_LAUNCH(star::launch_top(l, k, logp_out, entropy_out, lse_out, top_ids, top_logp, again, static_cast<hipStream_t>(hip_stream)));
     return STAR_OK;

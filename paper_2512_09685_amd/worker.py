@@ -282,8 +282,8 @@ def star_top_logprobs(logits, targets, logp_out, *, entropy_out=None, lse_out=No
 def star_top_logprobs_grad(logits, targets, dlogits, *, dlogp=None, dentropy=None, top_ids=None, dtop=None,
                            temperature: float = 1.0, stream=None) -> None:
     """``dlogits`` of a function whose derivatives are ``dlogp`` (by the taken tokens' log-probabilities) and ``dentropy``, float32
-    [tokens], and ``dtop`` (by the log-probabilities of the words ``top_ids``), float32 [tokens, k]; each may be None.  Any words
-    in any order; one outside the vocabulary does not count.  ``dlogits`` may be ``logits``."""
+    [tokens], and ``dtop`` (by the log-probabilities of the words ``top_ids``), float32 [tokens, k]; each may be None.  (A
+    derivative by the normaliser has no place here.)  Any words in any order; one outside the vocabulary does not count.  ``dlogits`` may be ``logits``."""
     lib = _library()
     head, out, device = _logits(logits, targets, dlogits)
     tokens = head[2]
@@ -301,7 +301,7 @@ def star_distill_loss(logits, teacher_ids, teacher_logp, stats_out, *, targets=N
     """Divergence of the student's ``logits`` from a teacher's alternatives (``teacher_ids`` int64 [tokens, k], ``teacher_logp``
     float32 [tokens, k], k up to 128, as ``star_top_logprobs`` gives them), the words not named taken together, or, with
     ``renormalise``, the named ones as the whole of the teacher; and, if ``dlogits`` is given, the gradient.  ``ce_coef`` adds
-    -log p of the ``targets``.  ``stats_out``: float32 [4]: loss, divergence, -log p, weight, each summed with ``scale *
+    -log p of the ``targets``, at the same ``temperature``.  ``stats_out``: float32 [4]: loss, divergence, -log p, weight, each summed with ``scale *
     weights``.  ``kl_out``: float32 [tokens].  ``scale``: None = 1 / tokens."""
     lib = _library()
     head, out, device = _logits(logits, targets, dlogits)
